@@ -321,6 +321,84 @@ tng_status tng_rosenbrock_value(const float* x_dev, uint64_t d, double* value_de
 /* w <- w - eta * v (the outer update of Eq. 1). */
 tng_status tng_sgd_update(float* w_dev, const float* v_dev, uint64_t d, float eta, void* stream);
 
+/* ---- training-layer operators: 8-bit linear layers and dropout ------------------------------- */
+/* Producers of gradients for layers of a network: a linear layer whose matrix products run in
+ * 8-bit integers, forward and backward, and dropout with a mask that is recomputed, never stored.
+ * They need no context.  The layer's weight gradient is fp32 with a row stride of the caller's, so
+ * it can be written straight into a worker's row of the gradients tng_step takes.
+ *
+ * Conventions.  Matrices are row-major, `ld*` is the row stride in elements.  Activations and
+ * gradients (x, y, dy, dx, residual) have a tng_dtype, any alignment of that type and any stride
+ * >= the row length; 16-byte aligned rows are fastest.  Codes (int8) start on a 16-byte boundary
+ * and their row stride is a multiple of 16 (tng_code_stride).  Scales, bias, dw, db are fp32.
+ * Rows and columns are below 2^31, contractions at most TNG_MAX_CONTRACTION long (the int32 sums
+ * are exact up to there).  A call with no rows succeeds: sums over the rows (dw, db, column scales and
+ * sums) are zero, and there is nothing else to write.  Outputs must not overlap inputs, except where stated. */
+typedef enum { TNG_F32 = 0, TNG_BF16 = 1, TNG_F16 = 2 } tng_dtype;
+
+/* Where random numbers come from: Philox4x32-10 with key (seed_lo, seed_hi) and counter
+ * (column / 4, row0 + row, layer + tag, step), tag 2^30 for rounding and 2^31 for dropout; word
+ * column % 4 belongs to the column, u = (word >> 8) 2^-24.  A number depends on the logical place
+ * alone, so a part of a batch (row0 = its first row) draws what the whole batch would, on any GPU,
+ * and never what tng_encode draws under the same key.  layer < 2^30, row0 + rows <= 2^32. */
+typedef struct {
+    uint32_t seed_lo, seed_hi, layer, step;
+    uint64_t row0;
+} tng_draw;
+
+#define TNG_MAX_CONTRACTION 131056
+/* Row stride of codes for lines of n values: n rounded up to 16. */
+size_t tng_code_stride(uint64_t n);
+
+/* Codes of a matrix, one scale a line.  With A = max|x| over the line, every operation one fp32
+ * rounding: scale = A/127, inv = 127/A, v = x inv; without a draw q = v rounded to the nearest integer
+ * (half to even), with one q = floor(v + u) cut to [-127, 127], so that E[q scale] = x up to
+ * rounding.  A < 2^-120: scale 0, codes 0.  A NaN or infinite: codes 0 and scale A/127, so that every
+ * product with the line is NaN.
+ * tng_quant8_rows: a line is a row (a scale per token); q is rows x cols.
+ * tng_quant8_cols: a line is a column (a scale per channel) and the codes come transposed: q is
+ *   cols x rows, so that a product can contract over the rows of x.  colsum (may be NULL) receives
+ *   the column sums of x in fp32.  scratch_dev: tng_quant8_cols_scratch_bytes, 256-byte aligned.
+ * Bytes between a line's end and the next multiple of 16 are written as zero. */
+tng_status tng_quant8_rows(const void* x_dev, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx,
+                           const tng_draw* draw, int8_t* q_dev, uint64_t ldq, float* scale_dev, void* stream);
+size_t tng_quant8_cols_scratch_bytes(uint64_t rows, uint64_t cols);
+tng_status tng_quant8_cols(const void* x_dev, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx,
+                           const tng_draw* draw, int8_t* q_dev, uint64_t ldq, float* scale_dev, float* colsum_dev,
+                           void* scratch_dev, void* stream);
+/* out[i][j] = (float(sum_l a[i][l] b[j][l]) sa[i]) sb[j] + bias[j]: i < m, j < n, l < k, the sum in
+ * int32, then fp32, one rounding to `type` at the end.  bias_dev may be NULL. */
+tng_status tng_product8(const int8_t* a_dev, uint64_t lda, const float* sa_dev, const int8_t* b_dev, uint64_t ldb,
+                        const float* sb_dev, const float* bias_dev, uint64_t m, uint64_t n, uint64_t k, void* out_dev,
+                        tng_dtype type, uint64_t ldo, void* stream);
+/* y = x W^T + bias for T tokens: codes of x by row (nearest), then the product with the codes of
+ * W (n x k, a scale per output channel: tng_quant8_rows of W).  y has x's type.  scratch_dev:
+ * tng_linear8_scratch_bytes, 256-byte aligned (codes and scales of x). */
+size_t tng_linear8_scratch_bytes(uint64_t tokens, uint64_t k);
+tng_status tng_linear8(const void* x_dev, tng_dtype type, uint64_t tokens, uint64_t k, uint64_t ldx, const int8_t* w_dev,
+                       uint64_t ldw, const float* sw_dev, uint64_t n, const float* bias_dev, void* y_dev, uint64_t ldy,
+                       void* scratch_dev, void* stream);
+/* Gradients of that layer from dy (T x n) and x (T x k), each output optional (NULL):
+ *   dx = dy W      codes of dy by row, wt = codes of W by column (k x n, a scale per INPUT channel:
+ *                  tng_quant8_cols of W); T x k, type of dy and x
+ *   dw = dy^T x    codes of dy and of x by column; n x k, fp32, row stride lddw
+ *   db = sum of dy over the tokens, fp32
+ * draw (NULL = nearest) rounds dy stochastically, so that dx and dw are unbiased given the other
+ * factor's codes; x is always rounded to nearest.  x_dev may be NULL when dw_dev is, wt_dev and
+ * swt_dev when dx_dev is.  scratch_dev: tng_linear8_grad_scratch_bytes, 256-byte aligned. */
+size_t tng_linear8_grad_scratch_bytes(uint64_t tokens, uint64_t k, uint64_t n);
+tng_status tng_linear8_grad(const void* dy_dev, uint64_t lddy, const void* x_dev, uint64_t ldx, tng_dtype type,
+                            uint64_t tokens, uint64_t k, uint64_t n, const int8_t* wt_dev, uint64_t ldwt,
+                            const float* swt_dev, const tng_draw* draw, void* dx_dev, uint64_t lddx, float* dw_dev,
+                            uint64_t lddw, float* db_dev, void* scratch_dev, void* stream);
+/* y = residual + (u >= p ? x / (1 - p) : 0), p in [0, 1], the quotient as x times the fp32 value of
+ * 1 / (1 - p); residual_dev may be NULL.  A dropped x contributes nothing, NaN and infinity included.
+ * The gradient with respect to x is the same call on dy without a residual and with the same draw; the
+ * gradient with respect to the residual is dy.  y may be x or residual itself (same stride). */
+tng_status tng_dropout(const void* x_dev, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx,
+                       const void* residual_dev, uint64_t ldr, float p, const tng_draw* draw, void* y_dev, uint64_t ldy,
+                       void* stream);
+
 #ifdef __cplusplus
 }
 #endif

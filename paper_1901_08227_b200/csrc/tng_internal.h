@@ -29,6 +29,8 @@ template <typename T>
 struct PerDevice {
     T v[kMaxDevices] = {};
 };
+// SM count of the current device (asked once per device index).
+int sm_count_now();
 
 // Small device-resident block: fusion statistics, coefficients, flags.
 struct FuseBlock {
@@ -96,5 +98,21 @@ cudaError_t launch_encode(const CodecGeom& g, uint32_t m_base, const float* grad
 // means: the M scalar references (read in TNG_NORM_MEAN only)
 cudaError_t launch_decode(const CodecGeom& g, const uint32_t* codes, const float* scales, const float* means, const float* ref,
                           const float* ref2, float* out_a, float* out_b, FuseBlock* fb, int sm_count, cudaStream_t st, int* launches);
+
+// ---- training-layer operators (tng_quant8.cu, tng_product8.cu) -----------------------
+cudaError_t launch_quant8_rows(const void* x, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx, const tng_draw* draw,
+                               int8_t* q, uint64_t ldq, float* scale, cudaStream_t st);
+cudaError_t launch_quant8_cols(const void* x, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx, const tng_draw* draw,
+                               int8_t* q, uint64_t ldq, float* scale, float* colsum, void* scratch, cudaStream_t st);
+struct Product8 {
+    const int8_t *a, *b;
+    uint64_t lda, ldb;
+    const float *sa, *sb, *bias;    // bias may be nullptr
+    uint64_t m, n, k;
+    void* out;
+    tng_dtype type;
+    uint64_t ldo;
+};
+cudaError_t launch_product8(const Product8& p, cudaStream_t st);
 
 }  // namespace tng

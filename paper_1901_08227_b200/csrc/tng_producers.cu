@@ -8,6 +8,20 @@
 #include "tng_internal.h"
 
 namespace tng {
+
+int sm_count_now() {
+    static PerDevice<int> cached;
+    const int slot = device_slot();
+    if (slot >= 0 && cached.v[slot] > 0) return cached.v[slot];
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) {
+        (void)cudaGetLastError();
+        sms = 1;
+    }
+    if (slot >= 0) cached.v[slot] = sms;
+    return sms;
+}
+
 namespace {
 
 constexpr int kMaxRowChunks = 64;
@@ -180,20 +194,6 @@ __global__ void __launch_bounds__(256) sgd_update_kernel(float* __restrict__ w, 
 // Row chunks of the transposed product: enough CTAs to fill the GPU (4 per SM), and, when a
 // count up to the limit exists, a total that is a multiple of the SM count so that no SM gets
 // one CTA more than another.
-// SM count of the current device (asked once per device index).
-int sm_count_now() {
-    static PerDevice<int> cached;
-    const int slot = device_slot();
-    if (slot >= 0 && cached.v[slot] > 0) return cached.v[slot];
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) {
-        (void)cudaGetLastError();
-        sms = 1;
-    }
-    if (slot >= 0) cached.v[slot] = sms;
-    return sms;
-}
-
 int row_chunks(uint64_t n, uint64_t d, bool vec) {
     const uint64_t colblocks = ((vec ? d / 4 : d) + 255) / 256;
     const uint64_t sms = (uint64_t)sm_count_now();

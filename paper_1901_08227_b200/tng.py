@@ -28,6 +28,8 @@ EXPORTS = [
     "tng_logistic_scratch_floats", "tng_logistic_grad", "tng_logistic_loss", "tng_rosenbrock_grad",
     "tng_rosenbrock_value", "tng_sgd_update", "tng_gram_static", "tng_state_bytes", "tng_save_state", "tng_load_state",
     "tng_selftest_bounded_wait", "tng_fuse_local", "tng_local_stats", "tng_local_stats_all", "tng_fuse_finish", "tng_encode_local", "tng_decode_commit",
+    "tng_code_stride", "tng_quant8_rows", "tng_quant8_cols_scratch_bytes", "tng_quant8_cols", "tng_product8", "tng_linear8_scratch_bytes",
+    "tng_linear8", "tng_linear8_grad_scratch_bytes", "tng_linear8_grad", "tng_dropout",
 ]
 
 
@@ -42,6 +44,17 @@ class Stats(C.Structure):
         ("ms_dots", C.c_double), ("ms_solve", C.c_double), ("ms_combine", C.c_double),
         ("ms_encode", C.c_double), ("ms_decode", C.c_double),
     ]
+
+
+class Draw(C.Structure):
+    """tng_draw: where an operator's random numbers come from (seed, layer, step, first row)."""
+    _fields_ = [("seed_lo", C.c_uint32), ("seed_hi", C.c_uint32), ("layer", C.c_uint32), ("step", C.c_uint32),
+                ("row0", C.c_uint64)]
+
+    def __init__(self, seed=0, layer=0, step=0, row0=0):
+        if not (0 <= seed < 1 << 64 and 0 <= layer < 1 << 30 and 0 <= step < 1 << 32 and 0 <= row0 <= 1 << 32):
+            raise ValueError("seed, layer, step and row0 are unsigned of 64, 30, 32 and 32 bits")
+        super().__init__(seed & 0xFFFFFFFF, seed >> 32, layer, step, row0)
 
 
 class TngError(RuntimeError):
@@ -100,6 +113,17 @@ def lib():
         L.tng_fuse_finish.argtypes = [vp, vp]
         L.tng_encode_local.argtypes = [vp, vp, u64, u32, u32, u32, vp]
         L.tng_decode_commit.argtypes = [vp, vp, vp]
+        draw, st = C.POINTER(Draw), C.c_size_t
+        L.tng_code_stride.argtypes, L.tng_code_stride.restype = [u64], st
+        L.tng_quant8_rows.argtypes = [vp, C.c_int, u64, u64, u64, draw, vp, u64, vp, vp]
+        L.tng_quant8_cols_scratch_bytes.argtypes, L.tng_quant8_cols_scratch_bytes.restype = [u64, u64], st
+        L.tng_quant8_cols.argtypes = [vp, C.c_int, u64, u64, u64, draw, vp, u64, vp, vp, vp, vp]
+        L.tng_product8.argtypes = [vp, u64, vp, vp, u64, vp, vp, u64, u64, u64, vp, C.c_int, u64, vp]
+        L.tng_linear8_scratch_bytes.argtypes, L.tng_linear8_scratch_bytes.restype = [u64, u64], st
+        L.tng_linear8.argtypes = [vp, C.c_int, u64, u64, u64, vp, u64, vp, u64, vp, vp, u64, vp, vp]
+        L.tng_linear8_grad_scratch_bytes.argtypes, L.tng_linear8_grad_scratch_bytes.restype = [u64, u64, u64], st
+        L.tng_linear8_grad.argtypes = [vp, u64, vp, u64, C.c_int, u64, u64, u64, vp, u64, vp, draw, vp, u64, vp, u64, vp, vp, vp]
+        L.tng_dropout.argtypes = [vp, C.c_int, u64, u64, u64, vp, u64, f32, draw, vp, u64, vp]
         L.tng_gram_static.argtypes = [C.POINTER(vp), u32, u64, vp, u32, u64, vp, vp]
         _lib = L
     return _lib
@@ -386,3 +410,144 @@ def rosenbrock_value(x, value):
 def sgd_update(w, v, eta):
     _check(lib().tng_sgd_update(_dev(w), _dev(v), w.numel(), float(eta), _stream()), "tng_sgd_update")
     return w
+
+
+# ---- training-layer operators ------------------------------------------------------------
+F32, BF16, F16 = 0, 1, 2
+_DTYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _matrix(t, name, dtype=None, shape=None):
+    """A 2-D CUDA tensor of the current device with unit column stride -> (pointer, row stride)."""
+    if not t.is_cuda or t.dim() != 2 or (t.dtype not in _DTYPE if dtype is None else t.dtype != dtype):
+        raise TypeError(f"{name} must be a 2-D CUDA tensor of type {dtype or 'float32, bfloat16 or float16'}")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    rows, cols = t.shape
+    ld, unit = t.stride()
+    if unit != 1 and cols != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), ld if rows > 1 else max(cols, ld)
+
+
+def _codes(t, name, shape=None):
+    p, ld = _matrix(t, name, torch.int8, shape)
+    return p, ld if ld % 16 == 0 or t.shape[0] > 1 else -(-ld // 16) * 16
+
+
+def _vector(t, name, n, dtype=torch.float32):
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise TypeError(f"{name} must be a contiguous CUDA {dtype} vector of {n} elements")
+    return t.data_ptr()
+
+
+def _scratch(buf, nbytes, device):
+    if buf is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if not buf.is_cuda or not buf.is_contiguous() or buf.numel() * buf.element_size() < nbytes:
+        raise ValueError(f"scratch must be a contiguous CUDA tensor of at least {nbytes} bytes")
+    return buf
+
+
+def _draw_ref(draw):
+    return None if draw is None else C.byref(draw)
+
+
+def empty_codes(lines, n, device="cuda"):
+    """Uninitialised codes of `lines` lines of n values, each line on a 16-byte boundary."""
+    return torch.empty((lines, -(-n // 16) * 16), dtype=torch.int8, device=device)[:, :n]
+
+
+def quant8_rows(x, draw=None, q=None, scale=None):
+    """Codes of x by row and a scale per row: (rows, cols) int8, (rows,) float32."""
+    p, ld = _matrix(x, "x")
+    rows, cols = x.shape
+    q = empty_codes(rows, cols, x.device) if q is None else q
+    scale = torch.empty(rows, device=x.device) if scale is None else scale
+    pq, ldq = _codes(q, "q", (rows, cols))
+    _check(lib().tng_quant8_rows(p, _DTYPE[x.dtype], rows, cols, ld, _draw_ref(draw), pq, ldq, _vector(scale, "scale", rows), _stream()),
+           "tng_quant8_rows")
+    return q, scale
+
+
+def quant8_cols(x, draw=None, q=None, scale=None, colsum=None, scratch=None):
+    """Codes of x by column, transposed, and a scale per column: (cols, rows) int8, (cols,) float32.
+    `colsum` (cols float32) receives the column sums of x."""
+    p, ld = _matrix(x, "x")
+    rows, cols = x.shape
+    q = empty_codes(cols, rows, x.device) if q is None else q
+    scale = torch.empty(cols, device=x.device) if scale is None else scale
+    pq, ldq = _codes(q, "q", (cols, rows))
+    buf = _scratch(scratch, lib().tng_quant8_cols_scratch_bytes(rows, cols), x.device)
+    _check(lib().tng_quant8_cols(p, _DTYPE[x.dtype], rows, cols, ld, _draw_ref(draw), pq, ldq, _vector(scale, "scale", cols),
+                                 _vector(colsum, "colsum", cols), buf.data_ptr(), _stream()), "tng_quant8_cols")
+    return q, scale
+
+
+def product8(a, sa, b, sb, bias=None, dtype=torch.bfloat16, out=None):
+    """out[i, j] = sum_l a[i, l] b[j, l] * sa[i] * sb[j] + bias[j]; a (m, k) and b (n, k) int8 codes."""
+    m, k = a.shape
+    n = b.shape[0]
+    pa, lda = _codes(a, "a")
+    pb, ldb = _codes(b, "b", (n, k))
+    if out is None:
+        out = torch.empty((m, n), dtype=dtype, device=a.device)
+    po, ldo = _matrix(out, "out", None, (m, n))
+    _check(lib().tng_product8(pa, lda, _vector(sa, "sa", m), pb, ldb, _vector(sb, "sb", n), _vector(bias, "bias", n), m, n, k,
+                              po, _DTYPE[out.dtype], ldo, _stream()), "tng_product8")
+    return out
+
+
+def linear8(x, w, sw, bias=None, out=None, scratch=None):
+    """y = x W^T + bias with x (tokens, k) coded by token in the call and W held as codes (n, k) with a
+    scale per output channel (`quant8_rows` of W).  y has x's type."""
+    px, ldx = _matrix(x, "x")
+    tokens, k = x.shape
+    n = w.shape[0]
+    pw, ldw = _codes(w, "w", (n, k))
+    if out is None:
+        out = torch.empty((tokens, n), dtype=x.dtype, device=x.device)
+    po, ldo = _matrix(out, "out", x.dtype, (tokens, n))
+    buf = _scratch(scratch, lib().tng_linear8_scratch_bytes(tokens, k), x.device)
+    _check(lib().tng_linear8(px, _DTYPE[x.dtype], tokens, k, ldx, pw, ldw, _vector(sw, "sw", n), n, _vector(bias, "bias", n), po, ldo,
+                             buf.data_ptr(), _stream()), "tng_linear8")
+    return out
+
+
+def linear8_grad(dy, x, wt, swt, draw=None, dx=None, dw=None, db=None, scratch=None):
+    """Gradients of y = x W^T + bias: (dx, dw, db) from dy (tokens, n) and x (tokens, k).  `wt` (k, n) and
+    `swt` (k) hold W by column (`quant8_cols` of W); with `draw` dy is rounded stochastically.  `dw` may be a
+    strided float32 view, such as a part of a worker's row of gradients."""
+    py, ldy = _matrix(dy, "dy")
+    tokens, n = dy.shape
+    k = x.shape[1]
+    px, ldx = _matrix(x, "x", dy.dtype, (tokens, k))
+    pw, ldw = _codes(wt, "wt", (k, n))
+    dx = torch.empty((tokens, k), dtype=dy.dtype, device=dy.device) if dx is None else dx
+    dw = torch.empty((n, k), device=dy.device) if dw is None else dw
+    db = torch.empty(n, device=dy.device) if db is None else db
+    pdx, lddx = _matrix(dx, "dx", dy.dtype, (tokens, k))
+    pdw, lddw = _matrix(dw, "dw", torch.float32, (n, k))
+    buf = _scratch(scratch, lib().tng_linear8_grad_scratch_bytes(tokens, k, n), dy.device)
+    _check(lib().tng_linear8_grad(py, ldy, px, ldx, _DTYPE[dy.dtype], tokens, k, n, pw, ldw, _vector(swt, "swt", k), _draw_ref(draw),
+                                  pdx, lddx, pdw, lddw, _vector(db, "db", n), buf.data_ptr(), _stream()), "tng_linear8_grad")
+    return dx, dw, db
+
+
+def dropout(x, p, draw, residual=None, out=None):
+    """residual + dropout(x): kept elements are scaled by 1/(1-p); the mask follows from `draw` alone."""
+    px, ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    if out is None:
+        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    po, ldo = _matrix(out, "out", x.dtype, (rows, cols))
+    pr, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, (rows, cols))
+    _check(lib().tng_dropout(px, _DTYPE[x.dtype], rows, cols, ldx, pr, ldr, p, _draw_ref(draw), po, ldo, _stream()), "tng_dropout")
+    return out
+
+
+def dropout_grad(dy, p, draw, out=None):
+    """Gradient of `dropout` with respect to x (with respect to the residual it is dy itself)."""
+    return dropout(dy, p, draw, None, out)
