@@ -1,61 +1,482 @@
 // Products of 8-bit codes with scales for each row of either side:
 //   out[i][j] = (float(sum_l a[i][l] b[j][l]) sa[i]) sb[j] + bias[j].
+//
+// The int32 sums are exact, so every variant below gives the same bits whatever order it sums in.
+#include <math_constants.h>
+
 #include "tng_layers.cuh"
+#include "tng_umma.cuh"
 
 namespace tng {
 namespace {
 
-__device__ __forceinline__ float scaled(int acc, float sa, float sb, float bias) {
-    return __fadd_rn(__fmul_rn(__fmul_rn((float)acc, sa), sb), bias);
+// A bounded wait gave up: the sums are incomplete and every output the CTA still owes becomes NaN, which is how
+// a call that never waits for the GPU reports it.
+__device__ __forceinline__ float scaled(int acc, float sa, float sb, bool has_bias, float bias) {
+    const float v = __fmul_rn(__fmul_rn((float)acc, sa), sb);
+    return has_bias ? __fadd_rn(v, bias) : v;
 }
 
-// Four codes starting at l, zero beyond k (l is a multiple of 4, rows are padded to 16 bytes).
-__device__ __forceinline__ int word4(const int8_t* row, uint64_t l, uint64_t k) {
-    if (l >= k) return 0;
-    uint32_t w = *reinterpret_cast<const uint32_t*>(row + l);
-    if (l + 4 > k) w &= (1u << (8 * (k - l))) - 1u;
-    return (int)w;
+__device__ __forceinline__ void st_global_v8(void* p, const uint32_t (&w)[8]) {   // 32-byte aligned
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
 
-// 64 x 64 outputs a CTA, 4 x 4 a thread, 64 codes of the contraction at a time.
+// 32 consecutive outputs of one row per lane.  `align` = what the output's rows are aligned to (32, 16 or less).
+// Where the rows are not aligned, or the tile ends inside the 32 columns, the values cross the warp through its
+// staging area (32 x 33 words), so that stores run along a row.
 template <typename T>
-__global__ void __launch_bounds__(256) product8_tile_kernel(Product8 p) {
-    __shared__ int sa[16][65], sb[16][65];
-    const uint64_t i0 = (uint64_t)blockIdx.y * 64, j0 = (uint64_t)blockIdx.x * 64;
-    const uint32_t tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    int acc[4][4] = {};
-    for (uint64_t l0 = 0; l0 < p.k; l0 += 64) {
+__device__ __forceinline__ void store_chunk(T* out, uint64_t ldo, uint64_t row0, uint64_t rows, uint64_t col, uint64_t cols, const float (&v)[32],
+                                            uint32_t align, float* stage, uint32_t lane) {
+    if (align >= 16 && col + 32 <= cols) {
+        if (row0 + lane >= rows) return;
+        T* p = out + (row0 + lane) * ldo + col;
+        constexpr int kPer = 32 / (int)sizeof(T);          // elements in 32 bytes
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const uint32_t r = ty + 16 * h;
-            sa[tx][r] = i0 + r < p.m ? word4(p.a + (i0 + r) * p.lda, l0 + 4 * tx, p.k) : 0;
-            sb[tx][r] = j0 + r < p.n ? word4(p.b + (j0 + r) * p.ldb, l0 + 4 * tx, p.k) : 0;
+        for (int i = 0; i < 32 / kPer; ++i) {
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (sizeof(T) == 4) w[j] = __float_as_uint(v[i * 8 + j]);
+                else w[j] = pack2<T>(v[i * 16 + 2 * j], v[i * 16 + 2 * j + 1]);
+            }
+            if (align >= 32) {
+                st_global_v8(p + i * kPer, w);
+            } else {
+                reinterpret_cast<uint4*>(p + i * kPer)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                reinterpret_cast<uint4*>(p + i * kPer)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            }
         }
-        __syncthreads();
+    } else {
 #pragma unroll
-        for (int w = 0; w < 16; ++w)
-#pragma unroll
-            for (int y = 0; y < 4; ++y)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) acc[y][x] = __dp4a(sa[w][ty * 4 + y], sb[w][tx * 4 + x], acc[y][x]);
-        __syncthreads();
+        for (int j = 0; j < 32; ++j) stage[lane * 33 + j] = v[j];
+        __syncwarp();
+        const uint32_t n = rows <= row0 ? 0u : (rows - row0 < 32 ? (uint32_t)(rows - row0) : 32u);
+        if (col + lane < cols)
+            for (uint32_t r = 0; r < n; ++r) out[(row0 + r) * ldo + col + lane] = from_f32<T>(stage[r * 33 + lane]);
+        __syncwarp();
     }
-    for (int y = 0; y < 4; ++y)
-        for (int x = 0; x < 4; ++x) {
-            const uint64_t i = i0 + ty * 4 + y, j = j0 + tx * 4 + x;
-            if (i < p.m && j < p.n)
-                static_cast<T*>(p.out)[i * p.ldo + j] = from_f32<T>(scaled(acc[y][x], p.sa[i], p.sb[j], p.bias ? p.bias[j] : 0.f));
+}
+
+// ---- pairs of CTAs: 256 x NT outputs a tile -------------------------------------------------------------
+// Two CTAs (two SMs) work on one tile: each holds 128 rows of a and NT/2 rows of b per stage, and the matrix
+// instruction of the even CTA reads both shared memories; the accumulators are 128 rows x NT columns in each
+// CTA's tensor memory, twice, so that one tile is written out while the next is summed.  A pair reads
+// 128 + NT/2 rows of operands per CTA for 128 NT outputs: half of what two single CTAs would read.
+// Warps: 0-7 write out (a quarter of the rows and half of the columns each), 8 feeds, 9 issues.
+constexpr int kPairThreads = 320;
+constexpr uint32_t kStageStride = 32 * 33 * 4;             // staging of one warp
+template <int NT> struct PairGeom {
+    static constexpr uint32_t kA = 128 * 128, kB = NT / 2 * 128, kStage = kA + kB;
+    static constexpr uint32_t kStages = NT == 256 ? 6 : 8;
+    static constexpr uint32_t kSmem = 1024 + kStages * kStage + 8 * kStageStride + 256;
+};
+
+struct TileWalk {                                          // tile order: groups of eight tile rows, columns outside
+    uint32_t tiles_m, tiles_n;
+    __device__ __forceinline__ void at(uint32_t t, uint32_t& tm, uint32_t& tn) const {
+        const uint32_t per = 8 * tiles_n, g = t / per, first = g * 8;
+        const uint32_t rows = tiles_m - first < 8 ? tiles_m - first : 8, r = t - g * per;
+        tn = r / rows;
+        tm = first + (r - tn * rows);
+    }
+};
+
+template <int NT, typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+    product8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Product8 p,
+                         uint32_t align) {
+    using G = PairGeom<NT>;
+    extern __shared__ unsigned char dyn[];
+    __shared__ uint32_t sh_tmem;
+    __shared__ volatile uint32_t sh_failed;
+    const uint32_t data = (smem_u32(dyn) + 1023u) & ~1023u;
+    float* staging = reinterpret_cast<float*>(dyn + (data - smem_u32(dyn)) + G::kStages * G::kStage);
+    const uint32_t bars = data + G::kStages * G::kStage + 8 * kStageStride;
+    const auto full = [&](uint32_t s) { return bars + 16u * s; };
+    const auto empty = [&](uint32_t s) { return bars + 16u * s + 8u; };
+    const uint32_t acc_full = bars + 16u * G::kStages, acc_empty = acc_full + 16u, drain = acc_full + 32u;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
+    const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const uint32_t kblocks = (uint32_t)((p.k + 127) / 128);
+    const TileWalk walk{(uint32_t)((p.m + 255) / 256), (uint32_t)((p.n + NT - 1) / NT)};
+    const uint32_t tiles = walk.tiles_m * walk.tiles_n;
+
+    if (threadIdx.x == 0) {
+        sh_failed = 0;
+        for (uint32_t s = 0; s < G::kStages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
         }
+        for (uint32_t i = 0; i < 2; ++i) {
+            mbar_init(acc_full + 8 * i, 1);
+            mbar_init(acc_empty + 8 * i, 16);              // eight warps of either CTA
+        }
+        mbar_init(drain, 1);
+        mbar_init_fence();
+        map_prefetch(&map_a);
+        map_prefetch(&map_b);
+    }
+    if (warp == 9) tmem_alloc<2>(smem_u32(&sh_tmem), 2 * NT);
+    umma_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    umma_fence_after();
+    const uint32_t tmem = sh_tmem;
+
+    if (warp == 8 && lane == 0) {
+        // ---- feed: this CTA's rows of either operand, completion counted on the even CTA's barrier
+        uint32_t it = 0;
+        bool ok = true;
+        for (uint32_t t = pair; t < tiles && ok; t += pairs) {
+            uint32_t tm, tn;
+            walk.at(t, tm, tn);
+            const int32_t ya = (int32_t)(tm * 256 + rank * 128), yb = (int32_t)(tn * NT + rank * (NT / 2));
+            for (uint32_t kb = 0; kb < kblocks; ++kb, ++it) {
+                const uint32_t s = it % G::kStages, use = it / G::kStages;
+                if (use > 0 && !mbar_wait_cluster(empty(s), (use - 1) & 1u)) { ok = false; break; }
+                if (rank == 0) mbar_expect_tx(full(s), 2 * G::kStage);
+                const uint32_t dst = data + s * G::kStage, bar = cluster_map(full(s), 0);
+                tile_load<2>(dst, &map_a, (int32_t)(kb * 128), ya, bar);
+                tile_load<2>(dst + G::kA, &map_b, (int32_t)(kb * 128), yb, bar);
+            }
+        }
+        if (!ok) {                                         // the odd CTA cannot see its copies land: leave them a millisecond
+            sh_failed = 1;
+            for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        }
+        // no CTA of the pair may leave before its copies have landed
+        if (rank == 0)
+            for (uint32_t j = it > G::kStages ? it - G::kStages : 0; j < it; ++j) (void)mbar_wait_cluster(full(j % G::kStages), (j / G::kStages) & 1u);
+    } else if (warp == 9 && lane == 0 && rank == 0) {
+        // ---- issue
+        constexpr uint32_t idesc = umma_idesc_s8(256, NT);
+        uint32_t it = 0, n_acc = 0;
+        bool ok = true;
+        for (uint32_t t = pair; t < tiles && ok; t += pairs, ++n_acc) {
+            const uint32_t acc = n_acc & 1u, use = n_acc >> 1;
+            if (use > 0 && !mbar_wait_cluster(acc_empty + 8 * acc, (use - 1) & 1u)) { ok = false; break; }
+            umma_fence_after();
+            for (uint32_t kb = 0; kb < kblocks; ++kb, ++it) {
+                const uint32_t s = it % G::kStages;
+                if (!mbar_wait_cluster(full(s), (it / G::kStages) & 1u)) { ok = false; break; }
+                umma_fence_after();
+                const uint64_t da = umma_desc(data + s * G::kStage), db = umma_desc(data + s * G::kStage + G::kA);
+                const uint64_t left = p.k - (uint64_t)kb * 128;
+                const uint32_t steps = left >= 128 ? 4u : (uint32_t)((left + 31) / 32);
+                for (uint32_t j = 0; j < steps; ++j) umma_s8<2>(tmem + acc * NT, da + 2 * j, db + 2 * j, idesc, kb > 0 || j > 0);
+                umma_commit<2>(empty(s));
+            }
+            if (ok) umma_commit<2>(acc_full + 8 * acc);
+        }
+        if (!ok) {
+            sh_failed = 1;
+            umma_commit<2>(drain);
+            (void)mbar_wait_cluster(drain, 0);
+        }
+    } else if (warp < 8) {
+        // ---- write out: rows 32 (warp % 4) + lane of this CTA's 128, columns of the half warp / 4
+        float* stage = staging + warp * (kStageStride / 4);
+        T* out = static_cast<T*>(p.out);
+        uint32_t n_acc = 0;
+        bool ok = true;
+        for (uint32_t t = pair; t < tiles; t += pairs, ++n_acc) {
+            const uint32_t acc = n_acc & 1u, use = n_acc >> 1;
+            uint32_t tm, tn;
+            walk.at(t, tm, tn);
+            const uint64_t row0 = (uint64_t)tm * 256 + rank * 128 + (warp & 3) * 32;
+            const uint64_t col0 = (uint64_t)tn * NT + (warp >> 2) * (NT / 2);
+            const float sa = row0 + lane < p.m ? __ldg(p.sa + row0 + lane) : 0.f;
+            if (ok && !mbar_wait_cluster(acc_full + 8 * acc, use & 1u)) ok = false;
+            ok = __all_sync(kFullMask, ok && !sh_failed);
+            umma_fence_after();
+#pragma unroll 1
+            for (uint32_t ch = 0; ch < NT / 64; ++ch) {
+                const uint64_t col = col0 + ch * 32;
+                uint32_t r[32];
+                if (ok) {
+                    tmem_ld32(tmem + (((warp & 3) * 32) << 16) + acc * NT + (warp >> 2) * (NT / 2) + ch * 32, r);
+                }
+                const bool in = col + lane < p.n;
+                stage[lane] = in ? __ldg(p.sb + col + lane) : 0.f;
+                stage[32 + lane] = in && p.bias ? __ldg(p.bias + col + lane) : 0.f;
+                __syncwarp();
+                if (ok) tmem_wait_ld();
+                if (ch == NT / 64 - 1) {                   // everything read: the next tile may overwrite it
+                    umma_fence_before();
+                    __syncwarp();
+                    if (lane == 0) cluster_arrive(cluster_map(acc_empty + 8 * acc, 0));
+                }
+                float v[32];
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    const float4 sb = *reinterpret_cast<const float4*>(stage + j), bi = *reinterpret_cast<const float4*>(stage + 32 + j);
+                    v[j] = scaled((int)r[j], sa, sb.x, p.bias, bi.x);
+                    v[j + 1] = scaled((int)r[j + 1], sa, sb.y, p.bias, bi.y);
+                    v[j + 2] = scaled((int)r[j + 2], sa, sb.z, p.bias, bi.z);
+                    v[j + 3] = scaled((int)r[j + 3], sa, sb.w, p.bias, bi.w);
+                }
+                if (!ok) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = CUDART_NAN_F;
+                }
+                __syncwarp();
+                if (col < p.n) store_chunk<T>(out, p.ldo, row0, p.m, col, p.n, v, align, stage, lane);
+            }
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    cluster_sync_all();
+    if (warp == 9) tmem_free<2>(tmem, 2 * NT);
+}
+
+// ---- few rows: 128 x NT tiles, the contraction split over a cluster ------------------------------------
+// The 128 rows are rows of b, the NT columns rows of a (tokens): with few tokens the weights are the long side, and an
+// output row then runs along the lanes.  The CTAs of a cluster take consecutive parts of the contraction, leave
+// their int32 sums in shared memory and each write out a part of the columns, summed over the cluster's shared
+// memories.  Warps: 0-3 write out, 4 feeds, 5 issues.
+constexpr int kSlimThreads = 192;
+template <int NT> struct SlimGeom {
+    static constexpr uint32_t kA = 128 * 128, kB = NT * 128, kStage = kA + kB;
+    static constexpr uint32_t kStages = NT == 128 ? 3 : 4;
+    static constexpr uint32_t kColumns = NT < 32 ? 32 : NT;
+    static constexpr uint32_t kSmem = 1024 + kStages * kStage + 256;
+    static_assert(kStages * kStage >= 128 * NT * 4, "the stages also hold the sums");
+};
+
+template <int NT, typename T>
+__global__ void __launch_bounds__(kSlimThreads)
+    product8_slim_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ Product8 p,
+                         uint32_t split, uint32_t tiles_n) {
+    using G = SlimGeom<NT>;
+    extern __shared__ unsigned char dyn[];
+    __shared__ uint32_t sh_tmem;
+    __shared__ volatile uint32_t sh_failed;
+    const uint32_t data = (smem_u32(dyn) + 1023u) & ~1023u;
+    int* sums = reinterpret_cast<int*>(dyn + (data - smem_u32(dyn)));
+    const uint32_t bars = data + G::kStages * G::kStage;
+    const auto full = [&](uint32_t s) { return bars + 16u * s; };
+    const auto empty = [&](uint32_t s) { return bars + 16u * s + 8u; };
+    const uint32_t acc_full = bars + 16u * G::kStages, drain = acc_full + 8u;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t part = blockIdx.x % split, tile = blockIdx.x / split;
+    const uint32_t tm = tile / tiles_n, tn = tile - tm * tiles_n;
+    const uint32_t kblocks = (uint32_t)((p.k + 127) / 128);
+    const uint32_t kb0 = (uint32_t)((uint64_t)kblocks * part / split), kb1 = (uint32_t)((uint64_t)kblocks * (part + 1) / split);
+    const uint32_t n = kb1 - kb0;
+
+    if (threadIdx.x == 0) {
+        sh_failed = 0;
+        for (uint32_t s = 0; s < G::kStages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        mbar_init(acc_full, 1);
+        mbar_init(drain, 1);
+        mbar_init_fence();
+    }
+    if (warp == 5) tmem_alloc<1>(smem_u32(&sh_tmem), G::kColumns);
+    umma_fence_before();
+    __syncthreads();
+    umma_fence_after();
+    const uint32_t tmem = sh_tmem;
+
+    if (warp == 4 && lane == 0) {
+        const int32_t yb = (int32_t)(tn * 128), ya = (int32_t)(tm * NT);
+        uint32_t i = 0;
+        for (; i < n; ++i) {
+            const uint32_t s = i % G::kStages, use = i / G::kStages;
+            if (use > 0 && !mbar_wait(empty(s), (use - 1) & 1u)) { sh_failed = 1; break; }
+            mbar_expect_tx(full(s), G::kStage);
+            const uint32_t dst = data + s * G::kStage;
+            tile_load<1>(dst, &map_b, (int32_t)((kb0 + i) * 128), yb, full(s));
+            tile_load<1>(dst + G::kA, &map_a, (int32_t)((kb0 + i) * 128), ya, full(s));
+        }
+        for (uint32_t j = i > G::kStages ? i - G::kStages : 0; j < i; ++j) (void)mbar_wait(full(j % G::kStages), (j / G::kStages) & 1u);
+    } else if (warp == 5 && lane == 0) {
+        constexpr uint32_t idesc = umma_idesc_s8(128, NT);
+        bool ok = true;
+        for (uint32_t i = 0; i < n; ++i) {
+            const uint32_t s = i % G::kStages;
+            if (!mbar_wait(full(s), (i / G::kStages) & 1u)) { ok = false; break; }
+            umma_fence_after();
+            const uint64_t db = umma_desc(data + s * G::kStage), da = umma_desc(data + s * G::kStage + G::kA);
+            const uint64_t left = p.k - (uint64_t)(kb0 + i) * 128;
+            const uint32_t steps = left >= 128 ? 4u : (uint32_t)((left + 31) / 32);
+            for (uint32_t j = 0; j < steps; ++j) umma_s8<1>(tmem, db + 2 * j, da + 2 * j, idesc, i > 0 || j > 0);
+            umma_commit<1>(empty(s));
+        }
+        if (!ok) {
+            sh_failed = 1;
+            __threadfence_block();
+        }
+        umma_commit<1>(acc_full);
+        if (!ok) {
+            umma_commit<1>(drain);
+            (void)mbar_wait(drain, 0);
+        }
+    }
+    __syncwarp();
+
+    bool ok = true;
+    const uint64_t chan = (uint64_t)tn * 128 + warp * 32 + lane;
+    const uint64_t tok0 = (uint64_t)tm * NT;
+    if (warp < 4) {
+        ok = mbar_wait(acc_full, 0);
+        umma_fence_after();
+    }
+    float sb = 0.f, bias = 0.f;
+    if (warp < 4 && chan < p.n) {
+        sb = __ldg(p.sb + chan);
+        if (p.bias) bias = __ldg(p.bias + chan);
+    }
+    T* out = static_cast<T*>(p.out);
+    const auto put = [&](uint32_t c, int acc, bool good) {
+        const uint64_t tok = tok0 + c;
+        if (chan < p.n && tok < p.m)
+            out[tok * p.ldo + chan] = from_f32<T>(good ? scaled(acc, __ldg(p.sa + tok), sb, p.bias, bias) : CUDART_NAN_F);
+    };
+    if (split == 1) {
+        if (warp < 4) {
+            const bool good = __all_sync(kFullMask, ok && !sh_failed);
+#pragma unroll 1
+            for (uint32_t c = 0; c < NT; c += 16) {
+                uint32_t r[16];
+                if (tok0 + c >= p.m) break;
+                tmem_ld16(tmem + ((warp * 32) << 16) + c, r);
+                tmem_wait_ld();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) put(c + j, (int)r[j], good);
+            }
+        }
+        umma_fence_before();
+        __syncthreads();
+    } else {
+        if (warp < 4) {
+            if (!ok) sh_failed = 1;
+#pragma unroll 1
+            for (uint32_t c = 0; c < NT; c += 16) {
+                uint32_t r[16];
+                tmem_ld16(tmem + ((warp * 32) << 16) + c, r);
+                tmem_wait_ld();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sums[(c + j) * 128 + warp * 32 + lane] = n > 0 ? (int)r[j] : 0;
+            }
+        }
+        umma_fence_before();
+        cluster_sync_all();                                // every part's sums are in place
+        if (warp < 4) {
+            bool good = true;
+            for (uint32_t q = 0; q < split; ++q) good = good && cluster_ld(cluster_map(smem_u32((void*)&sh_failed), q)) == 0;
+            const uint32_t c0 = NT * part / split, c1 = NT * (part + 1) / split;
+            for (uint32_t c = c0; c < c1; ++c) {
+                if (tok0 + c >= p.m) break;
+                int acc = 0;
+                const uint32_t at = data + ((c * 128) + warp * 32 + lane) * 4;
+                for (uint32_t q = 0; q < split; ++q) acc += cluster_ld(cluster_map(at, q));
+                put(c, acc, good);
+            }
+        }
+        cluster_sync_all();                                // nobody leaves while its sums are being read
+    }
+    if (warp == 5) tmem_free<1>(tmem, G::kColumns);
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(f);
+    }();
+    return fn;
+}
+// `lines` lines of k codes, boxes of 128 codes x `box` lines; codes beyond a line's end read as zero.
+bool make_map(CUtensorMap* map, const int8_t* codes, uint64_t lines, uint64_t k, uint64_t ld, uint32_t box) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {k, lines}, strides[1] = {ld};
+    const cuuint32_t boxes[2] = {128, box}, steps[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(codes), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The dynamic shared-memory opt-in of one kernel instantiation, once per device.
+template <typename K> cudaError_t allow_smem(K kernel, uint32_t bytes, PerDevice<bool>& done) {
+    const int slot = device_slot();
+    if (slot >= 0 && done.v[slot]) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess && slot >= 0) done.v[slot] = true;
+    return e;
+}
+
+template <int NT, typename T> cudaError_t launch_pair(const Product8& p, cudaStream_t st) {
+    using G = PairGeom<NT>;
+    static PerDevice<bool> done;
+    const auto kernel = product8_pair_kernel<NT, T>;
+    cudaError_t e = allow_smem(kernel, G::kSmem, done);
+    if (e != cudaSuccess) return e;
+    CUtensorMap ma, mb;
+    if (!make_map(&ma, p.a, p.m, p.k, p.lda, 128) || !make_map(&mb, p.b, p.n, p.k, p.ldb, NT / 2)) return cudaErrorNotSupported;
+    const uint64_t tiles = (p.m + 255) / 256 * ((p.n + NT - 1) / NT), pairs = (uint64_t)sm_count_now() / 2;
+    if (tiles >= (1ull << 31)) return cudaErrorInvalidValue;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p.out) | (p.m > 1 ? p.ldo * sizeof(T) : 0);
+    const uint32_t align = at % 32 == 0 ? 32u : at % 16 == 0 ? 16u : 1u;
+    kernel<<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), kPairThreads, G::kSmem, st>>>(ma, mb, p, align);
+    return cudaGetLastError();
+}
+
+template <int NT, typename T> cudaError_t launch_slim(const Product8& p, uint32_t split, cudaStream_t st) {
+    using G = SlimGeom<NT>;
+    static PerDevice<bool> done;
+    const auto kernel = product8_slim_kernel<NT, T>;
+    cudaError_t e = allow_smem(kernel, G::kSmem, done);
+    if (e != cudaSuccess) return e;
+    CUtensorMap ma, mb;
+    if (!make_map(&mb, p.b, p.n, p.k, p.ldb, 128) || !make_map(&ma, p.a, p.m, p.k, p.lda, NT)) return cudaErrorNotSupported;
+    const uint32_t tiles_n = (uint32_t)((p.n + 127) / 128);
+    const uint64_t ctas = (p.m + NT - 1) / NT * tiles_n * split;
+    if (ctas >= (1ull << 31)) return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kSlimThreads);
+    cfg.dynamicSmemBytes = G::kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, mb, ma, p, split, tiles_n);
 }
 
 }  // namespace
 
 cudaError_t launch_product8(const Product8& p, cudaStream_t st) {
-    const uint64_t gx = (p.n + 63) / 64, gy = (p.m + 63) / 64;
-    if (gy > 65535) return cudaErrorInvalidValue;
+    const uint64_t sms = (uint64_t)sm_count_now(), kblocks = (p.k + 127) / 128;
     return with_type(p.type, [&](auto t) {
-        product8_tile_kernel<decltype(t)><<<dim3((unsigned)gx, (unsigned)gy), 256, 0, st>>>(p);
-        return cudaGetLastError();
+        using T = decltype(t);
+        if (p.m <= 128) {
+            const uint64_t nt = p.m <= 16 ? 16 : p.m <= 32 ? 32 : p.m <= 64 ? 64 : 128;
+            const uint64_t tiles = (p.n + 127) / 128 * ((p.m + nt - 1) / nt);
+            uint32_t split = 1;
+            while (split < 8 && tiles * split * 2 <= 2 * sms && kblocks >= split * 4) split *= 2;
+            if (nt == 16) return launch_slim<16, T>(p, split, st);
+            if (nt == 32) return launch_slim<32, T>(p, split, st);
+            if (nt == 64) return launch_slim<64, T>(p, split, st);
+            return launch_slim<128, T>(p, split, st);
+        }
+        const uint64_t wide = (p.m + 255) / 256 * ((p.n + 255) / 256);
+        return wide >= sms / 2 ? launch_pair<256, T>(p, st) : launch_pair<128, T>(p, st);
     });
 }
 
