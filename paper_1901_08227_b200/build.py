@@ -12,7 +12,7 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libtng.so"
 SOURCES = ["tng_api.cu", "tng_fuse.cu", "tng_codec.cu", "tng_producers.cu", "tng_static.cu",
            "tng_dropout.cu", "tng_quant8.cu", "tng_product8.cu", "tng_linear8.cu"]
-HEADERS = [CSRC / "tng_device.cuh", CSRC / "tng_layers.cuh", CSRC / "tng_pipeline.cuh", CSRC / "tng_internal.h", ROOT / "include" / "tng.h"]
+HEADERS = [CSRC / "tng_device.cuh", CSRC / "tng_layers.cuh", CSRC / "tng_codes.cuh", CSRC / "tng_umma.cuh", CSRC / "tng_pipeline.cuh", CSRC / "tng_internal.h", ROOT / "include" / "tng.h"]
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",

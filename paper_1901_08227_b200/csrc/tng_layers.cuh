@@ -102,6 +102,8 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float (
     }
 }
 
+__device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
 // Calls f(T()) for the element type of `type`.
 template <class F> inline cudaError_t with_type(tng_dtype type, F&& f) {
     switch (type) {

@@ -23,7 +23,9 @@ struct Carver {
 
 extern "C" {
 
-size_t tng_linear8_scratch_bytes(uint64_t tokens, uint64_t k) { return (size_t)(codes_bytes(tokens, k) + scales_bytes(tokens)); }
+size_t tng_linear8_scratch_bytes(uint64_t tokens, uint64_t k) {
+    return product8_streams(tokens, k) ? 0 : (size_t)(codes_bytes(tokens, k) + scales_bytes(tokens));
+}
 
 tng_status tng_linear8(const void* x_dev, tng_dtype type, uint64_t tokens, uint64_t k, uint64_t ldx, const int8_t* w_dev,
                        uint64_t ldw, const float* sw_dev, uint64_t n, const float* bias_dev, void* y_dev, uint64_t ldy,
@@ -31,9 +33,14 @@ tng_status tng_linear8(const void* x_dev, tng_dtype type, uint64_t tokens, uint6
     if (!type_ok(type) || n < 1 || k < 1 || k > TNG_MAX_CONTRACTION || !dims_ok(tokens, n)) return TNG_ERR_INVALID_ARG;
     if (tokens == 0) return TNG_OK;
     if (!matrix_ok(x_dev, type, k, ldx) || !codes_ok(w_dev, k, ldw) || !sw_dev || !aligned(sw_dev, 4) || !aligned(bias_dev, 4) ||
-        !matrix_ok(y_dev, type, n, ldy) || !scratch_dev || !aligned(scratch_dev, 256))
+        !matrix_ok(y_dev, type, n, ldy))
         return TNG_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (product8_streams(tokens, k)) {
+        const Product8 p{nullptr, w_dev, 0, ldw, nullptr, sw_dev, bias_dev, tokens, n, k, y_dev, type, ldy};
+        return launch_linear8_stream(x_dev, ldx, p, st) == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
+    }
+    if (!scratch_dev || !aligned(scratch_dev, 256)) return TNG_ERR_INVALID_ARG;
     Carver c{static_cast<unsigned char*>(scratch_dev)};
     int8_t* q = c.take<int8_t>(codes_bytes(tokens, k));
     float* s = c.take<float>(scales_bytes(tokens));

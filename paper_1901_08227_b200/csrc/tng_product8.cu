@@ -4,7 +4,7 @@
 // The int32 sums are exact, so every variant below gives the same bits whatever order it sums in.
 #include <math_constants.h>
 
-#include "tng_layers.cuh"
+#include "tng_codes.cuh"
 #include "tng_umma.cuh"
 
 namespace tng {
@@ -55,6 +55,156 @@ __device__ __forceinline__ void store_chunk(T* out, uint64_t ldo, uint64_t row0,
         if (col + lane < cols)
             for (uint32_t r = 0; r < n; ++r) out[(row0 + r) * ldo + col + lane] = from_f32<T>(stage[r * 33 + lane]);
         __syncwarp();
+    }
+}
+
+// ---- at most 16 tokens: the weights are streamed past them ----------------------------------------------
+// Bound by reading b once.  The tokens' codes stay in shared memory; a CTA goes over tiles of eight rows of b, KS
+// warps sharing a tile along the contraction, 512 codes a warp and step: eight 16-byte loads a lane, the next
+// step's issued before this one's are used.  A warp-wide m16n8k32 instruction takes the tokens as its 16 rows and
+// the weights as its 8 columns straight from the loaded words: the contraction may run in any order as long as
+// both sides agree, so a lane's 16 consecutive codes serve as its words of two instructions.  (The tensor-memory
+// kernel below needs its operands in shared memory and takes 2.5x the time here: set-up and barriers, not traffic.)
+// X = int8_t: codes with scales; a floating type: the CTA codes the tokens itself, while its first weights travel.
+constexpr int kStreamThreads = 256, kStreamTokens = 16;
+constexpr uint32_t kStreamSmem = 96 * 1024;
+__host__ __device__ inline uint32_t stream_pitch(uint64_t k) { return (uint32_t)((k + 511) / 512 * 512 + 64); }   // 64 mod 128: no bank conflicts
+
+__device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The tokens' codes and scales into shared memory, zero up to a multiple of 512 codes.  TPT threads a token.
+template <typename X>
+__device__ __forceinline__ void stream_tokens(const X* x, uint64_t ldx, const float* sa, uint32_t tokens, uint32_t k, int8_t* codes, uint32_t pitch,
+                                              float* scales, uint32_t* part) {
+    const uint32_t groups = (k + 7) / 8, all = (k + 511) / 512 * 64;
+    uint32_t tpt = kStreamThreads;                          // threads a token: a power of two, a warp at least
+    while (tpt > 32 && (uint64_t)tpt * tokens > kStreamThreads) tpt >>= 1;
+    const uint32_t at_once = kStreamThreads / tpt, me = threadIdx.x / tpt, lane = threadIdx.x & (tpt - 1);
+    for (uint32_t t0 = 0; t0 < tokens; t0 += at_once) {
+        const uint32_t t = t0 + me;
+        const bool live = t < tokens;
+        const X* row = x + (uint64_t)(live ? t : 0) * ldx;
+        uint2* dst = reinterpret_cast<uint2*>(codes + (live ? t : 0) * pitch);
+        if constexpr (sizeof(X) == 1) {
+            if (live) {
+                for (uint32_t g = lane; g < all; g += tpt) {
+                    uint2 w = make_uint2(0u, 0u);
+                    if (g < groups) w = __ldg(reinterpret_cast<const uint2*>(row) + g);
+                    if (g * 8 + 8 > k) {                    // what follows a line does not count
+                        uint32_t n = g * 8 < k ? k - g * 8 : 0;
+                        w.x &= n >= 4 ? ~0u : (1u << (8 * n)) - 1u;
+                        n = n > 4 ? n - 4 : 0;
+                        w.y &= n >= 4 ? ~0u : (1u << (8 * n)) - 1u;
+                    }
+                    dst[g] = w;
+                }
+                if (lane == 0) scales[t] = __ldg(sa + t);
+            }
+        } else {
+            const bool vec = aligned16(row);
+            uint32_t m = 0;
+            if (live) {
+#pragma unroll 4
+                for (uint32_t g = lane; g < groups; g += tpt) {
+                    float v[8];
+                    if (vec) fetch8<X, true>(row, (uint64_t)g * 8, k, v);
+                    else fetch8<X, false>(row, (uint64_t)g * 8, k, v);
+                    m = max8(v, m);
+                }
+            }
+            m = __reduce_max_sync(kFullMask, m);
+            if (tpt > 32) {
+                if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
+                __syncthreads();
+                const uint32_t w = tpt >> 5;
+                for (uint32_t i = 0; i < w; ++i) m = max(m, part[me * w + i]);
+                __syncthreads();
+            }
+            const LineScale s = line_scale(m);
+            if (live) {
+                if (lane == 0) scales[t] = s.scale;
+#pragma unroll 4
+                for (uint32_t g = lane; g < all; g += tpt) {
+                    uint2 w = make_uint2(0u, 0u);
+                    if (g < groups) {
+                        float v[8];
+                        if (vec) fetch8<X, true>(row, (uint64_t)g * 8, k, v);
+                        else fetch8<X, false>(row, (uint64_t)g * 8, k, v);
+                        w = code8<false>(v, s.inv, DrawArgs{}, 0, 0);
+                    }
+                    dst[g] = w;
+                }
+            }
+        }
+    }
+}
+
+template <typename X, typename T, bool WIDE>               // WIDE: more than 8 tokens
+__global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(const X* __restrict__ x, uint64_t ldx, const __grid_constant__ Product8 p) {
+    extern __shared__ __align__(16) unsigned char dyn[];
+    __shared__ float scales[kStreamTokens];
+    __shared__ uint32_t part[8];
+    __shared__ int red[2][8][32][4];
+    int8_t* codes = reinterpret_cast<int8_t*>(dyn);
+    const uint32_t k = (uint32_t)p.k, pitch = stream_pitch(k), kparts = (k + 511) / 512, tokens = (uint32_t)p.m;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const uint32_t ks = kparts >= 5 ? 8u : kparts >= 3 ? 4u : kparts;          // warps sharing a tile
+    const uint32_t per_round = 8 / ks, sub = warp / ks, kp0 = warp & (ks - 1);
+    const uint32_t steps = (kparts + ks - 1) / ks;          // of 512 codes, for a warp that has the most
+    const uint64_t rounds = ((p.n + 7) / 8 + per_round - 1) / per_round;
+    const uint64_t mine = blockIdx.x < rounds ? (rounds - 1 - blockIdx.x) / gridDim.x + 1 : 0;
+
+    uint4 buf[8];
+    const auto load = [&](uint64_t round, uint32_t step) {
+        const uint64_t row = (round * per_round + sub) * 8 + g;
+        const uint32_t c = (kp0 + step * ks) * 512 + q * 16;
+        const int8_t* src = p.b + row * p.ldb + c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            buf[i] = row < p.n && c + 64 * i < k ? __ldcs(reinterpret_cast<const uint4*>(src + 64 * i)) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    if (mine) load(blockIdx.x, 0);
+    stream_tokens<X>(x, ldx, p.sa, tokens, k, codes, pitch, scales, part);
+    __syncthreads();
+
+    T* out = static_cast<T*>(p.out);
+    for (uint64_t j = 0; j < mine; ++j) {
+        const uint64_t round = blockIdx.x + j * gridDim.x;
+        int acc[4] = {};
+        for (uint32_t step = 0; step < steps; ++step) {
+            uint4 w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = buf[i];
+            if (step + 1 < steps) load(round, step + 1);
+            else if (j + 1 < mine) load(round + gridDim.x, 0);
+            const uint32_t c = (kp0 + step * ks) * 512 + q * 16;
+            if (kp0 + step * ks < kparts) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+                    const uint4 lo = g < tokens ? *reinterpret_cast<const uint4*>(codes + g * pitch + c + 64 * i) : zero;
+                    const uint4 hi = WIDE && g + 8 < tokens ? *reinterpret_cast<const uint4*>(codes + (g + 8) * pitch + c + 64 * i) : zero;
+                    mma_s8(acc, lo.x, hi.x, lo.y, hi.y, w[i].x, w[i].y);
+                    mma_s8(acc, lo.z, hi.z, lo.w, hi.w, w[i].z, w[i].w);
+                }
+            }
+        }
+        int(*mem)[32][4] = red[j & 1];
+        *reinterpret_cast<int4*>(mem[warp][lane]) = make_int4(acc[0], acc[1], acc[2], acc[3]);
+        __syncthreads();                                    // the other half of `red` is free: its readers passed this barrier last round
+        const uint32_t chans = per_round * 8;
+        for (uint32_t i = threadIdx.x; i < chans * tokens; i += kStreamThreads) {
+            const uint32_t tok = i / chans, ch = i - tok * chans;
+            const uint64_t row = round * chans + ch;
+            if (row >= p.n) continue;
+            const uint32_t tile = ch >> 3, in = ch & 7, from = (tok & 7) * 4 + (in >> 1), reg = (tok >> 3) * 2 + (in & 1);
+            int a = 0;
+            for (uint32_t s = 0; s < ks; ++s) a += mem[tile * ks + s][from][reg];
+            out[(uint64_t)tok * p.ldo + row] = from_f32<T>(scaled(a, scales[tok], __ldg(p.sb + row), p.bias, p.bias ? __ldg(p.bias + row) : 0.f));
+        }
     }
 }
 
@@ -459,12 +609,36 @@ template <int NT, typename T> cudaError_t launch_slim(const Product8& p, uint32_
     return cudaLaunchKernelEx(&cfg, kernel, mb, ma, p, split, tiles_n);
 }
 
+template <typename X, typename T, bool WIDE> cudaError_t launch_stream_one(const X* x, uint64_t ldx, const Product8& p, cudaStream_t st) {
+    static PerDevice<bool> done;
+    const auto kernel = product8_stream_kernel<X, T, WIDE>;
+    const cudaError_t e = allow_smem(kernel, kStreamSmem, done);
+    if (e != cudaSuccess) return e;
+    const uint64_t kparts = (p.k + 511) / 512, ks = kparts >= 5 ? 8 : kparts >= 3 ? 4 : kparts;
+    const uint64_t rounds = ((p.n + 7) / 8 * ks + 7) / 8, most = 2ull * sm_count_now();
+    kernel<<<(unsigned)(rounds < most ? rounds : most), kStreamThreads, p.m * stream_pitch(p.k), st>>>(x, ldx, p);
+    return cudaGetLastError();
+}
+template <typename X, typename T> cudaError_t launch_stream(const X* x, uint64_t ldx, const Product8& p, cudaStream_t st) {
+    return p.m > 8 ? launch_stream_one<X, T, true>(x, ldx, p, st) : launch_stream_one<X, T, false>(x, ldx, p, st);
+}
+
 }  // namespace
+
+bool product8_streams(uint64_t tokens, uint64_t k) { return tokens <= kStreamTokens && tokens * stream_pitch(k) <= kStreamSmem; }
+
+cudaError_t launch_linear8_stream(const void* x, uint64_t ldx, const Product8& p, cudaStream_t st) {
+    return with_type(p.type, [&](auto t) {
+        using T = decltype(t);
+        return launch_stream<T, T>(static_cast<const T*>(x), ldx, p, st);
+    });
+}
 
 cudaError_t launch_product8(const Product8& p, cudaStream_t st) {
     const uint64_t sms = (uint64_t)sm_count_now(), kblocks = (p.k + 127) / 128;
     return with_type(p.type, [&](auto t) {
         using T = decltype(t);
+        if (product8_streams(p.m, p.k)) return launch_stream<int8_t, T>(p.a, p.lda, p, st);
         if (p.m <= 128) {
             const uint64_t nt = p.m <= 16 ? 16 : p.m <= 32 ? 32 : p.m <= 64 ? 64 : 128;
             const uint64_t tiles = (p.n + 127) / 128 * ((p.m + nt - 1) / nt);

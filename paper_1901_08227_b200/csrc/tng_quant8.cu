@@ -1,66 +1,10 @@
 // 8-bit codes of a matrix with one scale a line: rows (a scale per token) or columns (a scale per
 // channel, codes transposed).  The codes are unique: scale, 1/scale, product and (with a draw) the sum
 // with the uniform are one fp32 rounding each, so any order of work gives the same bytes.
-#include "tng_layers.cuh"
+#include "tng_codes.cuh"
 
 namespace tng {
 namespace {
-
-constexpr uint32_t kInfBits = 0x7F800000u;
-constexpr float kTiny = 0x1p-120f;
-
-struct LineScale {
-    float scale, inv;    // inv = 0: all codes of the line are zero
-};
-// `bits`: largest |x| of the line as a bit pattern; a NaN's is above every number's and wins.
-__device__ __forceinline__ LineScale line_scale(uint32_t bits) {
-    const float top = __uint_as_float(bits);
-    LineScale s;
-    s.scale = __fdiv_rn(top, 127.f);
-    s.inv = __fdiv_rn(127.f, top);
-    if (top < kTiny) s.scale = s.inv = 0.f;
-    if (bits >= kInfBits) s.inv = 0.f;
-    return s;
-}
-
-// Adding 1.5 * 2^23 leaves the rounded integer in the low bits: to nearest even with round-to-nearest, the
-// floor with round-down; the low byte is the two's complement code.
-template <bool DRAW> __device__ __forceinline__ uint32_t code_bits(float x, float inv, uint32_t word) {
-    const float v = __fmul_rn(x, inv);
-    if constexpr (DRAW) {
-        // cut before the floor: -127 <= t < 128 gives the same codes as cutting the floor to [-127, 127]
-        const float t = fminf(fmaxf(__fadd_rn(v, uniform24(word)), -127.f), 127.5f);
-        return __float_as_uint(__fadd_rd(t, 12582912.f));
-    } else {
-        return __float_as_uint(__fadd_rn(v, 12582912.f));
-    }
-}
-__device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
-}
-
-// Eight codes of a row; a line with inv = 0 has code zero everywhere (0 * NaN would not).
-template <bool DRAW> __device__ __forceinline__ uint2 code8(const float (&v)[8], float inv, const DrawArgs& d, uint32_t group, uint32_t row) {
-    uint32_t w[8] = {};
-    if constexpr (DRAW) {
-        const uint4 a = draw_words(d, 2 * group, row), b = draw_words(d, 2 * group + 1, row);
-        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-    }
-    uint32_t q[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) q[j] = code_bits<DRAW>(v[j], inv, w[j]);
-    return inv == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bytes(q[0], q[1], q[2], q[3]), pack_bytes(q[4], q[5], q[6], q[7]));
-}
-
-template <typename T, bool VEC> __device__ __forceinline__ void fetch8(const T* row, uint64_t c, uint64_t cols, float (&v)[8]) {
-    if (VEC && c + 8 <= cols) widen8(load_raw8(row + c), v);
-    else load_part8(row + c, (int64_t)cols - (int64_t)c, v);
-}
-__device__ __forceinline__ uint32_t max8(const float (&v)[8], uint32_t m) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-    return m;
-}
 
 // ---- rows --------------------------------------------------------------------------------------------
 // blockDim.x threads share a row, blockDim.y rows a CTA (more than one only where a row is one warp).

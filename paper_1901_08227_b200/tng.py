@@ -139,7 +139,7 @@ def _check(status, what):
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())   # current_stream() builds an object: 3 us a call
 
 
 def _dev(t, dtype=torch.float32):
@@ -421,18 +421,20 @@ def _matrix(t, name, dtype=None, shape=None):
     """A 2-D CUDA tensor of the current device with unit column stride -> (pointer, row stride)."""
     if not t.is_cuda or t.dim() != 2 or (t.dtype not in _DTYPE if dtype is None else t.dtype != dtype):
         raise TypeError(f"{name} must be a 2-D CUDA tensor of type {dtype or 'float32, bfloat16 or float16'}")
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
-    rows, cols = t.shape
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is not on the current CUDA device")
+    rows, cols = size = t.shape
+    if shape is not None and size != shape:
+        raise ValueError(f"{name} has shape {tuple(size)}, expected {tuple(shape)}")
     ld, unit = t.stride()
-    if unit != 1 and cols != 1:
+    if unit != 1 and cols > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return t.data_ptr(), ld if rows > 1 else max(cols, ld)
+    return t.data_ptr(), ld if rows > 1 or ld > cols else cols
 
 
 def _codes(t, name, shape=None):
     p, ld = _matrix(t, name, torch.int8, shape)
-    return p, ld if ld % 16 == 0 or t.shape[0] > 1 else -(-ld // 16) * 16
+    return p, ld if t.shape[0] > 1 else -(-ld // 16) * 16
 
 
 def _vector(t, name, n, dtype=torch.float32):
@@ -440,19 +442,20 @@ def _vector(t, name, n, dtype=torch.float32):
         return None
     if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
         raise TypeError(f"{name} must be a contiguous CUDA {dtype} vector of {n} elements")
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is not on the current CUDA device")
     return t.data_ptr()
 
 
-def _scratch(buf, nbytes, device):
+def _scratch(buf, nbytes, like):
+    """(pointer, owner) of at least nbytes; the owner is to be kept until the call has been enqueued."""
+    if nbytes == 0:
+        return None, None
     if buf is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if not buf.is_cuda or not buf.is_contiguous() or buf.numel() * buf.element_size() < nbytes:
+        buf = like.new_empty(nbytes, dtype=torch.uint8)
+    elif not buf.is_cuda or not buf.is_contiguous() or buf.numel() * buf.element_size() < nbytes or buf.device != like.device:
         raise ValueError(f"scratch must be a contiguous CUDA tensor of at least {nbytes} bytes")
-    return buf
-
-
-def _draw_ref(draw):
-    return None if draw is None else C.byref(draw)
+    return buf.data_ptr(), buf
 
 
 def empty_codes(lines, n, device="cuda"):
@@ -467,7 +470,7 @@ def quant8_rows(x, draw=None, q=None, scale=None):
     q = empty_codes(rows, cols, x.device) if q is None else q
     scale = torch.empty(rows, device=x.device) if scale is None else scale
     pq, ldq = _codes(q, "q", (rows, cols))
-    _check(lib().tng_quant8_rows(p, _DTYPE[x.dtype], rows, cols, ld, _draw_ref(draw), pq, ldq, _vector(scale, "scale", rows), _stream()),
+    _check(lib().tng_quant8_rows(p, _DTYPE[x.dtype], rows, cols, ld, draw, pq, ldq, _vector(scale, "scale", rows), _stream()),
            "tng_quant8_rows")
     return q, scale
 
@@ -480,9 +483,9 @@ def quant8_cols(x, draw=None, q=None, scale=None, colsum=None, scratch=None):
     q = empty_codes(cols, rows, x.device) if q is None else q
     scale = torch.empty(cols, device=x.device) if scale is None else scale
     pq, ldq = _codes(q, "q", (cols, rows))
-    buf = _scratch(scratch, lib().tng_quant8_cols_scratch_bytes(rows, cols), x.device)
-    _check(lib().tng_quant8_cols(p, _DTYPE[x.dtype], rows, cols, ld, _draw_ref(draw), pq, ldq, _vector(scale, "scale", cols),
-                                 _vector(colsum, "colsum", cols), buf.data_ptr(), _stream()), "tng_quant8_cols")
+    ps, _keep = _scratch(scratch, lib().tng_quant8_cols_scratch_bytes(rows, cols), x)
+    _check(lib().tng_quant8_cols(p, _DTYPE[x.dtype], rows, cols, ld, draw, pq, ldq, _vector(scale, "scale", cols),
+                                 _vector(colsum, "colsum", cols), ps, _stream()), "tng_quant8_cols")
     return q, scale
 
 
@@ -508,11 +511,11 @@ def linear8(x, w, sw, bias=None, out=None, scratch=None):
     n = w.shape[0]
     pw, ldw = _codes(w, "w", (n, k))
     if out is None:
-        out = torch.empty((tokens, n), dtype=x.dtype, device=x.device)
+        out = x.new_empty((tokens, n))
     po, ldo = _matrix(out, "out", x.dtype, (tokens, n))
-    buf = _scratch(scratch, lib().tng_linear8_scratch_bytes(tokens, k), x.device)
+    ps, _keep = _scratch(scratch, lib().tng_linear8_scratch_bytes(tokens, k), x)
     _check(lib().tng_linear8(px, _DTYPE[x.dtype], tokens, k, ldx, pw, ldw, _vector(sw, "sw", n), n, _vector(bias, "bias", n), po, ldo,
-                             buf.data_ptr(), _stream()), "tng_linear8")
+                             ps, _stream()), "tng_linear8")
     return out
 
 
@@ -525,14 +528,14 @@ def linear8_grad(dy, x, wt, swt, draw=None, dx=None, dw=None, db=None, scratch=N
     k = x.shape[1]
     px, ldx = _matrix(x, "x", dy.dtype, (tokens, k))
     pw, ldw = _codes(wt, "wt", (k, n))
-    dx = torch.empty((tokens, k), dtype=dy.dtype, device=dy.device) if dx is None else dx
-    dw = torch.empty((n, k), device=dy.device) if dw is None else dw
-    db = torch.empty(n, device=dy.device) if db is None else db
+    dx = dy.new_empty((tokens, k)) if dx is None else dx
+    dw = dy.new_empty((n, k), dtype=torch.float32) if dw is None else dw
+    db = dy.new_empty(n, dtype=torch.float32) if db is None else db
     pdx, lddx = _matrix(dx, "dx", dy.dtype, (tokens, k))
     pdw, lddw = _matrix(dw, "dw", torch.float32, (n, k))
-    buf = _scratch(scratch, lib().tng_linear8_grad_scratch_bytes(tokens, k, n), dy.device)
-    _check(lib().tng_linear8_grad(py, ldy, px, ldx, _DTYPE[dy.dtype], tokens, k, n, pw, ldw, _vector(swt, "swt", k), _draw_ref(draw),
-                                  pdx, lddx, pdw, lddw, _vector(db, "db", n), buf.data_ptr(), _stream()), "tng_linear8_grad")
+    ps, _keep = _scratch(scratch, lib().tng_linear8_grad_scratch_bytes(tokens, k, n), dy)
+    _check(lib().tng_linear8_grad(py, ldy, px, ldx, _DTYPE[dy.dtype], tokens, k, n, pw, ldw, _vector(swt, "swt", k), draw,
+                                  pdx, lddx, pdw, lddw, _vector(db, "db", n), ps, _stream()), "tng_linear8_grad")
     return dx, dw, db
 
 
@@ -541,10 +544,10 @@ def dropout(x, p, draw, residual=None, out=None):
     px, ldx = _matrix(x, "x")
     rows, cols = x.shape
     if out is None:
-        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    po, ldo = _matrix(out, "out", x.dtype, (rows, cols))
-    pr, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, (rows, cols))
-    _check(lib().tng_dropout(px, _DTYPE[x.dtype], rows, cols, ldx, pr, ldr, p, _draw_ref(draw), po, ldo, _stream()), "tng_dropout")
+        out = torch.empty_like(x)
+    po, ldo = _matrix(out, "out", x.dtype, x.shape)
+    pr, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, x.shape)
+    _check(lib().tng_dropout(px, _DTYPE[x.dtype], rows, cols, ldx, pr, ldr, p, draw, po, ldo, _stream()), "tng_dropout")
     return out
 
 

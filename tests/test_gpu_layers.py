@@ -201,7 +201,7 @@ def test_linear_forward(dtype, T, K, N):
         assert same(f32(tng.linear8(x, w, sw, bias=b)), want)
         assert same(f32(tng.linear8(strided(x, 3), w, sw, bias=b)), want)
     # what the caller's scratch held before makes no difference
-    scratch = torch.full((tng.lib().tng_linear8_scratch_bytes(T, K),), 0xA5, dtype=torch.uint8, device="cuda")
+    scratch = torch.full((tng.lib().tng_linear8_scratch_bytes(T, K) + 256,), 0xA5, dtype=torch.uint8, device="cuda")
     assert same(f32(tng.linear8(x, w, sw, bias=bias, scratch=scratch)), want)
 
 
@@ -341,10 +341,10 @@ def test_another_stream():
 
 
 def test_calls_can_be_captured_in_a_graph():
-    x = values((12, 512), torch.bfloat16, 1)
+    x = values((40, 512), torch.bfloat16, 1)
     w, sw = tng.quant8_rows(values((256, 512), torch.float32, 2))
-    out, y = torch.empty((12, 256), dtype=torch.bfloat16, device="cuda"), torch.empty((12, 256), dtype=torch.bfloat16, device="cuda")
-    scratch = torch.empty(tng.lib().tng_linear8_scratch_bytes(12, 512), dtype=torch.uint8, device="cuda")
+    out, y = torch.empty((40, 256), dtype=torch.bfloat16, device="cuda"), torch.empty((40, 256), dtype=torch.bfloat16, device="cuda")
+    scratch = torch.empty(tng.lib().tng_linear8_scratch_bytes(40, 512), dtype=torch.uint8, device="cuda")
     d = tng.Draw(1, 2, 3)
     tng.linear8(x, w, sw, out=out, scratch=scratch)
     torch.cuda.synchronize()
@@ -352,7 +352,7 @@ def test_calls_can_be_captured_in_a_graph():
     with torch.cuda.graph(graph):
         tng.linear8(x, w, sw, out=out, scratch=scratch)
         tng.dropout(out, 0.2, d, out=y)
-    x.copy_(values((12, 512), torch.bfloat16, 5))
+    x.copy_(values((40, 512), torch.bfloat16, 5))
     graph.replay()
     want = tng.linear8(x, w, sw)
     assert torch.equal(out, want) and torch.equal(y, tng.dropout(want, 0.2, d))
@@ -404,7 +404,8 @@ def test_refusals():
     refuses(lambda: tng.linear8(x, w, sw.double()))
     refuses(lambda: tng.linear8(x, w, sw, bias=torch.zeros(31, device="cuda")))
     refuses(lambda: tng.linear8(x, w, sw, out=torch.empty((8, 32), device="cuda")))
-    refuses(lambda: tng.linear8(x, w, sw, scratch=torch.empty(8, dtype=torch.uint8, device="cuda")))
+    x20 = values((20, 64), torch.bfloat16, 1)
+    refuses(lambda: tng.linear8(x20, w, sw, scratch=torch.empty(8, dtype=torch.uint8, device="cuda")))
     refuses(lambda: tng.linear8(x[:1].expand(8, 64), w, sw), tng.TngError)          # rows that overlap
     odd = torch.zeros((32, 65), dtype=torch.int8, device="cuda")
     refuses(lambda: tng.linear8(x, odd[:, :64], sw), tng.TngError)                  # codes off their 16-byte rows
@@ -434,4 +435,4 @@ def test_refusals():
     assert L.tng_dropout(x.data_ptr(), tng.BF16, 8, 0, 64, None, 0, 0.5, d, x.data_ptr(), 64, st) == tng.ERR_INVALID_ARG
     assert L.tng_dropout(x.data_ptr(), tng.BF16, 8, 64, 63, None, 0, 0.5, d, x.data_ptr(), 64, st) == tng.ERR_INVALID_ARG
     assert L.tng_quant8_cols(x.data_ptr(), tng.BF16, 8, 64, 64, None, a.data_ptr(), 16, sa.data_ptr(), None, None, st) == tng.ERR_INVALID_ARG
-    assert L.tng_linear8(x.data_ptr(), tng.BF16, 8, 64, 64, w.data_ptr(), 64, sw.data_ptr(), 32, None, x.data_ptr(), 32, None, st) == tng.ERR_INVALID_ARG
+    assert L.tng_linear8(x20.data_ptr(), tng.BF16, 20, 64, 64, w.data_ptr(), 64, sw.data_ptr(), 32, None, x.data_ptr(), 32, None, st) == tng.ERR_INVALID_ARG
