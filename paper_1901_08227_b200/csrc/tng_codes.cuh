@@ -51,14 +51,49 @@ template <bool DRAW> __device__ __forceinline__ uint2 code8(const float (&v)[8],
     return inv == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bytes(q[0], q[1], q[2], q[3]), pack_bytes(q[4], q[5], q[6], q[7]));
 }
 
-template <typename T, bool VEC> __device__ __forceinline__ void fetch8(const T* row, uint64_t c, uint64_t cols, float (&v)[8]) {
-    if (VEC && c + 8 <= cols) widen8(load_raw8(row + c), v);
-    else load_part8(row + c, (int64_t)cols - (int64_t)c, v);
-}
-__device__ __forceinline__ uint32_t max8(const float (&v)[8], uint32_t m) {
+// Eight elements of a row from column c as they lie in memory; zero beyond the row.  VEC: the row is 16-byte aligned.
+template <typename T, bool VEC> __device__ __forceinline__ Raw8<T> fetch_raw8(const T* row, uint64_t c, uint64_t cols) {
+    if (VEC && c + 8 <= cols) return load_raw8(row + c);
+    Raw8<T> r;
+    uint32_t* w = reinterpret_cast<uint32_t*>(&r);
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+        for (int j = 0; j < 8; ++j) w[j] = c + j < cols ? __ldg(reinterpret_cast<const uint32_t*>(row) + c + j) : 0u;
+    } else {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(row) + c;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t lo = c + 2 * j < cols ? __ldg(h + 2 * j) : 0u, hi = c + 2 * j + 1 < cols ? __ldg(h + 2 * j + 1) : 0u;
+            w[j] = lo | hi << 16;
+        }
+    }
+    return r;
+}
+template <typename T> __device__ __forceinline__ Raw8<T> zero_raw8() {
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.w[i] = make_uint4(0u, 0u, 0u, 0u);
+    return r;
+}
+
+// Running maximum of magnitudes as integers, which order like the magnitudes with NaN on top: 16-bit types two to a word.
+template <typename T> __device__ __forceinline__ uint32_t top_word(uint32_t w, uint32_t m) {
+    if constexpr (sizeof(T) == 4) return max(m, w & 0x7FFFFFFFu);
+    else return __vmaxu2(m, w & 0x7FFF7FFFu);
+}
+template <typename T> __device__ __forceinline__ uint32_t top_raw8(const Raw8<T>& r, uint32_t m) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) m = top_word<T>(r.w[i].x, top_word<T>(r.w[i].y, top_word<T>(r.w[i].z, top_word<T>(r.w[i].w, m))));
     return m;
+}
+// A magnitude (the low half of a word for 16-bit types) as the bit pattern of the fp32 value.
+template <typename T> __device__ __forceinline__ uint32_t top_bits(uint32_t m) {
+    if constexpr (sizeof(T) == 4) return m;
+    else return __float_as_uint(unpack2<T>(m).x);
+}
+template <typename T> __device__ __forceinline__ uint32_t top_of_halves(uint32_t m) {
+    if constexpr (sizeof(T) == 4) return m;
+    else return max(m & 0xFFFFu, m >> 16);
 }
 
 }  // namespace tng

@@ -39,6 +39,8 @@ template <typename T> __device__ __forceinline__ Raw8<T> load_stream8(const T* p
 // step, so no division in the loop.
 template <typename T, bool RES>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(const T* x, const T* res, T* y, const __grid_constant__ DropArgs a) {
+    grid_wait();
+    grid_go();
     const uint32_t per_row = (uint32_t)((a.cols + 7) / 8);
     const uint64_t total = a.rows * per_row, stride = (uint64_t)gridDim.x * kThreads;
     const uint64_t first = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
@@ -91,6 +93,8 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const T* x, const T* 
 // would touch every sector of the warp's span once an access.)
 template <typename T, bool RES>
 __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const T* x, const T* res, T* y, const __grid_constant__ DropArgs a) {
+    grid_wait();
+    grid_go();
     const uint32_t lane = threadIdx.x & 31;
     const uint32_t per_row = (uint32_t)((a.cols + 127) / 128);
     const uint64_t total = a.rows * per_row, stride = (uint64_t)gridDim.x * (kThreads / 32);
@@ -138,14 +142,8 @@ cudaError_t launch_dropout(const void* x, const void* res, void* y, const DropAr
     const uint64_t work = vec ? a.rows * ((a.cols + 7) / 8) : a.rows * ((a.cols + 127) / 128) * 32;
     const uint64_t want = (work + kThreads - 1) / kThreads, cap = (uint64_t)sm_count_now() * 8u;
     const unsigned grid = (unsigned)(want < cap ? want : cap);
-    if (vec) {
-        if (res) dropout_kernel<T, true><<<grid, kThreads, 0, st>>>(px, pr, py, a);
-        else dropout_kernel<T, false><<<grid, kThreads, 0, st>>>(px, pr, py, a);
-    } else {
-        if (res) dropout_any_kernel<T, true><<<grid, kThreads, 0, st>>>(px, pr, py, a);
-        else dropout_any_kernel<T, false><<<grid, kThreads, 0, st>>>(px, pr, py, a);
-    }
-    return cudaGetLastError();
+    const auto kernel = vec ? (res ? dropout_kernel<T, true> : dropout_kernel<T, false>) : (res ? dropout_any_kernel<T, true> : dropout_any_kernel<T, false>);
+    return launch_layer(kernel, grid, kThreads, 0, 1, st, px, pr, py, a);
 }
 
 }  // namespace

@@ -74,11 +74,6 @@ template <typename T> __device__ __forceinline__ Raw8<T> load_raw8(const T* p) {
     for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
     return r;
 }
-// Any alignment; elements at or beyond n read as zero.
-template <typename T> __device__ __forceinline__ void load_part8(const T* p, int64_t n, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(__ldg(p + i)) : 0.f;
-}
 template <typename T> __device__ __forceinline__ void widen8(const Raw8<T>& r, float (&v)[8]) {
     if constexpr (sizeof(T) == 4) {
         v[0] = __uint_as_float(r.w[0].x); v[1] = __uint_as_float(r.w[0].y);
@@ -103,6 +98,29 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float (
 }
 
 __device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// The layer kernels are launched so that one may be set up while the one before it on the stream ends (a few
+// microseconds a launch, in chains of short kernels).  Every thread calls grid_wait() before it touches global memory:
+// it returns when all earlier work on the stream is complete and visible; grid_go() lets the next launch begin its set-up.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <typename... P, typename... A>
+cudaError_t launch_layer(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, unsigned cluster, cudaStream_t st, const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
 
 // Calls f(T()) for the element type of `type`.
 template <class F> inline cudaError_t with_type(tng_dtype type, F&& f) {

@@ -7,36 +7,31 @@ namespace tng {
 namespace {
 
 // ---- rows --------------------------------------------------------------------------------------------
-// blockDim.x threads share a row, blockDim.y rows a CTA (more than one only where a row is one warp).
-// Rows of up to 8 * kHold * blockDim.x columns are read once and kept in registers; longer ones twice.
-constexpr int kHold = 4;
+// blockDim.x threads share a row, blockDim.y rows a CTA (more than one only where a row is one warp).  A thread keeps
+// up to 128 bytes of its row in registers as they came: all its loads are in flight at once, and the row is read once;
+// longer rows (above 1024 threads' worth) are read twice.
+template <typename T> constexpr int kHold = 16 / (int)sizeof(T);       // groups of eight elements
 template <typename T, bool VEC, bool DRAW>
 __global__ void quant8_rows_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, int8_t* __restrict__ q,
                                    uint64_t ldq, float* __restrict__ scale, const __grid_constant__ DrawArgs draw) {
     __shared__ uint32_t part[32];
+    grid_wait();
+    grid_go();
     const uint64_t row = (uint64_t)blockIdx.x * blockDim.y + threadIdx.y;
     if (row >= rows) return;                       // whole warps only: with blockDim.y > 1 there is no block barrier
     const T* src = x + row * ldx;
     const uint32_t groups = (uint32_t)((cols + 7) / 8), step = blockDim.x;
-    float v[kHold][8];
+    Raw8<T> v[kHold<T>];
     uint32_t m = 0;
 #pragma unroll
-    for (int h = 0; h < kHold; ++h) {
+    for (int h = 0; h < kHold<T>; ++h) {
         const uint32_t g = threadIdx.x + h * step;
-        if (g < groups) fetch8<T, VEC>(src, (uint64_t)g * 8, cols, v[h]);
-        else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[h][j] = 0.f;
-        }
+        v[h] = g < groups ? fetch_raw8<T, VEC>(src, (uint64_t)g * 8, cols) : zero_raw8<T>();
     }
 #pragma unroll
-    for (int h = 0; h < kHold; ++h) m = max8(v[h], m);
-    for (uint32_t g = threadIdx.x + kHold * step; g < groups; g += step) {
-        float t[8];
-        fetch8<T, VEC>(src, (uint64_t)g * 8, cols, t);
-        m = max8(t, m);
-    }
-    m = __reduce_max_sync(kFullMask, m);
+    for (int h = 0; h < kHold<T>; ++h) m = top_raw8<T>(v[h], m);
+    for (uint32_t g = threadIdx.x + kHold<T> * step; g < groups; g += step) m = top_raw8<T>(fetch_raw8<T, VEC>(src, (uint64_t)g * 8, cols), m);
+    m = __reduce_max_sync(kFullMask, top_bits<T>(top_of_halves<T>(m)));
     if (blockDim.x > 32) {
         const uint32_t lane = threadIdx.x & 31, warps = blockDim.x >> 5;
         if (lane == 0) part[threadIdx.x >> 5] = m;
@@ -47,107 +42,139 @@ __global__ void quant8_rows_kernel(const T* __restrict__ x, uint64_t rows, uint6
     if (threadIdx.x == 0) scale[row] = s.scale;
     const uint32_t out_groups = (uint32_t)((cols + 15) / 16 * 2);      // zeros up to the next multiple of 16
     uint2* dst = reinterpret_cast<uint2*>(q + row * ldq);
+    const auto put = [&](uint32_t g, const Raw8<T>& r) {
+        float f[8];
+        widen8(r, f);
+        dst[g] = g < groups ? code8<DRAW>(f, s.inv, draw, g, (uint32_t)row) : make_uint2(0u, 0u);
+    };
 #pragma unroll
-    for (int h = 0; h < kHold; ++h) {
+    for (int h = 0; h < kHold<T>; ++h) {
         const uint32_t g = threadIdx.x + h * step;
-        if (g < out_groups) dst[g] = g < groups ? code8<DRAW>(v[h], s.inv, draw, g, (uint32_t)row) : make_uint2(0u, 0u);
+        if (g < out_groups) put(g, v[h]);
     }
-    for (uint32_t g = threadIdx.x + kHold * step; g < out_groups; g += step) {
-        float t[8] = {};
-        if (g < groups) fetch8<T, VEC>(src, (uint64_t)g * 8, cols, t);
-        dst[g] = g < groups ? code8<DRAW>(t, s.inv, draw, g, (uint32_t)row) : make_uint2(0u, 0u);
-    }
+    for (uint32_t g = threadIdx.x + kHold<T> * step; g < out_groups; g += step)
+        put(g, g < groups ? fetch_raw8<T, VEC>(src, (uint64_t)g * 8, cols) : zero_raw8<T>());
 }
 
 // ---- columns -----------------------------------------------------------------------------------------
-// Largest |x| and sum of every column over a chunk of rows.  A thread owns eight columns and every eighth row
-// of the chunk; a CTA owns 256 columns.  Chunks are combined, in order, by the kernel that makes the codes.
+// Two passes over a panel of columns that the L2 cache can hold, so that the second finds the panel there: largest |x|
+// and sum of every column, then the codes.
+//
+// Statistics.  A thread owns eight columns and every eighth row of a chunk; a CTA owns 256 columns.  Maxima meet in
+// `tops` (cleared before) by atomic maximum of bit patterns, which no order changes; the chunks' sums are kept apart and
+// added in order by the second pass.
 constexpr int kStatCols = 256, kStatLanes = 8;
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) column_stats_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx,
-                                                           uint64_t rows_per_chunk, uint32_t* __restrict__ tops, float* __restrict__ sums) {
-    __shared__ uint32_t sh_top[kStatLanes][kStatCols];
-    __shared__ float sh_sum[kStatLanes][kStatCols];
+template <typename T, bool VEC, bool SUMS>
+__global__ void __launch_bounds__(256) column_stats_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, uint64_t c_first,
+                                                           uint64_t c_last, uint64_t rows_per_chunk, uint32_t* __restrict__ tops,
+                                                           float* __restrict__ sums) {
+    constexpr int kWords = 2 * (int)sizeof(T);
+    __shared__ uint32_t sh_top[kStatLanes][32 * kWords];
+    __shared__ float sh_sum[SUMS ? kStatLanes : 1][kStatCols];
+    grid_wait();
+    grid_go();
     const uint32_t cg = threadIdx.x & 31, lane = threadIdx.x >> 5;
-    const uint64_t c = (uint64_t)blockIdx.x * kStatCols + cg * 8;
+    const uint64_t c0 = c_first + (uint64_t)blockIdx.x * kStatCols, c = c0 + cg * 8;
     const uint64_t r0 = (uint64_t)blockIdx.y * rows_per_chunk;
     const uint64_t r1 = r0 + rows_per_chunk < rows ? r0 + rows_per_chunk : rows;
-    uint32_t top[8] = {};
+    uint32_t top[kWords] = {};
     float sum[8] = {};
-    if (c < cols) {
-#pragma unroll 4
-        for (uint64_t r = r0 + lane; r < r1; r += kStatLanes) {
-            float v[8];
-            fetch8<T, VEC>(x + r * ldx, c, cols, v);
+    if (c < c_last) {
+        const auto take = [&](const Raw8<T>& r) {
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(&r);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                top[j] = max(top[j], __float_as_uint(v[j]) & 0x7FFFFFFFu);
-                sum[j] += v[j];
+            for (int j = 0; j < kWords; ++j) top[j] = top_word<T>(w[j], top[j]);
+            if (SUMS) {
+                float v[8];
+                widen8(r, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += v[j];
             }
+        };
+        uint64_t r = r0 + lane;
+        constexpr int kAhead = 32 / (int)sizeof(T) / 2;    // 128 bytes a thread in flight
+        for (; r + (kAhead - 1) * kStatLanes < r1; r += kAhead * kStatLanes) {
+            Raw8<T> v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) v[i] = fetch_raw8<T, VEC>(x + (r + i * kStatLanes) * ldx, c, cols);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) take(v[i]);
         }
+        for (; r < r1; r += kStatLanes) take(fetch_raw8<T, VEC>(x + r * ldx, c, cols));
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        sh_top[lane][cg * 8 + j] = top[j];
-        sh_sum[lane][cg * 8 + j] = sum[j];
+    for (int j = 0; j < kWords; ++j) sh_top[lane][cg * kWords + j] = top[j];
+    if (SUMS) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sh_sum[lane][cg * 8 + j] = sum[j];
     }
     __syncthreads();
-    const uint64_t col = (uint64_t)blockIdx.x * kStatCols + threadIdx.x;
-    if (col >= cols) return;
+    const uint64_t col = c0 + threadIdx.x;
+    if (col >= c_last) return;
+    constexpr int kPer = 4 / (int)sizeof(T);               // elements in a word
     uint32_t t = 0;
-    float s = 0.f;
 #pragma unroll
-    for (int l = 0; l < kStatLanes; ++l) {
-        t = max(t, sh_top[l][threadIdx.x]);
-        s += sh_sum[l][threadIdx.x];
+    for (int l = 0; l < kStatLanes; ++l) t = top_word<T>(sh_top[l][threadIdx.x / kPer], t);
+    if (kPer == 2) t = threadIdx.x & 1 ? t >> 16 : t & 0xFFFFu;
+    atomicMax(tops + col, top_bits<T>(t));
+    if (SUMS) {
+        float s = 0.f;
+#pragma unroll
+        for (int l = 0; l < kStatLanes; ++l) s += sh_sum[l][threadIdx.x];
+        sums[(uint64_t)blockIdx.y * cols + col] = s;
     }
-    tops[(uint64_t)blockIdx.y * cols + col] = t;
-    if (sums) sums[(uint64_t)blockIdx.y * cols + col] = s;
 }
 
 // Codes, transposed.  A CTA owns 64 columns and kRowsPerCta rows, 128 rows at a time: a thread codes 4 rows x 8
 // columns, packs the four rows of a column into a word (rows are contiguous in the output), and the words
-// cross the CTA through shared memory so that a warp writes 128 contiguous bytes of one column.
+// cross the CTA through shared memory so that a warp writes 128 contiguous bytes of one column.  The next 128
+// rows' loads are issued before that.
 constexpr int kColTile = 64, kRowTile = 128, kRowsPerCta = 512;
 template <typename T, bool VEC, bool DRAW>
-__global__ void __launch_bounds__(256) quant8_cols_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx,
-                                                          const uint32_t* __restrict__ tops, const float* __restrict__ sums, uint32_t chunks,
-                                                          int8_t* __restrict__ q, uint64_t ldq, float* __restrict__ scale,
+__global__ void __launch_bounds__(256) quant8_cols_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, uint64_t c_first,
+                                                          uint64_t c_last, const uint32_t* __restrict__ tops, const float* __restrict__ sums,
+                                                          uint32_t chunks, int8_t* __restrict__ q, uint64_t ldq, float* __restrict__ scale,
                                                           float* __restrict__ colsum, const __grid_constant__ DrawArgs draw) {
     __shared__ uint32_t words[kColTile][kRowTile / 4 + 1];
-    __shared__ uint32_t sh_top[4][kColTile];
-    __shared__ float sh_inv[kColTile];
-    const uint32_t tiles = (uint32_t)((cols + kColTile - 1) / kColTile), slab = blockIdx.x / tiles;
-    const uint64_t c0 = (uint64_t)(blockIdx.x - slab * tiles) * kColTile;
-    {
-        const uint32_t lc = threadIdx.x & 63, quarter = threadIdx.x >> 6;
-        uint32_t t = 0;
-        if (c0 + lc < cols)
-            for (uint32_t k = quarter; k < chunks; k += 4) t = max(t, __ldg(tops + (uint64_t)k * cols + c0 + lc));
-        sh_top[quarter][lc] = t;
-        __syncthreads();
-        if (threadIdx.x < kColTile) {
-            t = max(max(sh_top[0][lc], sh_top[1][lc]), max(sh_top[2][lc], sh_top[3][lc]));
-            const LineScale s = line_scale(t);
-            sh_inv[lc] = s.inv;
-            if (slab == 0 && c0 + lc < cols) {
-                scale[c0 + lc] = s.scale;
-                if (colsum) {
-                    float a = 0.f;
-                    for (uint32_t k = 0; k < chunks; ++k) a += __ldg(sums + (uint64_t)k * cols + c0 + lc);
-                    colsum[c0 + lc] = a;
-                }
-            }
-        }
-        __syncthreads();
-    }
+    __shared__ float sh_inv[kColTile], sh_sum[4][kColTile];
+    grid_wait();
+    grid_go();
+    const uint32_t tiles = (uint32_t)((c_last - c_first + kColTile - 1) / kColTile), slab = blockIdx.x / tiles;
+    const uint64_t c0 = c_first + (uint64_t)(blockIdx.x - slab * tiles) * kColTile;
     const uint32_t cg = threadIdx.x & 7, rg = threadIdx.x >> 3;       // eight columns, four rows
     const uint64_t c = c0 + cg * 8;
+    const uint64_t first = (uint64_t)slab * kRowsPerCta;
+    const uint64_t last = first + kRowsPerCta < rows ? first + kRowsPerCta : rows;
+    Raw8<T> v[4];
+    const auto fetch = [&](uint64_t r0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t r = r0 + rg * 4 + i;
+            v[i] = r < last && c < c_last ? fetch_raw8<T, VEC>(x + r * ldx, c, cols) : zero_raw8<T>();
+        }
+    };
+    fetch(first);
+    if (threadIdx.x < kColTile) {
+        const uint64_t col = c0 + threadIdx.x;
+        const LineScale s = line_scale(col < c_last ? __ldg(tops + col) : 0u);
+        sh_inv[threadIdx.x] = s.inv;
+        if (slab == 0 && col < c_last) scale[col] = s.scale;
+    }
+    if (slab == 0 && colsum) {                             // the chunks' sums: a quarter to a thread, the quarters in order
+        const uint32_t lc = threadIdx.x & 63, quarter = threadIdx.x >> 6;
+        float a = 0.f;
+        if (c0 + lc < c_last) {
+#pragma unroll 8
+            for (uint32_t k = chunks * quarter / 4; k < chunks * (quarter + 1) / 4; ++k) a += __ldg(sums + (uint64_t)k * cols + c0 + lc);
+        }
+        sh_sum[quarter][lc] = a;
+    }
+    __syncthreads();
+    if (slab == 0 && colsum && threadIdx.x < kColTile && c0 + threadIdx.x < c_last)
+        colsum[c0 + threadIdx.x] = (sh_sum[0][threadIdx.x] + sh_sum[1][threadIdx.x]) + (sh_sum[2][threadIdx.x] + sh_sum[3][threadIdx.x]);
     float inv[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) inv[j] = sh_inv[cg * 8 + j];
-    const uint64_t first = (uint64_t)slab * kRowsPerCta;
-    const uint64_t last = first + kRowsPerCta < rows ? first + kRowsPerCta : rows;
     const uint64_t padded = (rows + 15) / 16 * 16;
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (uint64_t r0 = first; r0 < last; r0 += kRowTile) {
@@ -155,74 +182,87 @@ __global__ void __launch_bounds__(256) quant8_cols_kernel(const T* __restrict__ 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint64_t r = r0 + rg * 4 + i;
-            float v[8] = {};
-            if (r < rows && c < cols) fetch8<T, VEC>(x + r * ldx, c, cols, v);
+            float f[8];
+            widen8(v[i], f);
             uint32_t w[8] = {};
             if constexpr (DRAW) {
                 const uint4 wa = draw_words(draw, (uint32_t)(c >> 2), (uint32_t)r), wb = draw_words(draw, (uint32_t)(c >> 2) + 1, (uint32_t)r);
                 w[0] = wa.x; w[1] = wa.y; w[2] = wa.z; w[3] = wa.w; w[4] = wb.x; w[5] = wb.y; w[6] = wb.z; w[7] = wb.w;
             }
+            // (a column that is zero or not finite has inv = 0: code zero also where 0 * x is NaN; rows past the end read as
+            // zero, and floor(0 + u) = 0)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) b[i][j] = (r < rows && inv[j] != 0.f) ? code_bits<DRAW>(v[j], inv[j], w[j]) : 0u;
+            for (int j = 0; j < 8; ++j) b[i][j] = inv[j] != 0.f ? code_bits<DRAW>(f[j], inv[j], w[j]) : 0u;
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) words[cg * 8 + j][rg] = pack_bytes(b[0][j], b[1][j], b[2][j], b[3][j]);
         __syncthreads();
+        if (r0 + kRowTile < last) fetch(r0 + kRowTile);
         const uint64_t r = r0 + lane * 4;
         if (r < padded) {
 #pragma unroll
             for (int k = 0; k < kColTile / 8; ++k) {
                 const uint32_t lc = warp + 8 * k;
-                if (c0 + lc < cols) *reinterpret_cast<uint32_t*>(q + (c0 + lc) * ldq + r) = words[lc][lane];
+                if (c0 + lc < c_last) *reinterpret_cast<uint32_t*>(q + (c0 + lc) * ldq + r) = words[lc][lane];
             }
         }
         __syncthreads();
     }
 }
 
-uint32_t column_chunks(uint64_t rows, uint64_t cols) {
-    const uint64_t blocks = (cols + kStatCols - 1) / kStatCols;
-    uint64_t chunks = (148 * 4 + blocks - 1) / blocks;      // about four CTAs an SM
+// Columns of a panel: what 32 MB hold, in whole CTAs.
+uint64_t panel_columns(uint64_t rows, uint64_t cols, uint64_t element) {
+    uint64_t n = (32ull << 20) / (rows * element) / kStatCols * kStatCols;
+    if (n < kStatCols) n = kStatCols;
+    return n < cols ? n : cols;
+}
+// Row chunks of the statistics: about four CTAs an SM, 64 rows at least.
+uint32_t column_chunks(uint64_t rows, uint64_t panel) {
+    const uint64_t blocks = (panel + kStatCols - 1) / kStatCols;
+    uint64_t chunks = (4 * 148 + blocks - 1) / blocks;
     const uint64_t most = (rows + 63) / 64;
     if (chunks > most) chunks = most;
-    if (chunks > 64) chunks = 64;
     return chunks < 1 ? 1u : (uint32_t)chunks;
 }
 
 template <typename T, bool VEC, bool DRAW>
 cudaError_t rows_launch(const void* x, uint64_t rows, uint64_t cols, uint64_t ldx, const DrawArgs& d, int8_t* q, uint64_t ldq,
                         float* scale, cudaStream_t st) {
-    // a warp a row up to 1024 columns, eight rows a CTA; above, two groups of eight columns a thread
+    // a warp a row while it can hold one, eight rows a CTA; above, as many threads as hold the row
     const uint64_t groups = (cols + 7) / 8;
     dim3 block(32, 8);
-    if (groups > 32 * kHold) {
-        uint64_t t = (groups + 1) / 2;
-        t = (t + 31) / 32 * 32;
-        block = dim3((unsigned)(t > 512 ? 512 : t), 1);
+    if (groups > 32 * kHold<T>) {
+        const uint64_t t = (groups + 32 * kHold<T> - 1) / (32 * kHold<T>) * 32;
+        block = dim3((unsigned)(t > 1024 ? 1024 : t), 1);
     }
     const unsigned grid = (unsigned)((rows + block.y - 1) / block.y);
-    quant8_rows_kernel<T, VEC, DRAW><<<grid, block, 0, st>>>(static_cast<const T*>(x), rows, cols, ldx, q, ldq, scale, d);
-    return cudaGetLastError();
+    return launch_layer(quant8_rows_kernel<T, VEC, DRAW>, grid, block, 0, 1, st, static_cast<const T*>(x), rows, cols, ldx, q, ldq, scale, d);
 }
 
 template <typename T, bool VEC>
 cudaError_t cols_launch(const void* x, uint64_t rows, uint64_t cols, uint64_t ldx, const tng_draw* draw, int8_t* q, uint64_t ldq,
                         float* scale, float* colsum, void* scratch, cudaStream_t st) {
-    const uint32_t chunks = column_chunks(rows, cols);
     uint32_t* tops = static_cast<uint32_t*>(scratch);
-    float* sums = colsum ? reinterpret_cast<float*>(tops + (uint64_t)chunks * cols) : nullptr;
-    const uint64_t per = (rows + chunks - 1) / chunks;
-    const dim3 sg((unsigned)((cols + kStatCols - 1) / kStatCols), chunks);
+    float* sums = reinterpret_cast<float*>(tops + cols);
     const T* px = static_cast<const T*>(x);
-    column_stats_kernel<T, VEC><<<sg, 256, 0, st>>>(px, rows, cols, ldx, per, tops, sums);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    // one dimension, columns fastest: y would end at 65535 slabs, and neighbours share the rows' lines
-    const uint64_t g = (cols + kColTile - 1) / kColTile * ((rows + kRowsPerCta - 1) / kRowsPerCta);
-    if (g >= (1ull << 31)) return cudaErrorInvalidValue;
-    if (draw) quant8_cols_kernel<T, VEC, true><<<(unsigned)g, 256, 0, st>>>(px, rows, cols, ldx, tops, sums, chunks, q, ldq, scale, colsum, make_draw(*draw, kTagRounding));
-    else quant8_cols_kernel<T, VEC, false><<<(unsigned)g, 256, 0, st>>>(px, rows, cols, ldx, tops, sums, chunks, q, ldq, scale, colsum, DrawArgs{});
-    return cudaGetLastError();
+    const uint64_t panel = panel_columns(rows, cols, sizeof(T));
+    const uint32_t chunks = column_chunks(rows, panel);
+    const uint64_t per = (rows + chunks - 1) / chunks, slabs = (rows + kRowsPerCta - 1) / kRowsPerCta;
+    if ((panel + kColTile - 1) / kColTile * slabs >= (1ull << 31)) return cudaErrorInvalidValue;
+    cudaError_t e = cudaMemsetAsync(tops, 0, cols * 4, st);
+    const DrawArgs d = draw ? make_draw(*draw, kTagRounding) : DrawArgs{};
+    for (uint64_t c0 = 0; c0 < cols && e == cudaSuccess; c0 += panel) {
+        const uint64_t c1 = c0 + panel < cols ? c0 + panel : cols;
+        const dim3 sg((unsigned)((c1 - c0 + kStatCols - 1) / kStatCols), chunks);
+        e = colsum ? launch_layer(column_stats_kernel<T, VEC, true>, sg, 256, 0, 1, st, px, rows, cols, ldx, c0, c1, per, tops, sums)
+                   : launch_layer(column_stats_kernel<T, VEC, false>, sg, 256, 0, 1, st, px, rows, cols, ldx, c0, c1, per, tops, sums);
+        if (e != cudaSuccess) break;
+        // one dimension, columns fastest: neighbours share the rows' lines
+        const unsigned g = (unsigned)((c1 - c0 + kColTile - 1) / kColTile * slabs);
+        e = draw ? launch_layer(quant8_cols_kernel<T, VEC, true>, g, 256, 0, 1, st, px, rows, cols, ldx, c0, c1, tops, sums, chunks, q, ldq, scale, colsum, d)
+                 : launch_layer(quant8_cols_kernel<T, VEC, false>, g, 256, 0, 1, st, px, rows, cols, ldx, c0, c1, tops, sums, chunks, q, ldq, scale, colsum, d);
+    }
+    return e;
 }
 
 template <typename T> bool rows_aligned(const void* x, uint64_t rows, uint64_t ldx) {
@@ -269,7 +309,9 @@ tng_status tng_quant8_rows(const void* x_dev, tng_dtype type, uint64_t rows, uin
 }
 
 size_t tng_quant8_cols_scratch_bytes(uint64_t rows, uint64_t cols) {
-    return (size_t)(((uint64_t)column_chunks(rows, cols) * cols * 8 + 255) / 256 * 256);
+    // maxima and the chunks' sums; chunks for the narrowest panel that any element type gives
+    const uint64_t panel = rows ? panel_columns(rows, cols, 4) : 1;
+    return (size_t)(((1 + (uint64_t)column_chunks(rows, panel)) * cols * 4 + 255) / 256 * 256);
 }
 
 tng_status tng_quant8_cols(const void* x_dev, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx, const tng_draw* draw,

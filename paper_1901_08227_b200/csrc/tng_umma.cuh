@@ -36,13 +36,12 @@ __device__ __forceinline__ void umma_s8(uint32_t tmem, uint64_t a, uint64_t b, u
                      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc),
                      "r"((uint32_t)accumulate) : "memory");
 }
-// Arrive on a barrier (GROUP = 2: on the same barrier of both CTAs) when every instruction issued so far is done.
-template <int GROUP> __device__ __forceinline__ void umma_commit(uint32_t bar) {
-    if constexpr (GROUP == 1)
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                     "h"((uint16_t)3) : "memory");
+// Arrive on a barrier when every instruction issued so far is done: this CTA's, or the same one of the CTAs of a mask.
+__device__ __forceinline__ void umma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint16_t ctas) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(ctas) : "memory");
 }
 __device__ __forceinline__ void umma_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void umma_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -121,19 +120,6 @@ __device__ __forceinline__ int cluster_ld(uint32_t remote) {
     int v;
     asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
     return v;
-}
-// Bounded wait whose arrivals may come from another CTA of the cluster; false = gave up.
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity) {
-    for (int i = 0; i < kSpinLimit; ++i) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok) : "r"(bar), "r"(parity), "r"(kConsumerNapNs) : "memory");
-        if (ok) return true;
-    }
-    return false;
 }
 
 }  // namespace tng

@@ -417,15 +417,17 @@ F32, BF16, F16 = 0, 1, 2
 _DTYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 
+_device = torch._C._cuda_getDevice
+
+
 def _matrix(t, name, dtype=None, shape=None):
     """A 2-D CUDA tensor of the current device with unit column stride -> (pointer, row stride)."""
-    if not t.is_cuda or t.dim() != 2 or (t.dtype not in _DTYPE if dtype is None else t.dtype != dtype):
-        raise TypeError(f"{name} must be a 2-D CUDA tensor of type {dtype or 'float32, bfloat16 or float16'}")
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} is not on the current CUDA device")
-    rows, cols = size = t.shape
-    if shape is not None and size != shape:
-        raise ValueError(f"{name} has shape {tuple(size)}, expected {tuple(shape)}")
+    if t.get_device() != _device() or (t.dtype not in _DTYPE if dtype is None else t.dtype != dtype):
+        raise TypeError(f"{name} must be a tensor on the current CUDA device of type {dtype or 'float32, bfloat16 or float16'}")
+    size = t.shape
+    if len(size) != 2 or (shape is not None and size != shape):
+        raise ValueError(f"{name} has shape {tuple(size)}, expected {'two dimensions' if shape is None else tuple(shape)}")
+    rows, cols = size
     ld, unit = t.stride()
     if unit != 1 and cols > 1:
         raise ValueError(f"{name} must have contiguous rows")
@@ -434,16 +436,14 @@ def _matrix(t, name, dtype=None, shape=None):
 
 def _codes(t, name, shape=None):
     p, ld = _matrix(t, name, torch.int8, shape)
-    return p, ld if t.shape[0] > 1 else -(-ld // 16) * 16
+    return p, ld if ld % 16 == 0 or t.shape[0] > 1 else -(-ld // 16) * 16
 
 
-def _vector(t, name, n, dtype=torch.float32):
+def _vector(t, name, n):
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        raise TypeError(f"{name} must be a contiguous CUDA {dtype} vector of {n} elements")
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} is not on the current CUDA device")
+    if t.dtype != torch.float32 or t.get_device() != _device() or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        raise TypeError(f"{name} must be a contiguous float32 vector of {n} elements on the current CUDA device")
     return t.data_ptr()
 
 
