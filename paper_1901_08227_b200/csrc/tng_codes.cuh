@@ -28,7 +28,7 @@ template <bool DRAW> __device__ __forceinline__ uint32_t code_bits(float x, floa
     const float v = __fmul_rn(x, inv);
     if constexpr (DRAW) {
         // cut before the floor: -127 <= t < 128 gives the same codes as cutting the floor to [-127, 127]
-        const float t = fminf(fmaxf(__fadd_rn(v, uniform24(word)), -127.f), 127.5f);
+        const float t = fminf(fmaxf(__fmaf_rn(__uint2float_rn(word >> 8), 0x1p-24f, v), -127.f), 127.5f);   // v + u, u exact
         return __float_as_uint(__fadd_rd(t, 12582912.f));
     } else {
         return __float_as_uint(__fadd_rn(v, 12582912.f));
@@ -39,10 +39,11 @@ __device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t 
 }
 
 // Eight codes of a row; a line with inv = 0 has code zero everywhere (0 * NaN would not).
-template <bool DRAW> __device__ __forceinline__ uint2 code8(const float (&v)[8], float inv, const DrawArgs& d, uint32_t group, uint32_t row) {
+template <bool DRAW> __device__ __forceinline__ uint2 code8(const float (&v)[8], float inv, const DrawArgs& d, const DrawRow& r, uint32_t group) {
     uint32_t w[8] = {};
     if constexpr (DRAW) {
-        const uint4 a = draw_words(d, 2 * group, row), b = draw_words(d, 2 * group + 1, row);
+        const uint64_t column = draw_column(2 * group);
+        const uint4 a = draw_words(d, r, column), b = draw_words(d, r, column + kPhiloxMul0);
         w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
     }
     uint32_t q[8];

@@ -20,6 +20,7 @@ struct DropArgs {
     uint64_t rows, cols, ldx, ldr, ldy;
     uint32_t threshold;    // keep when word >= threshold ...
     uint32_t none;         // ... unless everything is dropped (p = 1)
+    uint32_t lanes_log;    // log2 of the threads that share a segment of a row
     float inv_keep;
 };
 
@@ -34,101 +35,146 @@ template <typename T> __device__ __forceinline__ Raw8<T> load_stream8(const T* p
     return r;
 }
 
-// Rows that start on 16-byte boundaries: a thread takes eight columns of a row at a time (two Philox
-// calls), the groups of eight of all rows in one grid-stride sequence.  (row, group) advances by a fixed
-// step, so no division in the loop.
+// Eight elements: mask, scale, residual, store.
 template <typename T, bool RES>
-__global__ void __launch_bounds__(kThreads) dropout_kernel(const T* x, const T* res, T* y, const __grid_constant__ DropArgs a) {
+__device__ __forceinline__ void drop8(const Raw8<T>& rx, const Raw8<T>& rr, T* py, uint64_t column, const DrawRow& dr, const DropArgs& a) {
+    const uint4 w0 = draw_words(a.draw, dr, column), w1 = draw_words(a.draw, dr, column + kPhiloxMul0);
+    const uint32_t w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+    float v[8];
+    widen8(rx, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = kept(v[j], w[j], a);
+    if (RES) {
+        float r[8];
+        widen8(rr, r);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __fadd_rn(r[j], v[j]);
+    }
+    store8(py, v);
+}
+
+// Rows that start on 16-byte boundaries.  `lanes` threads (a power of two up to 32) take a segment of 32 lanes columns of
+// a row: four vectors of eight columns a thread, `lanes` vectors apart, their loads issued together.  WARP: 32 lanes (rows
+// of 1024 columns and up), so that the distances are constants.  Bound by issue slots as much as by memory: a wide
+// multiply takes three of them, 72 slots of Philox for four elements (after the two hoisted ones), so addresses, the row's
+// part of Philox and the walk over (row, segment) are paid once in 32 elements.
+template <typename T, bool RES, bool WARP>
+__global__ void __launch_bounds__(kThreads, 3) dropout_kernel(const T* x, const T* res, T* y, const __grid_constant__ DropArgs a) {
+    constexpr int kVec = 4;
     grid_wait();
     grid_go();
-    const uint32_t per_row = (uint32_t)((a.cols + 7) / 8);
-    const uint64_t total = a.rows * per_row, stride = (uint64_t)gridDim.x * kThreads;
-    const uint64_t first = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-    uint64_t row = first / per_row;
-    uint32_t g = (uint32_t)(first - row * per_row);
-    const uint64_t drow = stride / per_row;
-    const uint32_t dg = (uint32_t)(stride - drow * per_row);
-    for (uint64_t i = first; i < total; i += stride) {
-        const uint64_t c = (uint64_t)g * 8;
+    const uint32_t lanes_log = WARP ? 5u : a.lanes_log, cols = (uint32_t)a.cols;
+    const uint32_t lane = threadIdx.x & ((1u << lanes_log) - 1u), span = 8u << lanes_log;          // columns from one vector to the next
+    const uint32_t segs = (cols - 1) / (kVec * span) + 1;
+    const uint64_t units = a.rows * segs, stride = ((uint64_t)gridDim.x * kThreads) >> lanes_log;
+    uint64_t unit = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) >> lanes_log;
+    uint32_t row = (uint32_t)(unit / segs), seg = (uint32_t)(unit - (uint64_t)row * segs);
+    const uint32_t drow = (uint32_t)(stride / segs), dseg = (uint32_t)(stride - (uint64_t)drow * segs);
+    const uint64_t next = draw_column(span >> 2);
+    for (; unit < units; unit += stride) {
+        const uint32_t c = seg * (kVec * span) + lane * 8;
         const T* px = x + row * a.ldx + c;
         const T* pr = RES ? res + row * a.ldr + c : nullptr;
         T* py = y + row * a.ldy + c;
-        const bool whole = c + 8 <= a.cols;
-        Raw8<T> rx, rr;
-        if (whole) {
-            rx = load_stream8(px);
-            if (RES) rr = load_stream8(pr);
-        }
-        const uint4 w0 = draw_words(a.draw, 2 * g, (uint32_t)row), w1 = draw_words(a.draw, 2 * g + 1, (uint32_t)row);
-        const uint32_t w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-        if (whole) {
-            float v[8];
-            widen8(rx, v);
+        const DrawRow dr = draw_row(a.draw, row);
+        uint64_t column = draw_column(c >> 2);
+        Raw8<T> rx[kVec], rr[kVec];
+        if (c + (kVec - 1) * span + 8 <= cols) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = kept(v[j], w[j], a);
-            if (RES) {
-                float r[8];
-                widen8(rr, r);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = __fadd_rn(r[j], v[j]);
+            for (int u = 0; u < kVec; ++u) {
+                rx[u] = load_stream8(px + u * span);
+                if (RES) rr[u] = load_stream8(pr + u * span);
             }
-            store8(py, v);
-        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (c + j >= a.cols) break;
-                const float v = kept(to_f32(px[j]), w[j], a);
-                py[j] = from_f32<T>(RES ? __fadd_rn(to_f32(pr[j]), v) : v);
+            for (int u = 0; u < kVec; ++u, column += next) drop8<T, RES>(rx[u], rr[u], py + u * span, column, dr, a);
+        } else {                                           // the row ends in this segment
+#pragma unroll 1
+            for (uint32_t u = 0; u < kVec && c + u * span < cols; ++u, column += next) {
+                const uint32_t left = cols - (c + u * span);
+                if (left >= 8) {
+                    rx[0] = load_stream8(px + u * span);
+                    if (RES) rr[0] = load_stream8(pr + u * span);
+                    drop8<T, RES>(rx[0], rr[0], py + u * span, column, dr, a);
+                } else {
+                    for (uint32_t j = 0; j < left; ++j) {
+                        const uint4 w = draw_words(a.draw, dr, column + (j < 4 ? 0u : kPhiloxMul0));
+                        const uint32_t word = j & 2 ? (j & 1 ? w.w : w.z) : (j & 1 ? w.y : w.x);
+                        const float v = kept(to_f32(px[u * span + j]), word, a);
+                        py[u * span + j] = from_f32<T>(RES ? __fadd_rn(to_f32(pr[u * span + j]), v) : v);
+                    }
+                }
             }
         }
         row += drow;
-        g += dg;
-        if (g >= per_row) { g -= per_row; ++row; }
+        seg += dseg;
+        if (seg >= segs) { seg -= segs; ++row; }
     }
 }
 
-// Any other alignment: a warp takes 128 columns of a row, one Philox call a lane, and turns the four keep
-// bits a lane drew into four ballots; loads and stores then run over the columns lane by lane, so that
-// they are contiguous across the warp wherever the row starts.  (Eight scalar accesses by one thread
-// would touch every sector of the warp's span once an access.)
-template <typename T, bool RES>
-__global__ void __launch_bounds__(kThreads) dropout_any_kernel(const T* x, const T* res, T* y, const __grid_constant__ DropArgs a) {
+// Any alignment: a warp takes VEC times 128 columns of a row, one Philox call a lane and 128, and turns the four keep
+// bits a lane drew into four ballots; loads and stores then run over the columns lane by lane, so that they are
+// contiguous across the warp wherever the row starts.  (Eight scalar accesses by one thread would touch every sector of
+// the warp's span once an access.)  VEC = 1 has the shortest path for a thread: the one for small arrays.
+template <typename T, bool RES, bool WHOLE>
+__device__ __forceinline__ void drop128(T* py, uint32_t left, uint32_t lane, uint64_t column, const DrawRow& dr, const float (&v)[4], const float (&r)[4], const DropArgs& a) {
+    const uint4 w = draw_words(a.draw, dr, column);
+    const uint32_t b0 = __ballot_sync(kFullMask, w.x >= a.threshold), b1 = __ballot_sync(kFullMask, w.y >= a.threshold);
+    const uint32_t b2 = __ballot_sync(kFullMask, w.z >= a.threshold), b3 = __ballot_sync(kFullMask, w.w >= a.threshold);
+    // column 32 q + lane of the 128 is word lane % 4 of lane 8 q + lane / 4
+    const uint32_t lo = lane & 1 ? b1 : b0, hi = lane & 1 ? b3 : b2;
+    const uint32_t bits = a.none ? 0u : (lane & 2 ? hi : lo) >> (lane >> 2);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float k = bits >> (8 * q) & 1u ? __fmul_rn(v[q], a.inv_keep) : 0.f;
+        if (WHOLE || 32u * q + lane < left) py[32 * q] = from_f32<T>(RES ? __fadd_rn(r[q], k) : k);
+    }
+}
+template <typename T, bool RES, int VEC>
+__global__ void __launch_bounds__(kThreads, VEC == 1 ? 4 : 3) dropout_any_kernel(const T* x, const T* res, T* y, const __grid_constant__ DropArgs a) {
     grid_wait();
     grid_go();
-    const uint32_t lane = threadIdx.x & 31;
-    const uint32_t per_row = (uint32_t)((a.cols + 127) / 128);
-    const uint64_t total = a.rows * per_row, stride = (uint64_t)gridDim.x * (kThreads / 32);
-    const uint64_t first = (uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    uint64_t row = first / per_row;
-    uint32_t g = (uint32_t)(first - row * per_row);
-    const uint64_t drow = stride / per_row;
-    const uint32_t dg = (uint32_t)(stride - drow * per_row);
-    for (uint64_t i = first; i < total; i += stride) {
-        const uint64_t c = (uint64_t)g * 128 + lane;
-        const T* px = x + row * a.ldx;
-        const T* pr = RES ? res + row * a.ldr : nullptr;
-        float v[4], r[4];
+    const uint32_t lane = threadIdx.x & 31, cols = (uint32_t)a.cols, segs = (cols - 1) / (128 * VEC) + 1;
+    const uint64_t units = a.rows * segs, stride = (uint64_t)gridDim.x * (kThreads / 32);
+    uint64_t unit = (uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    uint32_t row = (uint32_t)(unit / segs), seg = (uint32_t)(unit - (uint64_t)row * segs);
+    const uint32_t drow = (uint32_t)(stride / segs), dseg = (uint32_t)(stride - (uint64_t)drow * segs);
+    const uint64_t next = draw_column(32);
+    for (; unit < units; unit += stride) {
+        const uint32_t c = seg * (128 * VEC);              // first column of the warp's segment
+        const T* px = x + row * a.ldx + c + lane;
+        const T* pr = RES ? res + row * a.ldr + c + lane : nullptr;
+        T* py = y + row * a.ldy + c + lane;
+        const DrawRow dr = draw_row(a.draw, row);
+        uint64_t column = draw_column(c / 4 + lane);
+        if (cols - c >= 128 * VEC) {
+            float v[VEC][4], r[VEC][4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const bool in = c + 32 * q < a.cols;
-            v[q] = in ? to_f32(px[c + 32 * q]) : 0.f;
-            r[q] = RES && in ? to_f32(pr[c + 32 * q]) : 0.f;
-        }
-        const uint4 w = draw_words(a.draw, 32 * g + lane, (uint32_t)row);
-        const uint32_t b0 = __ballot_sync(kFullMask, w.x >= a.threshold), b1 = __ballot_sync(kFullMask, w.y >= a.threshold);
-        const uint32_t b2 = __ballot_sync(kFullMask, w.z >= a.threshold), b3 = __ballot_sync(kFullMask, w.w >= a.threshold);
-        // column 32 q + lane of the 128 is word lane % 4 of lane 8 q + lane / 4
-        const uint32_t lo = lane & 1 ? b1 : b0, hi = lane & 1 ? b3 : b2;
-        const uint32_t bits = (lane & 2 ? hi : lo) >> (lane >> 2);
+            for (int u = 0; u < VEC; ++u)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (c + 32 * q >= a.cols) break;
-            const float k = ((bits >> (8 * q)) & 1u) && !a.none ? __fmul_rn(v[q], a.inv_keep) : 0.f;
-            y[row * a.ldy + c + 32 * q] = from_f32<T>(RES ? __fadd_rn(r[q], k) : k);
+                for (int q = 0; q < 4; ++q) {
+                    v[u][q] = to_f32(px[128 * u + 32 * q]);
+                    r[u][q] = RES ? to_f32(pr[128 * u + 32 * q]) : 0.f;
+                }
+#pragma unroll
+            for (int u = 0; u < VEC; ++u, column += next)
+                drop128<T, RES, true>(py + 128 * u, 128, lane, column, dr, v[u], r[u], a);
+        } else {
+#pragma unroll 1
+            for (uint32_t at = 0; at < cols - c; at += 128, column += next) {
+                const uint32_t left = cols - c - at;
+                float v[4], r[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const bool in = 32u * q + lane < left;
+                    v[q] = in ? to_f32(px[at + 32 * q]) : 0.f;
+                    r[q] = RES && in ? to_f32(pr[at + 32 * q]) : 0.f;
+                }
+                drop128<T, RES, false>(py + at, left, lane, column, dr, v, r, a);
+            }
         }
         row += drow;
-        g += dg;
-        if (g >= per_row) { g -= per_row; ++row; }
+        seg += dseg;
+        if (seg >= segs) { seg -= segs; ++row; }
     }
 }
 
@@ -139,10 +185,19 @@ cudaError_t launch_dropout(const void* x, const void* res, void* y, const DropAr
     const uint64_t e = sizeof(T);
     const bool vec = aligned(x, 16) && aligned(y, 16) && (!res || aligned(res, 16)) &&
                      (a.rows == 1 || ((a.ldx * e) % 16 == 0 && (a.ldy * e) % 16 == 0 && (!res || (a.ldr * e) % 16 == 0)));
-    const uint64_t work = vec ? a.rows * ((a.cols + 7) / 8) : a.rows * ((a.cols + 127) / 128) * 32;
-    const uint64_t want = (work + kThreads - 1) / kThreads, cap = (uint64_t)sm_count_now() * 8u;
+    // Small arrays (a wave of 128 columns a warp holds them) take the kernel with the least work a thread, whatever their
+    // alignment: 16 x 1024 bf16 1.6 us, 2.4 us with 32 elements a thread.
+    const uint64_t sms = (uint64_t)sm_count_now();
+    const bool small = a.rows * ((a.cols + 127) / 128) <= sms * 32, warp = a.lanes_log == 5;
+    const uint64_t span = 32ull << a.lanes_log;
+    const uint64_t work = small ? a.rows * ((a.cols + 127) / 128) * 32
+                          : vec ? a.rows * ((a.cols + span - 1) / span) << a.lanes_log : a.rows * ((a.cols + 511) / 512) * 32;
+    const uint64_t want = (work + kThreads - 1) / kThreads, cap = sms * 8u;
     const unsigned grid = (unsigned)(want < cap ? want : cap);
-    const auto kernel = vec ? (res ? dropout_kernel<T, true> : dropout_kernel<T, false>) : (res ? dropout_any_kernel<T, true> : dropout_any_kernel<T, false>);
+    const auto kernel = small ? (res ? dropout_any_kernel<T, true, 1> : dropout_any_kernel<T, false, 1>)
+                        : !vec ? (res ? dropout_any_kernel<T, true, 4> : dropout_any_kernel<T, false, 4>)
+                        : warp ? (res ? dropout_kernel<T, true, true> : dropout_kernel<T, false, true>)
+                               : (res ? dropout_kernel<T, true, false> : dropout_kernel<T, false, false>);
     return launch_layer(kernel, grid, kThreads, 0, 1, st, px, pr, py, a);
 }
 
@@ -164,6 +219,8 @@ extern "C" tng_status tng_dropout(const void* x_dev, tng_dtype type, uint64_t ro
     a.draw = make_draw(*draw, kTagDropout);
     a.rows = rows; a.cols = cols; a.ldx = ldx; a.ldr = ldr; a.ldy = ldy;
     const uint64_t grid24 = (uint64_t)ceil((double)p * 16777216.0);    // exact: p has 24 significant bits
+    a.lanes_log = 0;
+    while (a.lanes_log < 5 && (32ull << a.lanes_log) < cols) ++a.lanes_log;
     a.none = grid24 >= (1u << 24);
     a.threshold = a.none ? 0u : (uint32_t)grid24 << 8;
     a.inv_keep = a.none ? 0.f : 1.0f / (1.0f - p);

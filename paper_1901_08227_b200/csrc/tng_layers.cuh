@@ -14,17 +14,22 @@ namespace tng {
 // gradient coding never share a counter under one key; nor do rounding and dropout of one layer.
 constexpr uint32_t kTagRounding = 1u << 30, kTagDropout = 1u << 31;
 
-// What a kernel needs of a tng_draw: the round keys and the counter words that a launch shares.
+// What a kernel needs of a tng_draw: the round keys and the counter words that a launch shares, and what follows from
+// them alone in the first round.  Of the 20 wide multiplies of a call two depend only on these and on the row, and
+// one more only on the column, where neighbouring calls differ by a constant: see DrawRow and draw_words.
 struct DrawArgs {
     uint32_t rk[20];
-    uint32_t row0, word2, step;
+    uint32_t row0, step_key;       // step ^ second key of round 1
+    uint32_t hi_key, lo;           // word2's product of round 1: high word ^ first key, low word ^ first key of round 2
 };
 inline DrawArgs make_draw(const tng_draw& d, uint32_t tag) {
     DrawArgs a;
     philox_round_keys(d.seed_lo, d.seed_hi, a.rk);
     a.row0 = (uint32_t)d.row0;
-    a.word2 = d.layer + tag;
-    a.step = d.step;
+    a.step_key = d.step ^ a.rk[1];
+    const uint64_t p = (uint64_t)kPhiloxMul1 * (d.layer + tag);
+    a.hi_key = (uint32_t)(p >> 32) ^ a.rk[0];
+    a.lo = (uint32_t)p ^ a.rk[2];
     return a;
 }
 // Host checks shared by the calls that take a draw over `rows` rows.
@@ -32,9 +37,34 @@ inline bool draw_ok(const tng_draw* d, uint64_t rows) {
     return d->layer < (1u << 30) && d->row0 <= (1ull << 32) && rows <= (1ull << 32) - d->row0;
 }
 
+// The row's share of rounds 1 and 2.
+struct DrawRow {
+    uint32_t hi_key, lo;           // M0 * (round 1's first word): high word ^ second key of round 2, low word
+};
+__device__ __forceinline__ DrawRow draw_row(const DrawArgs& a, uint32_t row) {
+    const uint64_t p = static_cast<uint64_t>(kPhiloxMul0) * (a.hi_key ^ (a.row0 + row));
+    return {static_cast<uint32_t>(p >> 32) ^ a.rk[3], static_cast<uint32_t>(p)};
+}
+// M0 * col4, what the column brings to round 1; the next column group's is this + M0.
+__device__ __forceinline__ uint64_t draw_column(uint32_t col4) { return static_cast<uint64_t>(kPhiloxMul0) * col4; }
 // The four words of columns 4*col4 .. 4*col4+3 of a row (row counted from the draw's row0).
-__device__ __forceinline__ uint4 draw_words(const DrawArgs& a, uint32_t col4, uint32_t row) {
-    return philox4x32_10_rk(col4, a.row0 + row, a.word2, a.step, a.rk);
+__device__ __forceinline__ uint4 draw_words(const DrawArgs& a, const DrawRow& r, uint64_t column) {
+    // after round 1: (hi_key ^ row, lo, hi(column) ^ step_key, lo(column)); round 2 from that
+    const uint64_t p = static_cast<uint64_t>(kPhiloxMul1) * (static_cast<uint32_t>(column >> 32) ^ a.step_key);
+    uint32_t c0 = static_cast<uint32_t>(p >> 32) ^ a.lo, c1 = static_cast<uint32_t>(p);
+    uint32_t c2 = r.hi_key ^ static_cast<uint32_t>(column), c3 = r.lo;
+#pragma unroll
+    for (int round = 2; round < 10; ++round) {
+        const uint64_t p0 = static_cast<uint64_t>(kPhiloxMul0) * c0;
+        const uint64_t p1 = static_cast<uint64_t>(kPhiloxMul1) * c2;
+        const uint32_t n0 = static_cast<uint32_t>(p1 >> 32) ^ c1 ^ a.rk[2 * round];
+        const uint32_t n2 = static_cast<uint32_t>(p0 >> 32) ^ c3 ^ a.rk[2 * round + 1];
+        c1 = static_cast<uint32_t>(p1);
+        c3 = static_cast<uint32_t>(p0);
+        c0 = n0;
+        c2 = n2;
+    }
+    return make_uint4(c0, c1, c2, c3);
 }
 
 template <typename T> __device__ __forceinline__ float to_f32(T v);

@@ -128,7 +128,7 @@ __device__ __forceinline__ void stream_tokens(const X* x, uint64_t ldx, const fl
                     if (g < groups) {
                         float v[8];
                         widen8(fetch(g), v);
-                        w = code8<false>(v, s.inv, DrawArgs{}, 0, 0);
+                        w = code8<false>(v, s.inv, DrawArgs{}, DrawRow{}, 0);
                     }
                     dst[g] = w;
                 }

@@ -42,10 +42,12 @@ __global__ void quant8_rows_kernel(const T* __restrict__ x, uint64_t rows, uint6
     if (threadIdx.x == 0) scale[row] = s.scale;
     const uint32_t out_groups = (uint32_t)((cols + 15) / 16 * 2);      // zeros up to the next multiple of 16
     uint2* dst = reinterpret_cast<uint2*>(q + row * ldq);
+    DrawRow dr = {};
+    if constexpr (DRAW) dr = draw_row(draw, (uint32_t)row);
     const auto put = [&](uint32_t g, const Raw8<T>& r) {
         float f[8];
         widen8(r, f);
-        dst[g] = g < groups ? code8<DRAW>(f, s.inv, draw, g, (uint32_t)row) : make_uint2(0u, 0u);
+        dst[g] = g < groups ? code8<DRAW>(f, s.inv, draw, dr, g) : make_uint2(0u, 0u);
     };
 #pragma unroll
     for (int h = 0; h < kHold<T>; ++h) {
@@ -65,7 +67,7 @@ __global__ void quant8_rows_kernel(const T* __restrict__ x, uint64_t rows, uint6
 // added in order by the second pass.
 constexpr int kStatCols = 256, kStatLanes = 8;
 template <typename T, bool VEC, bool SUMS>
-__global__ void __launch_bounds__(256) column_stats_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, uint64_t c_first,
+__global__ void __launch_bounds__(256, 4) column_stats_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, uint64_t c_first,
                                                            uint64_t c_last, uint64_t rows_per_chunk, uint32_t* __restrict__ tops,
                                                            float* __restrict__ sums) {
     constexpr int kWords = 2 * (int)sizeof(T);
@@ -92,7 +94,7 @@ __global__ void __launch_bounds__(256) column_stats_kernel(const T* __restrict__
             }
         };
         uint64_t r = r0 + lane;
-        constexpr int kAhead = 32 / (int)sizeof(T) / 2;    // 128 bytes a thread in flight
+        constexpr int kAhead = 8 / (int)sizeof(T);          // 64 bytes a thread in flight
         for (; r + (kAhead - 1) * kStatLanes < r1; r += kAhead * kStatLanes) {
             Raw8<T> v[kAhead];
 #pragma unroll
@@ -131,7 +133,7 @@ __global__ void __launch_bounds__(256) column_stats_kernel(const T* __restrict__
 // rows' loads are issued before that.
 constexpr int kColTile = 64, kRowTile = 128, kRowsPerCta = 512;
 template <typename T, bool VEC, bool DRAW>
-__global__ void __launch_bounds__(256) quant8_cols_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, uint64_t c_first,
+__global__ void __launch_bounds__(256, DRAW ? 3 : 4) quant8_cols_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, uint64_t c_first,
                                                           uint64_t c_last, const uint32_t* __restrict__ tops, const float* __restrict__ sums,
                                                           uint32_t chunks, int8_t* __restrict__ q, uint64_t ldq, float* __restrict__ scale,
                                                           float* __restrict__ colsum, const __grid_constant__ DrawArgs draw) {
@@ -175,7 +177,7 @@ __global__ void __launch_bounds__(256) quant8_cols_kernel(const T* __restrict__ 
     float inv[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) inv[j] = sh_inv[cg * 8 + j];
-    const uint64_t padded = (rows + 15) / 16 * 16;
+    const uint64_t padded = (rows + 15) / 16 * 16, column = draw_column((uint32_t)(c >> 2));
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (uint64_t r0 = first; r0 < last; r0 += kRowTile) {
         uint32_t b[4][8];
@@ -186,7 +188,8 @@ __global__ void __launch_bounds__(256) quant8_cols_kernel(const T* __restrict__ 
             widen8(v[i], f);
             uint32_t w[8] = {};
             if constexpr (DRAW) {
-                const uint4 wa = draw_words(draw, (uint32_t)(c >> 2), (uint32_t)r), wb = draw_words(draw, (uint32_t)(c >> 2) + 1, (uint32_t)r);
+                const DrawRow dr = draw_row(draw, (uint32_t)r);
+                const uint4 wa = draw_words(draw, dr, column), wb = draw_words(draw, dr, column + kPhiloxMul0);
                 w[0] = wa.x; w[1] = wa.y; w[2] = wa.z; w[3] = wa.w; w[4] = wb.x; w[5] = wb.y; w[6] = wb.z; w[7] = wb.w;
             }
             // (a column that is zero or not finite has inv = 0: code zero also where 0 * x is NaN; rows past the end read as
