@@ -13,10 +13,14 @@ namespace {
 template <typename T> constexpr int kHold = 16 / (int)sizeof(T);       // groups of eight elements
 template <typename T, bool VEC, bool DRAW>
 __global__ void quant8_rows_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, int8_t* __restrict__ q,
-                                   uint64_t ldq, float* __restrict__ scale, const __grid_constant__ DrawArgs draw) {
+                                   uint64_t ldq, float* __restrict__ scale, uint32_t* __restrict__ clear, uint64_t n_clear,
+                                   const __grid_constant__ DrawArgs draw) {
     __shared__ uint32_t part[32];
     grid_wait();
     grid_go();
+    // what the launch after this one wants cleared (a gradient's column maxima)
+    const uint32_t threads = blockDim.x * blockDim.y, me = threadIdx.y * blockDim.x + threadIdx.x;
+    for (uint64_t i = (uint64_t)blockIdx.x * threads + me; i < n_clear; i += (uint64_t)gridDim.x * threads) clear[i] = 0u;
     const uint64_t row = (uint64_t)blockIdx.x * blockDim.y + threadIdx.y;
     if (row >= rows) return;                       // whole warps only: with blockDim.y > 1 there is no block barrier
     const T* src = x + row * ldx;
@@ -59,34 +63,54 @@ __global__ void quant8_rows_kernel(const T* __restrict__ x, uint64_t rows, uint6
 }
 
 // ---- columns -----------------------------------------------------------------------------------------
-// Two passes over a panel of columns that the L2 cache can hold, so that the second finds the panel there: largest |x|
-// and sum of every column, then the codes.
-//
+// Two passes, the first for the largest |x| and the sum of every column, the second for the codes; up to two matrices of
+// one type a launch (a gradient's dy and x).  (Panels of columns small enough for the L2 cache to hold between the passes
+// saved the second read but lost as much to the ends of twice as many launches: 16384 x 4096 bf16, 83 us in panels of
+// 64 MB, 76 us whole.)
+template <typename T> struct ColumnJob {
+    const T* x;
+    uint64_t rows, cols, ldx, rows_per_chunk;
+    uint32_t blocks, tiles, chunks;   // CTA columns of the first pass and of the second, row chunks of the first
+    uint32_t* tops;                // largest |x| as bit patterns, cleared before
+    float* sums;                   // chunks x cols, or nullptr
+    int8_t* q;
+    uint64_t ldq;
+    float *scale, *colsum;
+};
+template <typename T> struct ColumnJobs {
+    ColumnJob<T> job[2];
+    uint32_t first2;               // first CTA of the second matrix
+};
+
 // Statistics.  A thread owns eight columns and every eighth row of a chunk; a CTA owns 256 columns.  Maxima meet in
 // `tops` (cleared before) by atomic maximum of bit patterns, which no order changes; the chunks' sums are kept apart and
 // added in order by the second pass.
 constexpr int kStatCols = 256, kStatLanes = 8;
-template <typename T, bool VEC, bool SUMS>
-__global__ void __launch_bounds__(256, 4) column_stats_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, uint64_t c_first,
-                                                           uint64_t c_last, uint64_t rows_per_chunk, uint32_t* __restrict__ tops,
-                                                           float* __restrict__ sums) {
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256, 4) column_stats_kernel(const __grid_constant__ ColumnJobs<T> jobs) {
     constexpr int kWords = 2 * (int)sizeof(T);
     __shared__ uint32_t sh_top[kStatLanes][32 * kWords];
-    __shared__ float sh_sum[SUMS ? kStatLanes : 1][kStatCols];
+    __shared__ float sh_sum[kStatLanes][kStatCols];
     grid_wait();
     grid_go();
+    const bool second = blockIdx.x >= jobs.first2;
+    const ColumnJob<T>& job = jobs.job[second];
+    const uint32_t cta = blockIdx.x - (second ? jobs.first2 : 0), chunk = cta / job.blocks;
+    const uint64_t rows = job.rows, cols = job.cols, ldx = job.ldx;
+    const T* x = job.x;
+    const bool want_sums = job.sums != nullptr;
     const uint32_t cg = threadIdx.x & 31, lane = threadIdx.x >> 5;
-    const uint64_t c0 = c_first + (uint64_t)blockIdx.x * kStatCols, c = c0 + cg * 8;
-    const uint64_t r0 = (uint64_t)blockIdx.y * rows_per_chunk;
-    const uint64_t r1 = r0 + rows_per_chunk < rows ? r0 + rows_per_chunk : rows;
+    const uint64_t c0 = (uint64_t)(cta - chunk * job.blocks) * kStatCols, c = c0 + cg * 8;
+    const uint64_t r0 = chunk * job.rows_per_chunk;
+    const uint64_t r1 = r0 + job.rows_per_chunk < rows ? r0 + job.rows_per_chunk : rows;
     uint32_t top[kWords] = {};
     float sum[8] = {};
-    if (c < c_last) {
+    if (c < cols) {
         const auto take = [&](const Raw8<T>& r) {
             const uint32_t* w = reinterpret_cast<const uint32_t*>(&r);
 #pragma unroll
             for (int j = 0; j < kWords; ++j) top[j] = top_word<T>(w[j], top[j]);
-            if (SUMS) {
+            if (want_sums) {
                 float v[8];
                 widen8(r, v);
 #pragma unroll
@@ -106,24 +130,24 @@ __global__ void __launch_bounds__(256, 4) column_stats_kernel(const T* __restric
     }
 #pragma unroll
     for (int j = 0; j < kWords; ++j) sh_top[lane][cg * kWords + j] = top[j];
-    if (SUMS) {
+    if (want_sums) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) sh_sum[lane][cg * 8 + j] = sum[j];
     }
     __syncthreads();
     const uint64_t col = c0 + threadIdx.x;
-    if (col >= c_last) return;
+    if (col >= cols) return;
     constexpr int kPer = 4 / (int)sizeof(T);               // elements in a word
     uint32_t t = 0;
 #pragma unroll
     for (int l = 0; l < kStatLanes; ++l) t = top_word<T>(sh_top[l][threadIdx.x / kPer], t);
     if (kPer == 2) t = threadIdx.x & 1 ? t >> 16 : t & 0xFFFFu;
-    atomicMax(tops + col, top_bits<T>(t));
-    if (SUMS) {
+    atomicMax(job.tops + col, top_bits<T>(t));
+    if (want_sums) {
         float s = 0.f;
 #pragma unroll
         for (int l = 0; l < kStatLanes; ++l) s += sh_sum[l][threadIdx.x];
-        sums[(uint64_t)blockIdx.y * cols + col] = s;
+        job.sums[(uint64_t)chunk * cols + col] = s;
     }
 }
 
@@ -131,97 +155,117 @@ __global__ void __launch_bounds__(256, 4) column_stats_kernel(const T* __restric
 // columns, packs the four rows of a column into a word (rows are contiguous in the output), and the words
 // cross the CTA through shared memory so that a warp writes 128 contiguous bytes of one column.  The next 128
 // rows' loads are issued before that.
-constexpr int kColTile = 64, kRowTile = 128, kRowsPerCta = 512;
+constexpr int kColTile = 64, kRowTile = 128, kRowsPerCta = 256;
 template <typename T, bool VEC, bool DRAW>
-__global__ void __launch_bounds__(256, DRAW ? 3 : 4) quant8_cols_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, uint64_t c_first,
-                                                          uint64_t c_last, const uint32_t* __restrict__ tops, const float* __restrict__ sums,
-                                                          uint32_t chunks, int8_t* __restrict__ q, uint64_t ldq, float* __restrict__ scale,
-                                                          float* __restrict__ colsum, const __grid_constant__ DrawArgs draw) {
-    __shared__ uint32_t words[kColTile][kRowTile / 4 + 1];
+__global__ void __launch_bounds__(256, DRAW ? 3 : 4) quant8_cols_kernel(const __grid_constant__ ColumnJobs<T> jobs, const __grid_constant__ DrawArgs draw) {
+    __shared__ uint32_t words[2][kColTile][kRowTile / 4 + 1];
     __shared__ float sh_inv[kColTile], sh_sum[4][kColTile];
     grid_wait();
     grid_go();
-    const uint32_t tiles = (uint32_t)((c_last - c_first + kColTile - 1) / kColTile), slab = blockIdx.x / tiles;
-    const uint64_t c0 = c_first + (uint64_t)(blockIdx.x - slab * tiles) * kColTile;
+    const bool second = blockIdx.x >= jobs.first2;
+    const ColumnJob<T>& job = jobs.job[second];
+    const uint32_t cta = blockIdx.x - (second ? jobs.first2 : 0), slab = cta / job.tiles;      // columns fastest: neighbours share the rows' lines
+    const uint64_t rows = job.rows, cols = job.cols, ldx = job.ldx, ldq = job.ldq;
+    const T* x = job.x;
+    const uint64_t c0 = (uint64_t)(cta - slab * job.tiles) * kColTile;
     const uint32_t cg = threadIdx.x & 7, rg = threadIdx.x >> 3;       // eight columns, four rows
     const uint64_t c = c0 + cg * 8;
     const uint64_t first = (uint64_t)slab * kRowsPerCta;
     const uint64_t last = first + kRowsPerCta < rows ? first + kRowsPerCta : rows;
+    const bool wide = VEC && c0 + kColTile <= cols;      // all 64 columns: vector loads, no tests on columns
     Raw8<T> v[4];
-    const auto fetch = [&](uint64_t r0) {
+    const T* px = x + (first + rg * 4) * ldx + c;
+    const auto fetch = [&](uint64_t r0) {                  // the next 128 rows, from r0
+        if (wide && r0 + kRowTile <= last) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint64_t r = r0 + rg * 4 + i;
-            v[i] = r < last && c < c_last ? fetch_raw8<T, VEC>(x + r * ldx, c, cols) : zero_raw8<T>();
+            for (int i = 0; i < 4; ++i) v[i] = load_raw8(px + i * ldx);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t r = r0 + rg * 4 + i;
+                v[i] = r < last && c < cols ? fetch_raw8<T, VEC>(x + r * ldx, c, cols) : zero_raw8<T>();
+            }
         }
+        px += kRowTile * ldx;
     };
     fetch(first);
+    bool bad = false;                                      // a column with a NaN or infinity: rare, its codes are zero
     if (threadIdx.x < kColTile) {
         const uint64_t col = c0 + threadIdx.x;
-        const LineScale s = line_scale(col < c_last ? __ldg(tops + col) : 0u);
+        const uint32_t top = col < cols ? __ldg(job.tops + col) : 0u;
+        const LineScale s = line_scale(top);
+        bad = top >= kInfBits;
         sh_inv[threadIdx.x] = s.inv;
-        if (slab == 0 && col < c_last) scale[col] = s.scale;
+        if (slab == 0 && col < cols) job.scale[col] = s.scale;
     }
-    if (slab == 0 && colsum) {                             // the chunks' sums: a quarter to a thread, the quarters in order
+    if (slab == 0 && job.colsum) {                         // the chunks' sums: a quarter to a thread, the quarters in order
         const uint32_t lc = threadIdx.x & 63, quarter = threadIdx.x >> 6;
         float a = 0.f;
-        if (c0 + lc < c_last) {
+        if (c0 + lc < cols) {
 #pragma unroll 8
-            for (uint32_t k = chunks * quarter / 4; k < chunks * (quarter + 1) / 4; ++k) a += __ldg(sums + (uint64_t)k * cols + c0 + lc);
+            for (uint32_t k = job.chunks * quarter / 4; k < job.chunks * (quarter + 1) / 4; ++k) a += __ldg(job.sums + (uint64_t)k * cols + c0 + lc);
         }
         sh_sum[quarter][lc] = a;
     }
-    __syncthreads();
-    if (slab == 0 && colsum && threadIdx.x < kColTile && c0 + threadIdx.x < c_last)
-        colsum[c0 + threadIdx.x] = (sh_sum[0][threadIdx.x] + sh_sum[1][threadIdx.x]) + (sh_sum[2][threadIdx.x] + sh_sum[3][threadIdx.x]);
+    const bool any_bad = __syncthreads_or(bad);
+    if (slab == 0 && job.colsum && threadIdx.x < kColTile && c0 + threadIdx.x < cols)
+        job.colsum[c0 + threadIdx.x] = (sh_sum[0][threadIdx.x] + sh_sum[1][threadIdx.x]) + (sh_sum[2][threadIdx.x] + sh_sum[3][threadIdx.x]);
     float inv[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) inv[j] = sh_inv[cg * 8 + j];
     const uint64_t padded = (rows + 15) / 16 * 16, column = draw_column((uint32_t)(c >> 2));
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (uint64_t r0 = first; r0 < last; r0 += kRowTile) {
-        uint32_t b[4][8];
+    int8_t* dst = job.q + (c0 + warp) * ldq + first + lane * 4;
+    uint32_t flip = 0;
+    for (uint64_t r0 = first; r0 < last; r0 += kRowTile, flip ^= 1) {
+        uint32_t pairs[8];                                 // codes of rows 0 and 1 in the low bytes, then all four
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint64_t r = r0 + rg * 4 + i;
-            float f[8];
-            widen8(v[i], f);
-            uint32_t w[8] = {};
-            if constexpr (DRAW) {
-                const DrawRow dr = draw_row(draw, (uint32_t)r);
-                const uint4 wa = draw_words(draw, dr, column), wb = draw_words(draw, dr, column + kPhiloxMul0);
-                w[0] = wa.x; w[1] = wa.y; w[2] = wa.z; w[3] = wa.w; w[4] = wb.x; w[5] = wb.y; w[6] = wb.z; w[7] = wb.w;
+        for (int h = 0; h < 2; ++h) {
+            uint32_t b[2][8];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float f[8];
+                widen8(v[2 * h + i], f);
+                uint32_t w[8] = {};
+                if constexpr (DRAW) {
+                    const DrawRow dr = draw_row(draw, (uint32_t)r0 + rg * 4 + 2 * h + i);
+                    const uint4 wa = draw_words(draw, dr, column), wb = draw_words(draw, dr, column + kPhiloxMul0);
+                    w[0] = wa.x; w[1] = wa.y; w[2] = wa.z; w[3] = wa.w; w[4] = wb.x; w[5] = wb.y; w[6] = wb.z; w[7] = wb.w;
+                }
+                // (rows past the end read as zero, a zero column has inv = 0: code zero, with a draw too, since floor(0 + u) = 0)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) b[i][j] = code_bits<DRAW>(f[j], inv[j], w[j]);
             }
-            // (a column that is zero or not finite has inv = 0: code zero also where 0 * x is NaN; rows past the end read as
-            // zero, and floor(0 + u) = 0)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) b[i][j] = inv[j] != 0.f ? code_bits<DRAW>(f[j], inv[j], w[j]) : 0u;
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t two = __byte_perm(b[0][j], b[1][j], 0x0040);
+                pairs[j] = h ? __byte_perm(pairs[j], two, 0x5410) : two;
+            }
+        }
+        if (any_bad) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (inv[j] == 0.f) pairs[j] = 0u;
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) words[cg * 8 + j][rg] = pack_bytes(b[0][j], b[1][j], b[2][j], b[3][j]);
-        __syncthreads();
+        for (int j = 0; j < 8; ++j) words[flip][cg * 8 + j][rg] = pairs[j];
+        __syncthreads();                                   // (the half written next was read before this barrier)
         if (r0 + kRowTile < last) fetch(r0 + kRowTile);
-        const uint64_t r = r0 + lane * 4;
-        if (r < padded) {
+        if (r0 + lane * 4 < padded) {
+            int8_t* to = dst;
 #pragma unroll
-            for (int k = 0; k < kColTile / 8; ++k) {
+            for (int k = 0; k < kColTile / 8; ++k, to += 8 * ldq) {
                 const uint32_t lc = warp + 8 * k;
-                if (c0 + lc < c_last) *reinterpret_cast<uint32_t*>(q + (c0 + lc) * ldq + r) = words[lc][lane];
+                if (wide || c0 + lc < cols) *reinterpret_cast<uint32_t*>(to) = words[flip][lc][lane];
             }
         }
-        __syncthreads();
+        dst += kRowTile;
     }
 }
 
-// Columns of a panel: what 32 MB hold, in whole CTAs.
-uint64_t panel_columns(uint64_t rows, uint64_t cols, uint64_t element) {
-    uint64_t n = (32ull << 20) / (rows * element) / kStatCols * kStatCols;
-    if (n < kStatCols) n = kStatCols;
-    return n < cols ? n : cols;
-}
 // Row chunks of the statistics: about four CTAs an SM, 64 rows at least.
-uint32_t column_chunks(uint64_t rows, uint64_t panel) {
-    const uint64_t blocks = (panel + kStatCols - 1) / kStatCols;
+uint32_t column_chunks(uint64_t rows, uint64_t cols) {
+    const uint64_t blocks = (cols + kStatCols - 1) / kStatCols;
     uint64_t chunks = (4 * 148 + blocks - 1) / blocks;
     const uint64_t most = (rows + 63) / 64;
     if (chunks > most) chunks = most;
@@ -230,7 +274,7 @@ uint32_t column_chunks(uint64_t rows, uint64_t panel) {
 
 template <typename T, bool VEC, bool DRAW>
 cudaError_t rows_launch(const void* x, uint64_t rows, uint64_t cols, uint64_t ldx, const DrawArgs& d, int8_t* q, uint64_t ldq,
-                        float* scale, cudaStream_t st) {
+                        float* scale, uint32_t* clear, uint64_t n_clear, cudaStream_t st) {
     // a warp a row while it can hold one, eight rows a CTA; above, as many threads as hold the row
     const uint64_t groups = (cols + 7) / 8;
     dim3 block(32, 8);
@@ -239,33 +283,17 @@ cudaError_t rows_launch(const void* x, uint64_t rows, uint64_t cols, uint64_t ld
         block = dim3((unsigned)(t > 1024 ? 1024 : t), 1);
     }
     const unsigned grid = (unsigned)((rows + block.y - 1) / block.y);
-    return launch_layer(quant8_rows_kernel<T, VEC, DRAW>, grid, block, 0, 1, st, static_cast<const T*>(x), rows, cols, ldx, q, ldq, scale, d);
+    return launch_layer(quant8_rows_kernel<T, VEC, DRAW>, grid, block, 0, 1, st, static_cast<const T*>(x), rows, cols, ldx, q, ldq, scale, clear, n_clear, d);
 }
 
-template <typename T, bool VEC>
-cudaError_t cols_launch(const void* x, uint64_t rows, uint64_t cols, uint64_t ldx, const tng_draw* draw, int8_t* q, uint64_t ldq,
-                        float* scale, float* colsum, void* scratch, cudaStream_t st) {
-    uint32_t* tops = static_cast<uint32_t*>(scratch);
-    float* sums = reinterpret_cast<float*>(tops + cols);
-    const T* px = static_cast<const T*>(x);
-    const uint64_t panel = panel_columns(rows, cols, sizeof(T));
-    const uint32_t chunks = column_chunks(rows, panel);
-    const uint64_t per = (rows + chunks - 1) / chunks, slabs = (rows + kRowsPerCta - 1) / kRowsPerCta;
-    if ((panel + kColTile - 1) / kColTile * slabs >= (1ull << 31)) return cudaErrorInvalidValue;
-    cudaError_t e = cudaMemsetAsync(tops, 0, cols * 4, st);
-    const DrawArgs d = draw ? make_draw(*draw, kTagRounding) : DrawArgs{};
-    for (uint64_t c0 = 0; c0 < cols && e == cudaSuccess; c0 += panel) {
-        const uint64_t c1 = c0 + panel < cols ? c0 + panel : cols;
-        const dim3 sg((unsigned)((c1 - c0 + kStatCols - 1) / kStatCols), chunks);
-        e = colsum ? launch_layer(column_stats_kernel<T, VEC, true>, sg, 256, 0, 1, st, px, rows, cols, ldx, c0, c1, per, tops, sums)
-                   : launch_layer(column_stats_kernel<T, VEC, false>, sg, 256, 0, 1, st, px, rows, cols, ldx, c0, c1, per, tops, sums);
-        if (e != cudaSuccess) break;
-        // one dimension, columns fastest: neighbours share the rows' lines
-        const unsigned g = (unsigned)((c1 - c0 + kColTile - 1) / kColTile * slabs);
-        e = draw ? launch_layer(quant8_cols_kernel<T, VEC, true>, g, 256, 0, 1, st, px, rows, cols, ldx, c0, c1, tops, sums, chunks, q, ldq, scale, colsum, d)
-                 : launch_layer(quant8_cols_kernel<T, VEC, false>, g, 256, 0, 1, st, px, rows, cols, ldx, c0, c1, tops, sums, chunks, q, ldq, scale, colsum, d);
-    }
-    return e;
+template <typename T, bool VEC> cudaError_t cols_launch(const ColumnJobs<T>& jobs, const DrawArgs* draw, uint64_t ctas1, uint64_t ctas2, cudaStream_t st) {
+    ColumnJobs<T> j = jobs;
+    j.first2 = (uint32_t)((uint64_t)j.job[0].blocks * j.job[0].chunks);
+    cudaError_t e = launch_layer(column_stats_kernel<T, VEC>, j.first2 + j.job[1].blocks * j.job[1].chunks, 256, 0, 1, st, j);
+    if (e != cudaSuccess) return e;
+    j.first2 = (uint32_t)ctas1;
+    return draw ? launch_layer(quant8_cols_kernel<T, VEC, true>, (unsigned)(ctas1 + ctas2), 256, 0, 1, st, j, *draw)
+                : launch_layer(quant8_cols_kernel<T, VEC, false>, (unsigned)(ctas1 + ctas2), 256, 0, 1, st, j, DrawArgs{});
 }
 
 template <typename T> bool rows_aligned(const void* x, uint64_t rows, uint64_t ldx) {
@@ -275,22 +303,55 @@ template <typename T> bool rows_aligned(const void* x, uint64_t rows, uint64_t l
 }  // namespace
 
 cudaError_t launch_quant8_rows(const void* x, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx, const tng_draw* draw,
-                               int8_t* q, uint64_t ldq, float* scale, cudaStream_t st) {
+                               int8_t* q, uint64_t ldq, float* scale, uint32_t* clear, uint64_t n_clear, cudaStream_t st) {
     return with_type(type, [&](auto t) {
         using T = decltype(t);
-        const bool vec = rows_aligned<T>(x, rows, ldx);
         const DrawArgs d = draw ? make_draw(*draw, kTagRounding) : DrawArgs{};
-        if (vec) return draw ? rows_launch<T, true, true>(x, rows, cols, ldx, d, q, ldq, scale, st) : rows_launch<T, true, false>(x, rows, cols, ldx, d, q, ldq, scale, st);
-        return draw ? rows_launch<T, false, true>(x, rows, cols, ldx, d, q, ldq, scale, st) : rows_launch<T, false, false>(x, rows, cols, ldx, d, q, ldq, scale, st);
+        const auto launch = rows_aligned<T>(x, rows, ldx) ? (draw ? rows_launch<T, true, true> : rows_launch<T, true, false>)
+                                                          : (draw ? rows_launch<T, false, true> : rows_launch<T, false, false>);
+        return launch(x, rows, cols, ldx, d, q, ldq, scale, clear, n_clear, st);
     });
 }
 
-cudaError_t launch_quant8_cols(const void* x, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx, const tng_draw* draw,
-                               int8_t* q, uint64_t ldq, float* scale, float* colsum, void* scratch, cudaStream_t st) {
+uint64_t quant8_cols_scratch(uint64_t rows, uint64_t cols, bool sums) { return (1 + (sums ? (uint64_t)column_chunks(rows, cols) : 0)) * cols; }
+
+// Jobs of one type whose maxima (the first words of their scratch) are clear.  Two of them share the launches where
+// they are alike in alignment and neither is drawn.
+cudaError_t launch_quant8_cols(const Quant8Cols* jobs, int n, tng_dtype type, cudaStream_t st) {
     return with_type(type, [&](auto t) {
         using T = decltype(t);
-        return rows_aligned<T>(x, rows, ldx) ? cols_launch<T, true>(x, rows, cols, ldx, draw, q, ldq, scale, colsum, scratch, st)
-                                             : cols_launch<T, false>(x, rows, cols, ldx, draw, q, ldq, scale, colsum, scratch, st);
+        ColumnJobs<T> j = {};
+        uint64_t ctas[2] = {};
+        bool vec[2] = {};
+        for (int i = 0; i < n; ++i) {
+            const Quant8Cols& in = jobs[i];
+            ColumnJob<T>& o = j.job[i];
+            o.x = static_cast<const T*>(in.x);
+            o.rows = in.rows; o.cols = in.cols; o.ldx = in.ldx;
+            o.chunks = column_chunks(in.rows, in.cols);
+            o.rows_per_chunk = (in.rows + o.chunks - 1) / o.chunks;
+            o.blocks = (uint32_t)((in.cols + kStatCols - 1) / kStatCols);
+            o.tiles = (uint32_t)((in.cols + kColTile - 1) / kColTile);
+            o.tops = in.scratch;
+            o.sums = in.colsum ? reinterpret_cast<float*>(in.scratch + in.cols) : nullptr;
+            o.q = in.q; o.ldq = in.ldq; o.scale = in.scale; o.colsum = in.colsum;
+            ctas[i] = o.tiles * ((in.rows + kRowsPerCta - 1) / kRowsPerCta);
+            vec[i] = rows_aligned<T>(in.x, in.rows, in.ldx);
+        }
+        if (ctas[0] + ctas[1] >= (1ull << 31)) return cudaErrorInvalidValue;
+        const auto one = [&](const ColumnJobs<T>& k, const tng_draw* draw, bool v, uint64_t c1, uint64_t c2) {
+            const DrawArgs d = draw ? make_draw(*draw, kTagRounding) : DrawArgs{};
+            return v ? cols_launch<T, true>(k, draw ? &d : nullptr, c1, c2, st) : cols_launch<T, false>(k, draw ? &d : nullptr, c1, c2, st);
+        };
+        if (n == 1) return one(j, jobs[0].draw, vec[0], ctas[0], 0);
+        if (vec[0] == vec[1] && !jobs[0].draw && !jobs[1].draw) return one(j, nullptr, vec[0], ctas[0], ctas[1]);
+        for (int i = 0; i < 2; ++i) {
+            ColumnJobs<T> k = {};
+            k.job[0] = j.job[i];
+            const cudaError_t e = one(k, jobs[i].draw, vec[i], ctas[i], 0);
+            if (e != cudaSuccess) return e;
+        }
+        return cudaSuccess;
     });
 }
 
@@ -307,14 +368,12 @@ tng_status tng_quant8_rows(const void* x_dev, tng_dtype type, uint64_t rows, uin
     if (!type_ok(type) || cols < 1 || !dims_ok(rows, cols) || (draw && !draw_ok(draw, rows))) return TNG_ERR_INVALID_ARG;
     if (rows == 0) return TNG_OK;
     if (!matrix_ok(x_dev, type, cols, ldx) || !codes_ok(q_dev, cols, ldq) || !scale_dev || !aligned(scale_dev, 4)) return TNG_ERR_INVALID_ARG;
-    return launch_quant8_rows(x_dev, type, rows, cols, ldx, draw, q_dev, ldq, scale_dev, static_cast<cudaStream_t>(stream)) == cudaSuccess
+    return launch_quant8_rows(x_dev, type, rows, cols, ldx, draw, q_dev, ldq, scale_dev, nullptr, 0, static_cast<cudaStream_t>(stream)) == cudaSuccess
                ? TNG_OK : TNG_ERR_CUDA;
 }
 
 size_t tng_quant8_cols_scratch_bytes(uint64_t rows, uint64_t cols) {
-    // maxima and the chunks' sums; chunks for the narrowest panel that any element type gives
-    const uint64_t panel = rows ? panel_columns(rows, cols, 4) : 1;
-    return (size_t)(((1 + (uint64_t)column_chunks(rows, panel)) * cols * 4 + 255) / 256 * 256);
+    return (size_t)((quant8_cols_scratch(rows, cols, true) * 4 + 255) / 256 * 256);
 }
 
 tng_status tng_quant8_cols(const void* x_dev, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx, const tng_draw* draw,
@@ -328,8 +387,11 @@ tng_status tng_quant8_cols(const void* x_dev, tng_dtype type, uint64_t rows, uin
     }
     if (!matrix_ok(x_dev, type, cols, ldx) || !codes_ok(q_dev, rows, ldq) || !scratch_dev || !aligned(scratch_dev, 256))
         return TNG_ERR_INVALID_ARG;
-    return launch_quant8_cols(x_dev, type, rows, cols, ldx, draw, q_dev, ldq, scale_dev, colsum_dev, scratch_dev,
-                              static_cast<cudaStream_t>(stream)) == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    uint32_t* scratch = static_cast<uint32_t*>(scratch_dev);
+    if (cudaMemsetAsync(scratch, 0, cols * 4, st) != cudaSuccess) return TNG_ERR_CUDA;
+    const Quant8Cols job{x_dev, rows, cols, ldx, draw, q_dev, ldq, scale_dev, colsum_dev, scratch};
+    return launch_quant8_cols(&job, 1, type, st) == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
 }
 
 }  // extern "C"
