@@ -219,6 +219,7 @@ constexpr int kPairThreads = 320;
 constexpr uint32_t kPairTile = 256;
 constexpr uint32_t kStageStride = 32 * 33 * 4;             // staging of one warp
 constexpr uint32_t kPairStages = 6, kPairHalf = 128 * 128, kPairStage = 2 * kPairHalf;
+static_assert(128 * kPairTile * 4 <= kPairStages * kPairStage, "the stages also hold the sums");
 constexpr uint32_t kPairSmem = 1024 + kPairStages * kPairStage + 8 * kStageStride + 256;
 
 struct TileWalk {                                          // tile order: groups of eight tile rows, columns outside
@@ -399,12 +400,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             }
         }
         __syncthreads();
-        cluster_sync_all();
+        cluster_meet_all();                                // the odd CTA's memory is read until the last instruction of the even one
     } else {
-        // ---- one tile: hand the other pairs their columns, then add up and write out one's own
+        // ---- one tile: leave the other pairs their columns in shared memory, then add up and write out one's own.  The
+        // exchange runs at 18 bytes a cycle and CTA whether it is loads from the other CTAs' memories or bulk copies into them
+        // (64 KB a CTA in two parts, 3500 cycles); as loads it overlaps with the first columns' output.
         const uint32_t cols = kPairTile / parts, mine = part * cols;
-        int* sums = reinterpret_cast<int*>(stages);        // every copy has landed and every instruction has read its operands
-        bool ok = true;
+        int4* sums = reinterpret_cast<int4*>(stages);      // [four columns][row]: a warp's access is contiguous; every copy
+        bool ok = true;                                    // has landed and every instruction has read its operands
         uint32_t tm, tn;
         walk.at(pair, tm, tn);
         const uint64_t row0 = (uint64_t)tm * kPairTile + row_in, col0 = (uint64_t)tn * kPairTile + mine;
@@ -425,16 +428,23 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                 uint32_t r[32];
                 tmem_ld32(tmem + ((quad * 32) << 16) + c, r);
                 tmem_wait_ld();
+                int4* to = sums + (c / 4) * 128 + quad * 32 + lane;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) sums[(c + j) * 128 + quad * 32 + lane] = (int)r[j];
+                for (int j = 0; j < 32; j += 4) to[j / 4 * 128] = make_int4((int)r[j], (int)r[j + 1], (int)r[j + 2], (int)r[j + 3]);
             }
             umma_fence_before();
         }
         cluster_sync_all();
         if (warp < 8) {
             umma_fence_after();
-            for (uint32_t q = 0; q < 2 * parts; ++q) ok = ok && cluster_ld(cluster_map(smem_u32((const void*)&sh_failed), q)) == 0;
-            ok = __all_sync(kFullMask, ok);
+            const auto fetch = [&](uint32_t c, uint32_t q, int4 (&v)[8]) {
+                const uint32_t from = cluster_map(data + ((c / 4) * 128 + quad * 32 + lane) * 16, ((part + q) & (parts - 1)) * 2 + rank);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = cluster_ld4(from + j * 2048);
+            };
+            int4 v[8];
+            fetch(mine + half * 32, 1, v);
+            ok = cluster_all_zero(smem_u32((const void*)&sh_failed), 2 * parts);
 #pragma unroll
             for (uint32_t i = 0; i < 2; ++i) {
                 if (i >= own) break;
@@ -442,17 +452,22 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                 uint32_t r[32];
                 tmem_ld32(tmem + ((quad * 32) << 16) + c, r);
                 tmem_wait_ld();
-                const uint32_t at = data + (c * 128 + quad * 32 + lane) * 4;
 #pragma unroll 1
                 for (uint32_t q = 1; q < parts; ++q) {
-                    const uint32_t from = cluster_map(at, ((part + q) & (parts - 1)) * 2 + rank);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) r[j] += (uint32_t)cluster_ld(from + j * 512);
+                    for (int j = 0; j < 8; ++j) {
+                        r[4 * j] += (uint32_t)v[j].x;
+                        r[4 * j + 1] += (uint32_t)v[j].y;
+                        r[4 * j + 2] += (uint32_t)v[j].z;
+                        r[4 * j + 3] += (uint32_t)v[j].w;
+                    }
+                    if (q + 1 < parts) fetch(c, q + 1, v);
                 }
-                finish_chunk<T>(p, r, ok, sa, cs[i], row0, (uint64_t)tn * kPairTile + c, align, stage, lane);
+                if (i + 1 < own) fetch(c + 64, 1, v);
+                finish_chunk<T>(p, r, ok, sa, cs[i], row0, col0 + (c - mine), align, stage, lane);
             }
         }
-        cluster_sync_all();                                // nobody leaves while its sums are being read
+        cluster_meet_all();                                // nobody leaves while its sums are being read
     }
     if (warp == 9) tmem_free<2>(tmem, 2 * kPairTile);
 }
@@ -480,7 +495,7 @@ __global__ void __launch_bounds__(kSlimThreads)
     __shared__ uint32_t sh_tmem;
     __shared__ volatile uint32_t sh_failed;
     const uint32_t data = (smem_u32(dyn) + 1023u) & ~1023u;
-    int* sums = reinterpret_cast<int*>(dyn + (data - smem_u32(dyn)));
+    int4* sums = reinterpret_cast<int4*>(dyn + (data - smem_u32(dyn)));     // [four columns][row]: a warp's access is contiguous
     const uint32_t bars = data + G::kStages * G::kStage;
     const auto full = [&](uint32_t s) { return bars + 16u * s; };
     const auto empty = [&](uint32_t s) { return bars + 16u * s + 8u; };
@@ -588,29 +603,37 @@ __global__ void __launch_bounds__(kSlimThreads)
                 uint32_t r[16];
                 tmem_ld16(tmem + ((warp * 32) << 16) + c, r);
                 tmem_wait_ld();
+                int4* to = sums + (c / 4) * 128 + warp * 32 + lane;
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sums[(c + j) * 128 + warp * 32 + lane] = n > 0 ? (int)r[j] : 0;
+                for (int j = 0; j < 16; j += 4) to[j / 4 * 128] = n > 0 ? make_int4((int)r[j], (int)r[j + 1], (int)r[j + 2], (int)r[j + 3]) : make_int4(0, 0, 0, 0);
             }
         }
         umma_fence_before();
         cluster_sync_all();                                // every part's sums are in place
         if (warp < 4) {
-            bool good = true;
-            for (uint32_t q = 0; q < split; ++q) good = good && cluster_ld(cluster_map(smem_u32((void*)&sh_failed), q)) == 0;
-            const uint32_t c0 = NT * part / split, c1 = NT * (part + 1) / split;
-            for (uint32_t c = c0; c < c1 && tok0 + c < p.m; c += 8) {          // 8 columns at a time, all loads in flight
-                int acc[8] = {};
-                for (uint32_t q = 0; q < split; ++q) {
-                    const uint32_t at = cluster_map(data + ((c * 128) + warp * 32 + lane) * 4, q);
+            const bool good = cluster_all_zero(smem_u32((const void*)&sh_failed), split);
+            const uint32_t cols = NT / split < 4 ? 4 : NT / split, c0 = cols * part;
+            const uint32_t at = data + (warp * 32 + lane) * 16;
+#pragma unroll 1
+            for (uint32_t c = c0; c < c0 + cols && c < NT && tok0 + c < p.m; c += 4) {
+                int4 v[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[j] += c + j < c1 ? cluster_ld(at + j * 512) : 0;
+                for (uint32_t q = 0; q < 8; ++q) v[q] = q < split ? cluster_ld4(cluster_map(at + c / 4 * 2048, q)) : make_int4(0, 0, 0, 0);
+                int4 a = v[0];
+#pragma unroll
+                for (int q = 1; q < 8; ++q) {
+                    a.x += v[q].x;
+                    a.y += v[q].y;
+                    a.z += v[q].z;
+                    a.w += v[q].w;
                 }
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < c1) put(c + j, acc[j], good);
+                put(c, a.x, good);
+                put(c + 1, a.y, good);
+                put(c + 2, a.z, good);
+                put(c + 3, a.w, good);
             }
         }
-        cluster_sync_all();                                // nobody leaves while its sums are being read
+        cluster_meet_all();                                // nobody leaves while its sums are being read
     }
     if (warp == 5) tmem_free<1>(tmem, G::kColumns);
 }

@@ -107,6 +107,10 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// The same as a mere meeting point: what the threads wrote is not made visible (no wait for their stores).
+__device__ __forceinline__ void cluster_meet_all() {
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
 // Address of `smem` (this CTA's) in the shared memory of CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t cluster_map(uint32_t smem, uint32_t rank) {
     uint32_t r;
@@ -120,6 +124,17 @@ __device__ __forceinline__ int cluster_ld(uint32_t remote) {
     int v;
     asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
     return v;
+}
+
+__device__ __forceinline__ int4 cluster_ld4(uint32_t remote) {              // 16-byte aligned
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(remote) : "memory");
+    return v;
+}
+// Whether a flag word of every CTA of the cluster is zero (whole warp, n <= 32 CTAs).
+__device__ __forceinline__ bool cluster_all_zero(uint32_t flag, uint32_t n) {
+    const uint32_t lane = threadIdx.x & 31;
+    return __all_sync(0xFFFFFFFFu, lane >= n || cluster_ld(cluster_map(flag, lane)) == 0);
 }
 
 }  // namespace tng
