@@ -3,6 +3,7 @@ marshal arguments (tensor -> device pointer, current CUDA stream -> void*)."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from pathlib import Path
 
 import torch
@@ -427,8 +428,8 @@ def _matrix(t, name, dtype=None, shape=None):
     size = t.shape
     if len(size) != 2 or (shape is not None and size != shape):
         raise ValueError(f"{name} has shape {tuple(size)}, expected {'two dimensions' if shape is None else tuple(shape)}")
-    rows, cols = size
     ld, unit = t.stride()
+    rows, cols = size
     if unit != 1 and cols > 1:
         raise ValueError(f"{name} must have contiguous rows")
     return t.data_ptr(), ld if rows > 1 or ld > cols else cols
@@ -456,6 +457,17 @@ def _scratch(buf, nbytes, like):
     elif not buf.is_cuda or not buf.is_contiguous() or buf.numel() * buf.element_size() < nbytes or buf.device != like.device:
         raise ValueError(f"scratch must be a contiguous CUDA tensor of at least {nbytes} bytes")
     return buf.data_ptr(), buf
+
+
+# sizes only: worth remembering, since a call through ctypes costs as much as the rest of the checks
+@functools.lru_cache(maxsize=4096)
+def _linear8_scratch(tokens, k):
+    return lib().tng_linear8_scratch_bytes(tokens, k)
+
+
+@functools.lru_cache(maxsize=4096)
+def _linear8_grad_scratch(tokens, k, n):
+    return lib().tng_linear8_grad_scratch_bytes(tokens, k, n)
 
 
 def empty_codes(lines, n, device="cuda"):
@@ -512,8 +524,10 @@ def linear8(x, w, sw, bias=None, out=None, scratch=None):
     pw, ldw = _codes(w, "w", (n, k))
     if out is None:
         out = x.new_empty((tokens, n))
-    po, ldo = _matrix(out, "out", x.dtype, (tokens, n))
-    ps, _keep = _scratch(scratch, lib().tng_linear8_scratch_bytes(tokens, k), x)
+        po, ldo = out.data_ptr(), n
+    else:
+        po, ldo = _matrix(out, "out", x.dtype, (tokens, n))
+    ps, _keep = _scratch(scratch, _linear8_scratch(tokens, k), x)
     _check(lib().tng_linear8(px, _DTYPE[x.dtype], tokens, k, ldx, pw, ldw, _vector(sw, "sw", n), n, _vector(bias, "bias", n), po, ldo,
                              ps, _stream()), "tng_linear8")
     return out
@@ -528,12 +542,15 @@ def linear8_grad(dy, x, wt, swt, draw=None, dx=None, dw=None, db=None, scratch=N
     k = x.shape[1]
     px, ldx = _matrix(x, "x", dy.dtype, (tokens, k))
     pw, ldw = _codes(wt, "wt", (k, n))
-    dx = dy.new_empty((tokens, k)) if dx is None else dx
-    dw = dy.new_empty((n, k), dtype=torch.float32) if dw is None else dw
-    db = dy.new_empty(n, dtype=torch.float32) if db is None else db
+    if dx is None:
+        dx = torch.empty_like(x) if x.is_contiguous() else x.new_empty((tokens, k))
+    if dw is None:
+        dw = dy.new_empty((n, k), dtype=torch.float32)
+    if db is None:
+        db = dy.new_empty(n, dtype=torch.float32)
     pdx, lddx = _matrix(dx, "dx", dy.dtype, (tokens, k))
     pdw, lddw = _matrix(dw, "dw", torch.float32, (n, k))
-    ps, _keep = _scratch(scratch, lib().tng_linear8_grad_scratch_bytes(tokens, k, n), dy)
+    ps, _keep = _scratch(scratch, _linear8_grad_scratch(tokens, k, n), dy)
     _check(lib().tng_linear8_grad(py, ldy, px, ldx, _DTYPE[dy.dtype], tokens, k, n, pw, ldw, _vector(swt, "swt", k), draw,
                                   pdx, lddx, pdw, lddw, _vector(db, "db", n), ps, _stream()), "tng_linear8_grad")
     return dx, dw, db
@@ -545,7 +562,9 @@ def dropout(x, p, draw, residual=None, out=None):
     rows, cols = x.shape
     if out is None:
         out = torch.empty_like(x)
-    po, ldo = _matrix(out, "out", x.dtype, x.shape)
+        po, ldo = out.data_ptr(), cols if rows == 1 else out.stride(0)
+    else:
+        po, ldo = _matrix(out, "out", x.dtype, x.shape)
     pr, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, x.shape)
     _check(lib().tng_dropout(px, _DTYPE[x.dtype], rows, cols, ldx, pr, ldr, p, draw, po, ldo, _stream()), "tng_dropout")
     return out
