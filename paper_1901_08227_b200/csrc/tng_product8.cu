@@ -17,47 +17,6 @@ __device__ __forceinline__ float scaled(int acc, float sa, float sb, bool has_bi
     return has_bias ? __fadd_rn(v, bias) : v;
 }
 
-__device__ __forceinline__ void st_global_v8(void* p, const uint32_t (&w)[8]) {   // 32-byte aligned
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
-}
-
-// 32 consecutive outputs of one row per lane.  `align` = what the output's rows are aligned to (32, 16 or less).
-// Where the rows are not aligned, or the tile ends inside the 32 columns, the values cross the warp through its
-// staging area (32 x 33 words), so that stores run along a row.
-template <typename T>
-__device__ __forceinline__ void store_chunk(T* out, uint64_t ldo, uint64_t row0, uint64_t rows, uint64_t col, uint64_t cols, const float (&v)[32],
-                                            uint32_t align, float* stage, uint32_t lane) {
-    if (align >= 16 && col + 32 <= cols) {
-        if (row0 + lane >= rows) return;
-        T* p = out + (row0 + lane) * ldo + col;
-        constexpr int kPer = 32 / (int)sizeof(T);          // elements in 32 bytes
-#pragma unroll
-        for (int i = 0; i < 32 / kPer; ++i) {
-            uint32_t w[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if constexpr (sizeof(T) == 4) w[j] = __float_as_uint(v[i * 8 + j]);
-                else w[j] = pack2<T>(v[i * 16 + 2 * j], v[i * 16 + 2 * j + 1]);
-            }
-            if (align >= 32) {
-                st_global_v8(p + i * kPer, w);
-            } else {
-                reinterpret_cast<uint4*>(p + i * kPer)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                reinterpret_cast<uint4*>(p + i * kPer)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) stage[lane * 33 + j] = v[j];
-        __syncwarp();
-        const uint32_t n = rows <= row0 ? 0u : (rows - row0 < 32 ? (uint32_t)(rows - row0) : 32u);
-        if (col + lane < cols)
-            for (uint32_t r = 0; r < n; ++r) out[(row0 + r) * ldo + col + lane] = from_f32<T>(stage[r * 33 + lane]);
-        __syncwarp();
-    }
-}
-
 // ---- at most 16 tokens: the weights are streamed past them ----------------------------------------------
 // Bound by reading b once.  The tokens' codes stay in shared memory; a CTA goes over tiles of eight rows of b, KS
 // warps sharing a tile along the contraction, 512 codes a warp and step: eight 16-byte loads a lane, the next
@@ -217,7 +176,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(cons
 // Warps: 0-7 write out (a quarter of the rows and half of the columns each), 8 feeds, 9 issues.
 constexpr int kPairThreads = 320;
 constexpr uint32_t kPairTile = 256;
-constexpr uint32_t kStageStride = 32 * 33 * 4;             // staging of one warp
+constexpr uint32_t kStageStride = 4096;                    // staging of one warp
 constexpr uint32_t kPairStages = 6, kPairHalf = 128 * 128, kPairStage = 2 * kPairHalf;
 static_assert(128 * kPairTile * 4 <= kPairStages * kPairStage, "the stages also hold the sums");
 constexpr uint32_t kPairSmem = 1024 + kPairStages * kPairStage + 8 * kStageStride + 256;
@@ -241,17 +200,31 @@ __device__ __forceinline__ ColumnScale column_scale(const Product8& p, uint64_t 
     return {in ? __ldg(p.sb + col) : 0.f, in && p.bias ? __ldg(p.bias + col) : 0.f};
 }
 
-// Scales and writes out 32 columns of a warp's 32 rows.  ok = false: NaN.
+// Scales 32 columns of a warp's 32 rows and writes them out through the warp's 4 KB of staging.  ok = false: NaN.
+// Rows of 16-byte multiples (TILES) go by copies of 64-byte wide boxes in the 64-byte swizzle (16-byte pieces by lane:
+// no bank conflicts), which clip at the matrix and run on while the next columns are scaled; others in rows of 32
+// elements by the warp.  (32-byte stores by each lane into its own row cost a cache line an access: 3500 cycles for
+// 32 x 32 fp32 against a stage's 513.)
 template <typename T>
-__device__ __forceinline__ void finish_chunk(const Product8& p, const uint32_t (&r)[32], bool ok, float sa, ColumnScale cs, uint64_t row0, uint64_t col,
-                                             uint32_t align, float* stage, uint32_t lane) {
-    stage[lane] = cs.sb;
-    stage[32 + lane] = cs.bias;
+__device__ __forceinline__ void finish_chunk(const Product8& p, const CUtensorMap* map_o, const uint32_t (&r)[32], bool ok, float sa, ColumnScale cs,
+                                             uint64_t row0, uint64_t col, bool tiles, unsigned char* stage, uint32_t flip, uint32_t lane) {
+    constexpr bool k32 = sizeof(T) == 4;                   // fp32: both 2 KB halves a time; 16 bits: the halves in turn
+    unsigned char* buf = stage + (k32 ? 0u : flip * 2048u);
+    if (tiles) {
+        if (lane == 0) {
+            if (k32) tile_store_wait_read<0>();
+            else tile_store_wait_read<1>();
+        }
+        __syncwarp();
+    }
+    float* scales = reinterpret_cast<float*>(buf);
+    scales[lane] = cs.sb;
+    scales[32 + lane] = cs.bias;
     __syncwarp();
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; j += 4) {
-        const float4 sb = *reinterpret_cast<const float4*>(stage + j), bi = *reinterpret_cast<const float4*>(stage + 32 + j);
+        const float4 sb = *reinterpret_cast<const float4*>(scales + j), bi = *reinterpret_cast<const float4*>(scales + 32 + j);
         v[j] = scaled((int)r[j], sa, sb.x, p.bias, bi.x);
         v[j + 1] = scaled((int)r[j + 1], sa, sb.y, p.bias, bi.y);
         v[j + 2] = scaled((int)r[j + 2], sa, sb.z, p.bias, bi.z);
@@ -262,13 +235,44 @@ __device__ __forceinline__ void finish_chunk(const Product8& p, const uint32_t (
         for (int j = 0; j < 32; ++j) v[j] = CUDART_NAN_F;
     }
     __syncwarp();
-    if (col < p.n) store_chunk<T>(static_cast<T*>(p.out), p.ldo, row0, p.m, col, p.n, v, align, stage, lane);
+    if (row0 >= p.m || col >= p.n) return;
+    if (tiles) {
+#pragma unroll
+        for (int i = 0; i < (k32 ? 8 : 4); ++i) {
+            uint4 w;
+            if constexpr (k32) w = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+            else w = make_uint4(pack2<T>(v[8 * i], v[8 * i + 1]), pack2<T>(v[8 * i + 2], v[8 * i + 3]), pack2<T>(v[8 * i + 4], v[8 * i + 5]), pack2<T>(v[8 * i + 6], v[8 * i + 7]));
+            *reinterpret_cast<uint4*>(buf + (i >> 2) * 2048 + lane * 64 + (((i & 3) ^ ((lane >> 1) & 3)) * 16)) = w;
+        }
+        smem_to_copies();
+        __syncwarp();
+        if (lane == 0) {
+            tile_store(map_o, (int32_t)col, (int32_t)row0, smem_u32(buf));
+            if (k32 && col + 16 < p.n) tile_store(map_o, (int32_t)col + 16, (int32_t)row0, smem_u32(buf) + 2048);
+        }
+    } else {
+        float* f = reinterpret_cast<float*>(stage);        // row r's column c at 32 r + (c ^ r)
+#pragma unroll
+        for (int j = 0; j < 32; ++j) f[lane * 32 + (j ^ lane)] = v[j];
+        __syncwarp();
+        const uint32_t n = p.m - row0 < 32 ? (uint32_t)(p.m - row0) : 32u;
+        if (col + lane < p.n) {
+            T* out = static_cast<T*>(p.out) + row0 * p.ldo + col + lane;
+            if (n == 32) {
+#pragma unroll
+                for (uint32_t i = 0; i < 32; ++i) out[i * p.ldo] = from_f32<T>(f[i * 32 + (lane ^ i)]);
+            } else {
+                for (uint32_t i = 0; i < n; ++i) out[i * p.ldo] = from_f32<T>(f[i * 32 + (lane ^ i)]);
+            }
+        }
+        __syncwarp();
+    }
 }
 
 template <typename T, bool SPLIT>
 __global__ void __launch_bounds__(kPairThreads, 1)
-    product8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Product8 p,
-                         uint32_t align, uint32_t split) {
+    product8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_o,
+                         const __grid_constant__ Product8 p, bool by_tiles, uint32_t split) {
     extern __shared__ unsigned char dyn[];
     __shared__ uint32_t sh_tmem;
     __shared__ volatile uint32_t sh_failed;
@@ -364,7 +368,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
     }
     __syncwarp();
-    float* stage = reinterpret_cast<float*>(stages + kPairStages * kPairStage) + warp * (kStageStride / 4);
+    unsigned char* stage = stages + kPairStages * kPairStage + warp * kStageStride;
     const uint32_t quad = warp & 3, half = warp >> 2, row_in = rank * 128 + quad * 32;
     if constexpr (!SPLIT) {
         if (warp < 8) {
@@ -395,10 +399,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                         __syncwarp();
                         if (lane == 0) cluster_arrive(cluster_map(acc_empty + 8 * acc, even));
                     }
-                    finish_chunk<T>(p, r, ok, sa, cs[ch], row0, col0 + ch * 32, align, stage, lane);
+                    finish_chunk<T>(p, &map_o, r, ok, sa, cs[ch], row0, col0 + ch * 32, by_tiles, stage, ch & 1u, lane);
                 }
             }
         }
+        if (warp < 8 && lane == 0) tile_store_wait_all();
         __syncthreads();
         cluster_meet_all();                                // the odd CTA's memory is read until the last instruction of the even one
     } else {
@@ -464,9 +469,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                     if (q + 1 < parts) fetch(c, q + 1, v);
                 }
                 if (i + 1 < own) fetch(c + 64, 1, v);
-                finish_chunk<T>(p, r, ok, sa, cs[i], row0, col0 + (c - mine), align, stage, lane);
+                finish_chunk<T>(p, &map_o, r, ok, sa, cs[i], row0, col0 + (c - mine), by_tiles, stage, i, lane);
             }
         }
+        if (warp < 8 && lane == 0) tile_store_wait_all();
+        __syncwarp();
         cluster_meet_all();                                // nobody leaves while its sums are being read
     }
     if (warp == 9) tmem_free<2>(tmem, 2 * kPairTile);
@@ -664,6 +671,17 @@ bool make_map(CUtensorMap* map, const int8_t* codes, uint64_t lines, uint64_t k,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Boxes of 64 bytes x 32 rows of the output.
+bool make_out_map(CUtensorMap* map, const Product8& p, uint32_t element) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {p.n, p.m}, strides[1] = {p.ldo * element};
+    const cuuint32_t boxes[2] = {64 / element, 32}, steps[2] = {1, 1};
+    return encode(map, element == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, p.out, dims, strides, boxes, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // The dynamic shared-memory opt-in of one kernel instantiation, once per device.
 template <typename K> cudaError_t allow_smem(K kernel, uint32_t bytes, PerDevice<bool>& done) {
     const int slot = device_slot();
@@ -682,10 +700,11 @@ template <typename T, bool SPLIT> cudaError_t launch_pair(const Product8& p, uin
     if (!make_map(&ma, p.a, p.m, p.k, p.lda, 128) || !make_map(&mb, p.b, p.n, p.k, p.ldb, 128)) return cudaErrorNotSupported;
     const uint64_t tiles = (p.m + 255) / 256 * ((p.n + 255) / 256), pairs = (uint64_t)sm_count_now() / 2;
     if (tiles >= (1ull << 31)) return cudaErrorInvalidValue;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p.out) | (p.m > 1 ? p.ldo * sizeof(T) : 0);
-    const uint32_t align = at % 32 == 0 ? 32u : at % 16 == 0 ? 16u : 1u;
+    const bool by_tiles = (reinterpret_cast<uintptr_t>(p.out) | p.ldo * sizeof(T)) % 16 == 0;
+    CUtensorMap mo = ma;
+    if (by_tiles && !make_out_map(&mo, p, sizeof(T))) return cudaErrorNotSupported;
     return launch_layer(kernel, (unsigned)(2 * (SPLIT ? tiles * split : tiles < pairs ? tiles : pairs)), kPairThreads, kPairSmem, 2 * split, st,
-                          ma, mb, p, align, split);
+                          ma, mb, mo, p, by_tiles, split);
 }
 
 // Clusters of `split` pairs that run at once on this device.

@@ -94,6 +94,16 @@ template <int GROUP> __device__ __forceinline__ void tile_load(uint32_t dst, con
             "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
             "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+// This CTA's shared memory into a box of the map, clipped to the matrix; x a multiple of 16 bytes, both >= 0.
+__device__ __forceinline__ void tile_store(const CUtensorMap* map, int32_t x, int32_t y, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// Until at most N of this thread's stores still read shared memory.
+template <int N> __device__ __forceinline__ void tile_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void tile_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// This thread's shared-memory writes become visible to copies issued after the next barrier.
+__device__ __forceinline__ void smem_to_copies() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void map_prefetch(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
