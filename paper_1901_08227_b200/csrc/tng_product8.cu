@@ -173,13 +173,14 @@ __global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(cons
 // for half the work, so small outputs split the contraction instead of the tile:
 // SPLIT: a cluster of S pairs takes S consecutive parts of one tile's contraction; pair q then adds the others' int32
 // sums, read from their shared memories, to its own for 256/S of the columns and writes those out.
-// Warps: 0-7 write out (a quarter of the rows and half of the columns each), 8 feeds, 9 issues.
-constexpr int kPairThreads = 320;
+// Warps: 0-15 write out (a quarter of the rows and of the columns each: with eight the last tile's output took 3 us), 16
+// feeds, 17 issues.
+constexpr int kPairThreads = 576;
 constexpr uint32_t kPairTile = 256;
-constexpr uint32_t kStageStride = 4096;                    // staging of one warp
+constexpr uint32_t kStageStride = 2048;                    // staging of one warp
 constexpr uint32_t kPairStages = 6, kPairHalf = 128 * 128, kPairStage = 2 * kPairHalf;
 static_assert(128 * kPairTile * 4 <= kPairStages * kPairStage, "the stages also hold the sums");
-constexpr uint32_t kPairSmem = 1024 + kPairStages * kPairStage + 8 * kStageStride + 256;
+constexpr uint32_t kPairSmem = 1024 + kPairStages * kPairStage + 16 * kStageStride + 256;
 
 struct TileWalk {                                          // tile order: groups of eight tile rows, columns outside
     uint32_t tiles_m, tiles_n;
@@ -200,85 +201,109 @@ __device__ __forceinline__ ColumnScale column_scale(const Product8& p, uint64_t 
     return {in ? __ldg(p.sb + col) : 0.f, in && p.bias ? __ldg(p.bias + col) : 0.f};
 }
 
-// Scales 32 columns of a warp's 32 rows and writes them out through the warp's 4 KB of staging.  ok = false: NaN.
-// Rows of 16-byte multiples (TILES) go by copies of 64-byte wide boxes in the 64-byte swizzle (16-byte pieces by lane:
-// no bank conflicts), which clip at the matrix and run on while the next columns are scaled; others in rows of 32
-// elements by the warp.  (32-byte stores by each lane into its own row cost a cache line an access: 3500 cycles for
+// Scales W columns of a warp's 32 rows and writes them out through the warp's 2 KB of staging.  ok = false: NaN.
+// TILES (rows of 16-byte multiples): W columns are 64 bytes, copied as a box in the 64-byte swizzle (16-byte pieces by
+// lane: no bank conflicts) that clips at the matrix and runs on while the next columns are scaled.  Else W = 16, two rows
+// of 16 elements an access.  (32-byte stores by each lane into its own row cost a cache line an access: 3500 cycles for
 // 32 x 32 fp32 against a stage's 513.)
-template <typename T>
-__device__ __forceinline__ void finish_chunk(const Product8& p, const CUtensorMap* map_o, const uint32_t (&r)[32], bool ok, float sa, ColumnScale cs,
-                                             uint64_t row0, uint64_t col, bool tiles, unsigned char* stage, uint32_t flip, uint32_t lane) {
-    constexpr bool k32 = sizeof(T) == 4;                   // fp32: both 2 KB halves a time; 16 bits: the halves in turn
-    unsigned char* buf = stage + (k32 ? 0u : flip * 2048u);
-    if (tiles) {
-        if (lane == 0) {
-            if (k32) tile_store_wait_read<0>();
-            else tile_store_wait_read<1>();
-        }
+template <typename T, int W, bool TILES>
+__device__ __forceinline__ void finish_chunk(const Product8& p, const CUtensorMap* map_o, const uint32_t (&r)[W], bool ok, float sa, ColumnScale cs,
+                                             uint32_t piece, uint64_t row0, uint64_t col, unsigned char* stage, uint32_t lane) {
+    static_assert(TILES ? W * sizeof(T) == 64 : W == 16, "2 KB of staging");
+    if (TILES) {
+        if (lane == 0) tile_store_wait_read<0>();
         __syncwarp();
     }
-    float* scales = reinterpret_cast<float*>(buf);
-    scales[lane] = cs.sb;
-    scales[32 + lane] = cs.bias;
+    float* scales = reinterpret_cast<float*>(stage);
+    if (W == 32 || (lane >> 4) == piece) {
+        scales[lane & (W - 1)] = cs.sb;
+        scales[W + (lane & (W - 1))] = cs.bias;
+    }
     __syncwarp();
-    float v[32];
+    float v[W];
 #pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-        const float4 sb = *reinterpret_cast<const float4*>(scales + j), bi = *reinterpret_cast<const float4*>(scales + 32 + j);
-        v[j] = scaled((int)r[j], sa, sb.x, p.bias, bi.x);
-        v[j + 1] = scaled((int)r[j + 1], sa, sb.y, p.bias, bi.y);
-        v[j + 2] = scaled((int)r[j + 2], sa, sb.z, p.bias, bi.z);
-        v[j + 3] = scaled((int)r[j + 3], sa, sb.w, p.bias, bi.w);
+    for (int j = 0; j < W; j += 4) {
+        const float4 sb = *reinterpret_cast<const float4*>(scales + j);
+        v[j] = __fmul_rn(__fmul_rn((float)(int)r[j], sa), sb.x);
+        v[j + 1] = __fmul_rn(__fmul_rn((float)(int)r[j + 1], sa), sb.y);
+        v[j + 2] = __fmul_rn(__fmul_rn((float)(int)r[j + 2], sa), sb.z);
+        v[j + 3] = __fmul_rn(__fmul_rn((float)(int)r[j + 3], sa), sb.w);
+    }
+    if (p.bias) {
+#pragma unroll
+        for (int j = 0; j < W; j += 4) {
+            const float4 bi = *reinterpret_cast<const float4*>(scales + W + j);
+            v[j] = __fadd_rn(v[j], bi.x);
+            v[j + 1] = __fadd_rn(v[j + 1], bi.y);
+            v[j + 2] = __fadd_rn(v[j + 2], bi.z);
+            v[j + 3] = __fadd_rn(v[j + 3], bi.w);
+        }
     }
     if (!ok) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = CUDART_NAN_F;
+        for (int j = 0; j < W; ++j) v[j] = CUDART_NAN_F;
     }
     __syncwarp();
     if (row0 >= p.m || col >= p.n) return;
-    if (tiles) {
+    if constexpr (TILES) {
 #pragma unroll
-        for (int i = 0; i < (k32 ? 8 : 4); ++i) {
+        for (int i = 0; i < 4; ++i) {
             uint4 w;
-            if constexpr (k32) w = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+            if constexpr (W == 16) w = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
             else w = make_uint4(pack2<T>(v[8 * i], v[8 * i + 1]), pack2<T>(v[8 * i + 2], v[8 * i + 3]), pack2<T>(v[8 * i + 4], v[8 * i + 5]), pack2<T>(v[8 * i + 6], v[8 * i + 7]));
-            *reinterpret_cast<uint4*>(buf + (i >> 2) * 2048 + lane * 64 + (((i & 3) ^ ((lane >> 1) & 3)) * 16)) = w;
+            *reinterpret_cast<uint4*>(stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) * 16)) = w;
         }
         smem_to_copies();
         __syncwarp();
-        if (lane == 0) {
-            tile_store(map_o, (int32_t)col, (int32_t)row0, smem_u32(buf));
-            if (k32 && col + 16 < p.n) tile_store(map_o, (int32_t)col + 16, (int32_t)row0, smem_u32(buf) + 2048);
-        }
+        if (lane == 0) tile_store(map_o, (int32_t)col, (int32_t)row0, smem_u32(stage));
     } else {
-        float* f = reinterpret_cast<float*>(stage);        // row r's column c at 32 r + (c ^ r)
+        float* f = reinterpret_cast<float*>(stage);        // row i's column c at 16 i + (c ^ (i & 15))
 #pragma unroll
-        for (int j = 0; j < 32; ++j) f[lane * 32 + (j ^ lane)] = v[j];
+        for (int j = 0; j < W; ++j) f[lane * 16 + (j ^ (lane & 15))] = v[j];
         __syncwarp();
+        const uint32_t c = lane & 15, r1 = lane >> 4;
         const uint32_t n = p.m - row0 < 32 ? (uint32_t)(p.m - row0) : 32u;
-        if (col + lane < p.n) {
-            T* out = static_cast<T*>(p.out) + row0 * p.ldo + col + lane;
+        if (col + c < p.n) {
+            T* out = static_cast<T*>(p.out) + (row0 + r1) * p.ldo + col + c;
+            const uint64_t step = 2 * p.ldo;
             if (n == 32) {
 #pragma unroll
-                for (uint32_t i = 0; i < 32; ++i) out[i * p.ldo] = from_f32<T>(f[i * 32 + (lane ^ i)]);
+                for (uint32_t i = 0; i < 32; i += 2, out += step) *out = from_f32<T>(f[(i + r1) * 16 + (c ^ ((i + r1) & 15))]);
             } else {
-                for (uint32_t i = 0; i < n; ++i) out[i * p.ldo] = from_f32<T>(f[i * 32 + (lane ^ i)]);
+                for (uint32_t i = r1; i < n; i += 2, out += step) *out = from_f32<T>(f[i * 16 + (c ^ (i & 15))]);
             }
         }
         __syncwarp();
     }
 }
 
-template <typename T, bool SPLIT>
+// 64 columns of a warp's 32 rows from tensor memory, W at a time; `done` runs when the last have been read.
+template <typename T, int W, bool TILES, class Done>
+__device__ __forceinline__ void finish_columns(const Product8& p, const CUtensorMap* map_o, uint32_t tmem, bool ok, float sa, const ColumnScale (&cs)[2],
+                                               uint64_t row0, uint64_t col, unsigned char* stage, uint32_t lane, Done&& done) {
+#pragma unroll
+    for (int i = 0; i < 64 / W; ++i) {
+        uint32_t r[W];
+        if (ok) {
+            if constexpr (W == 32) tmem_ld32(tmem + i * W, r);
+            else tmem_ld16(tmem + i * W, r);
+            tmem_wait_ld();
+        }
+        if (i == 64 / W - 1) done();
+        finish_chunk<T, W, TILES>(p, map_o, r, ok, sa, cs[i * W / 32], i & 1, row0, col + i * W, stage, lane);
+    }
+}
+
+template <typename T, bool SPLIT, bool TILES>
 __global__ void __launch_bounds__(kPairThreads, 1)
     product8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_o,
-                         const __grid_constant__ Product8 p, bool by_tiles, uint32_t split) {
+                         const __grid_constant__ Product8 p, uint32_t split) {
     extern __shared__ unsigned char dyn[];
     __shared__ uint32_t sh_tmem;
     __shared__ volatile uint32_t sh_failed;
     const uint32_t data = (smem_u32(dyn) + 1023u) & ~1023u;
     unsigned char* stages = dyn + (data - smem_u32(dyn));
-    const uint32_t bars = data + kPairStages * kPairStage + 8 * kStageStride;
+    const uint32_t bars = data + kPairStages * kPairStage + 16 * kStageStride;
     const auto full = [&](uint32_t s) { return bars + 16u * s; };
     const auto empty = [&](uint32_t s) { return bars + 16u * s + 8u; };
     const uint32_t acc_full = bars + 16u * kPairStages, acc_empty = acc_full + 16u, drain = acc_full + 32u;
@@ -299,14 +324,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
         for (uint32_t i = 0; i < 2; ++i) {
             mbar_init(acc_full + 8 * i, 1);
-            mbar_init(acc_empty + 8 * i, 16);              // eight warps of either CTA
+            mbar_init(acc_empty + 8 * i, 32);              // sixteen warps of either CTA
         }
         mbar_init(drain, 1);
         mbar_init_fence();
         map_prefetch(&map_a);
         map_prefetch(&map_b);
     }
-    if (warp == 9) tmem_alloc<2>(smem_u32(&sh_tmem), 2 * kPairTile);
+    if (warp == 17) tmem_alloc<2>(smem_u32(&sh_tmem), 2 * kPairTile);
     umma_fence_before();
     __syncthreads();
     cluster_sync_all();
@@ -315,7 +340,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     grid_wait();
     grid_go();
 
-    if (warp == 8 && lane == 0) {
+    if (warp == 16 && lane == 0) {
         // ---- feed: this CTA's rows of either operand, completion counted on the even CTA's barrier
         uint32_t it = 0;
         bool ok = true;
@@ -339,7 +364,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         // no CTA of the pair may leave before its copies have landed
         if (rank == 0)
             for (uint32_t j = it > kPairStages ? it - kPairStages : 0; j < it; ++j) (void)mbar_wait(full(j % kPairStages), (j / kPairStages) & 1u);
-    } else if (warp == 9 && lane == 0 && rank == 0) {
+    } else if (warp == 17 && lane == 0 && rank == 0) {
         // ---- issue
         constexpr uint32_t idesc = umma_idesc_s8(256, kPairTile);
         const uint16_t both = (uint16_t)(3u << even);
@@ -369,41 +394,32 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     }
     __syncwarp();
     unsigned char* stage = stages + kPairStages * kPairStage + warp * kStageStride;
-    const uint32_t quad = warp & 3, half = warp >> 2, row_in = rank * 128 + quad * 32;
+    const uint32_t quad = warp & 3, group = warp >> 2, row_in = rank * 128 + quad * 32;
+    constexpr int kWidth = TILES && sizeof(T) == 2 ? 32 : 16;
     if constexpr (!SPLIT) {
-        if (warp < 8) {
-            // ---- write out: rows 32 quad + lane of this CTA's 128, columns of the half
+        if (warp < 16) {
+            // ---- write out: rows 32 quad + lane of this CTA's 128, 64 columns
             uint32_t n_acc = 0;
             bool ok = true;
             for (uint32_t t = pair; t < tiles; t += pairs, ++n_acc) {
                 const uint32_t acc = n_acc & 1u, use = n_acc >> 1;
                 uint32_t tm, tn;
                 walk.at(t, tm, tn);
-                const uint64_t row0 = (uint64_t)tm * kPairTile + row_in, col0 = (uint64_t)tn * kPairTile + half * 128;
+                const uint64_t row0 = (uint64_t)tm * kPairTile + row_in, col0 = (uint64_t)tn * kPairTile + group * 64;
                 const float sa = row0 + lane < p.m ? __ldg(p.sa + row0 + lane) : 0.f;
-                ColumnScale cs[4];
-#pragma unroll
-                for (int ch = 0; ch < 4; ++ch) cs[ch] = column_scale(p, col0 + ch * 32 + lane);
+                const ColumnScale cs[2] = {column_scale(p, col0 + lane), column_scale(p, col0 + 32 + lane)};
                 if (ok && !mbar_wait(acc_full + 8 * acc, use & 1u)) ok = false;
                 ok = __all_sync(kFullMask, ok && !sh_failed);
                 umma_fence_after();
-#pragma unroll
-                for (uint32_t ch = 0; ch < 4; ++ch) {
-                    uint32_t r[32];
-                    if (ok) {
-                        tmem_ld32(tmem + ((quad * 32) << 16) + acc * kPairTile + half * 128 + ch * 32, r);
-                        tmem_wait_ld();
-                    }
-                    if (ch == 3) {                         // everything read: the next tile may overwrite it
-                        umma_fence_before();
-                        __syncwarp();
-                        if (lane == 0) cluster_arrive(cluster_map(acc_empty + 8 * acc, even));
-                    }
-                    finish_chunk<T>(p, &map_o, r, ok, sa, cs[ch], row0, col0 + ch * 32, by_tiles, stage, ch & 1u, lane);
-                }
+                finish_columns<T, kWidth, TILES>(p, &map_o, tmem + ((quad * 32) << 16) + acc * kPairTile + group * 64, ok, sa, cs, row0, col0, stage, lane, [&] {
+                    umma_fence_before();                   // everything read: the next tile may overwrite it
+                    __syncwarp();
+                    if (lane == 0) cluster_arrive(cluster_map(acc_empty + 8 * acc, even));
+                });
             }
+            if (TILES && lane == 0) tile_store_wait_all();
         }
-        if (warp < 8 && lane == 0) tile_store_wait_all();
+        __syncwarp();
         __syncthreads();
         cluster_meet_all();                                // the odd CTA's memory is read until the last instruction of the even one
     } else {
@@ -415,20 +431,19 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         bool ok = true;                                    // has landed and every instruction has read its operands
         uint32_t tm, tn;
         walk.at(pair, tm, tn);
-        const uint64_t row0 = (uint64_t)tm * kPairTile + row_in, col0 = (uint64_t)tn * kPairTile + mine;
-        const uint32_t own = cols / 64;                    // chunks of 32 columns a warp writes out: half, half + 2
+        const uint64_t row0 = (uint64_t)tm * kPairTile + row_in, col0 = (uint64_t)tn * kPairTile + mine + group * 32;
+        const bool own = group * 32 < cols;                // 32 columns a warp, of one's own
         float sa = 0.f;
-        ColumnScale cs[2] = {};
-        if (warp < 8) {
+        ColumnScale cs = {};
+        if (warp < 16) {
             if (row0 + lane < p.m) sa = __ldg(p.sa + row0 + lane);
-            cs[0] = column_scale(p, col0 + half * 32 + lane);
-            if (own > 1) cs[1] = column_scale(p, col0 + (half + 2) * 32 + lane);
+            if (own) cs = column_scale(p, col0 + lane);
             ok = mbar_wait(acc_full, 0);
             umma_fence_after();
             if (!ok) sh_failed = 1;
 #pragma unroll 1
-            for (uint32_t ch = 0; ch < 4; ++ch) {
-                const uint32_t c = half * 128 + ch * 32;
+            for (uint32_t ch = 0; ch < 2; ++ch) {
+                const uint32_t c = group * 64 + ch * 32;
                 if (c >= mine && c < mine + cols) continue;
                 uint32_t r[32];
                 tmem_ld32(tmem + ((quad * 32) << 16) + c, r);
@@ -440,43 +455,48 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             umma_fence_before();
         }
         cluster_sync_all();
-        if (warp < 8) {
+        if (warp < 16 && own) {
             umma_fence_after();
-            const auto fetch = [&](uint32_t c, uint32_t q, int4 (&v)[8]) {
+            const uint32_t c = mine + group * 32;
+            const auto fetch = [&](uint32_t q, int4 (&v)[8]) {
                 const uint32_t from = cluster_map(data + ((c / 4) * 128 + quad * 32 + lane) * 16, ((part + q) & (parts - 1)) * 2 + rank);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = cluster_ld4(from + j * 2048);
             };
             int4 v[8];
-            fetch(mine + half * 32, 1, v);
+            fetch(1, v);
             ok = cluster_all_zero(smem_u32((const void*)&sh_failed), 2 * parts);
-#pragma unroll
-            for (uint32_t i = 0; i < 2; ++i) {
-                if (i >= own) break;
-                const uint32_t c = mine + (half + 2 * i) * 32;
-                uint32_t r[32];
-                tmem_ld32(tmem + ((quad * 32) << 16) + c, r);
-                tmem_wait_ld();
+            uint32_t r[32];
+            tmem_ld32(tmem + ((quad * 32) << 16) + c, r);
+            tmem_wait_ld();
 #pragma unroll 1
-                for (uint32_t q = 1; q < parts; ++q) {
+            for (uint32_t q = 1; q < parts; ++q) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        r[4 * j] += (uint32_t)v[j].x;
-                        r[4 * j + 1] += (uint32_t)v[j].y;
-                        r[4 * j + 2] += (uint32_t)v[j].z;
-                        r[4 * j + 3] += (uint32_t)v[j].w;
-                    }
-                    if (q + 1 < parts) fetch(c, q + 1, v);
+                for (int j = 0; j < 8; ++j) {
+                    r[4 * j] += (uint32_t)v[j].x;
+                    r[4 * j + 1] += (uint32_t)v[j].y;
+                    r[4 * j + 2] += (uint32_t)v[j].z;
+                    r[4 * j + 3] += (uint32_t)v[j].w;
                 }
-                if (i + 1 < own) fetch(c + 64, 1, v);
-                finish_chunk<T>(p, &map_o, r, ok, sa, cs[i], row0, col0 + (c - mine), by_tiles, stage, i, lane);
+                if (q + 1 < parts) fetch(q + 1, v);
             }
+            if constexpr (kWidth == 32) {
+                finish_chunk<T, 32, TILES>(p, &map_o, r, ok, sa, cs, 0, row0, col0, stage, lane);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t half[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) half[j] = r[16 * i + j];
+                    finish_chunk<T, 16, TILES>(p, &map_o, half, ok, sa, cs, i, row0, col0 + 16 * i, stage, lane);
+                }
+            }
+            if (TILES && lane == 0) tile_store_wait_all();
         }
-        if (warp < 8 && lane == 0) tile_store_wait_all();
         __syncwarp();
         cluster_meet_all();                                // nobody leaves while its sums are being read
     }
-    if (warp == 9) tmem_free<2>(tmem, 2 * kPairTile);
+    if (warp == 17) tmem_free<2>(tmem, 2 * kPairTile);
 }
 
 // ---- few rows: 128 x NT tiles, the contraction split over a cluster ------------------------------------
@@ -691,20 +711,24 @@ template <typename K> cudaError_t allow_smem(K kernel, uint32_t bytes, PerDevice
     return e;
 }
 
-template <typename T, bool SPLIT> cudaError_t launch_pair(const Product8& p, uint32_t split, cudaStream_t st) {
+template <typename T, bool SPLIT, bool TILES> cudaError_t launch_pair_as(const Product8& p, uint32_t split, cudaStream_t st) {
     static PerDevice<bool> done;
-    const auto kernel = product8_pair_kernel<T, SPLIT>;
+    const auto kernel = product8_pair_kernel<T, SPLIT, TILES>;
     cudaError_t e = allow_smem(kernel, kPairSmem, done);
     if (e != cudaSuccess) return e;
-    CUtensorMap ma, mb;
+    CUtensorMap ma, mb, mo;
     if (!make_map(&ma, p.a, p.m, p.k, p.lda, 128) || !make_map(&mb, p.b, p.n, p.k, p.ldb, 128)) return cudaErrorNotSupported;
+    mo = ma;
+    if (TILES && !make_out_map(&mo, p, sizeof(T))) return cudaErrorNotSupported;
     const uint64_t tiles = (p.m + 255) / 256 * ((p.n + 255) / 256), pairs = (uint64_t)sm_count_now() / 2;
     if (tiles >= (1ull << 31)) return cudaErrorInvalidValue;
-    const bool by_tiles = (reinterpret_cast<uintptr_t>(p.out) | p.ldo * sizeof(T)) % 16 == 0;
-    CUtensorMap mo = ma;
-    if (by_tiles && !make_out_map(&mo, p, sizeof(T))) return cudaErrorNotSupported;
     return launch_layer(kernel, (unsigned)(2 * (SPLIT ? tiles * split : tiles < pairs ? tiles : pairs)), kPairThreads, kPairSmem, 2 * split, st,
-                          ma, mb, mo, p, by_tiles, split);
+                        ma, mb, mo, p, split);
+}
+template <typename T> cudaError_t launch_pair(const Product8& p, uint32_t split, cudaStream_t st) {
+    const bool tiles = (reinterpret_cast<uintptr_t>(p.out) | p.ldo * sizeof(T)) % 16 == 0;
+    if (split > 1) return tiles ? launch_pair_as<T, true, true>(p, split, st) : launch_pair_as<T, true, false>(p, split, st);
+    return tiles ? launch_pair_as<T, false, true>(p, 1, st) : launch_pair_as<T, false, false>(p, 1, st);
 }
 
 // Clusters of `split` pairs that run at once on this device.
@@ -714,7 +738,7 @@ template <typename T> uint64_t resident_clusters(uint32_t split) {
     PerDevice<int>& table = known[split == 2 ? 0 : 1];
     if (slot >= 0 && table.v[slot] > 0) return (uint64_t)table.v[slot] - 1;
     static PerDevice<bool> done;
-    const auto kernel = product8_pair_kernel<T, true>;
+    const auto kernel = product8_pair_kernel<T, true, true>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * split);
     cfg.blockDim = dim3(kPairThreads);
@@ -793,7 +817,7 @@ cudaError_t launch_product8(const Product8& p, cudaStream_t st) {
         const uint64_t tiles = (p.m + 255) / 256 * ((p.n + 255) / 256);
         uint32_t split = 1;
         while (split < 4 && kblocks >= split * 8 && tiles <= resident_clusters<T>(split * 2)) split *= 2;
-        return split > 1 ? launch_pair<T, true>(p, split, st) : launch_pair<T, false>(p, 1, st);
+        return launch_pair<T>(p, split, st);
     });
 }
 

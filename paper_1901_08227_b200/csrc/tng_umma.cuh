@@ -127,8 +127,9 @@ __device__ __forceinline__ uint32_t cluster_map(uint32_t smem, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem), "r"(rank));
     return r;
 }
+// Relaxed: it orders nothing but what tensor-memory fences order (a release here waits 1500 cycles for stores).
 __device__ __forceinline__ void cluster_arrive(uint32_t remote_bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote_bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote_bar) : "memory");
 }
 __device__ __forceinline__ int cluster_ld(uint32_t remote) {
     int v;
