@@ -100,9 +100,8 @@ cudaError_t launch_decode(const CodecGeom& g, const uint32_t* codes, const float
                           const float* ref2, float* out_a, float* out_b, FuseBlock* fb, int sm_count, cudaStream_t st, int* launches);
 
 // ---- training-layer operators (tng_quant8.cu, tng_product8.cu) -----------------------
-// clear (n_clear words, may be nullptr / 0): set to zero on the way.
 cudaError_t launch_quant8_rows(const void* x, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx, const tng_draw* draw,
-                               int8_t* q, uint64_t ldq, float* scale, uint32_t* clear, uint64_t n_clear, cudaStream_t st);
+                               int8_t* q, uint64_t ldq, float* scale, cudaStream_t st);
 struct Quant8Cols {
     const void* x;
     uint64_t rows, cols, ldx;
@@ -111,6 +110,10 @@ struct Quant8Cols {
     uint64_t ldq;
     float *scale, *colsum;          // colsum may be nullptr
     uint32_t* scratch;              // quant8_cols_scratch words, the first `cols` of them zero
+    uint32_t* row_tops;             // row codes too: `rows` words, zero; else nullptr
+    int8_t* row_q;
+    uint64_t ld_row;
+    float* row_scale;
 };
 uint64_t quant8_cols_scratch(uint64_t rows, uint64_t cols, bool sums);
 cudaError_t launch_quant8_cols(const Quant8Cols* jobs, int n, tng_dtype type, cudaStream_t st);   // n = 1 or 2

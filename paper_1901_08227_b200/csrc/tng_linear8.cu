@@ -45,7 +45,7 @@ tng_status tng_linear8(const void* x_dev, tng_dtype type, uint64_t tokens, uint6
     int8_t* q = c.take<int8_t>(codes_bytes(tokens, k));
     float* s = c.take<float>(scales_bytes(tokens));
     const uint64_t ldq = tng_code_stride(k);
-    if (launch_quant8_rows(x_dev, type, tokens, k, ldx, nullptr, q, ldq, s, nullptr, 0, st) != cudaSuccess) return TNG_ERR_CUDA;
+    if (launch_quant8_rows(x_dev, type, tokens, k, ldx, nullptr, q, ldq, s, st) != cudaSuccess) return TNG_ERR_CUDA;
     const Product8 p{q, w_dev, ldq, ldw, s, sw_dev, bias_dev, tokens, n, k, y_dev, type, ldy};
     return launch_product8(p, st) == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
 }
@@ -53,7 +53,7 @@ tng_status tng_linear8(const void* x_dev, tng_dtype type, uint64_t tokens, uint6
 size_t tng_linear8_grad_scratch_bytes(uint64_t tokens, uint64_t k, uint64_t n) {
     if (tokens == 0) return 256;
     return (size_t)(codes_bytes(tokens, n) + scales_bytes(tokens) + codes_bytes(n, tokens) + scales_bytes(n) + codes_bytes(k, tokens) +
-                    scales_bytes(k) + up256(4 * (k + quant8_cols_scratch(tokens, n, true))));
+                    scales_bytes(k) + up256(4 * (k + tokens + quant8_cols_scratch(tokens, n, true))));
 }
 
 tng_status tng_linear8_grad(const void* dy_dev, uint64_t lddy, const void* x_dev, uint64_t ldx, tng_dtype type, uint64_t tokens,
@@ -73,8 +73,8 @@ tng_status tng_linear8_grad(const void* dy_dev, uint64_t lddy, const void* x_dev
     if (dw_dev && !matrix_ok(x_dev, type, k, ldx)) return TNG_ERR_INVALID_ARG;
     if (dx_dev && (!matrix_ok(dx_dev, type, k, lddx) || !codes_ok(wt_dev, n, ldwt) || !swt_dev || !aligned(swt_dev, 4)))
         return TNG_ERR_INVALID_ARG;
-    // The column maxima of x and of dy lie side by side, so that the row codes' launch can clear them all; then both
-    // matrices' columns, then the products: five launches.
+    // With a sum over the tokens to form, dy's row and column codes come from the same passes, and x's columns share their
+    // launches: clear the maxima (side by side), maxima, codes, two products.  dx alone needs the rows only.
     Carver c{static_cast<unsigned char*>(scratch_dev)};
     const uint64_t ldr = tng_code_stride(n), ldc = tng_code_stride(tokens);
     int8_t* qr = c.take<int8_t>(codes_bytes(tokens, n));
@@ -84,18 +84,15 @@ tng_status tng_linear8_grad(const void* dy_dev, uint64_t lddy, const void* x_dev
     int8_t* qx = c.take<int8_t>(codes_bytes(k, tokens));
     float* sx = c.take<float>(scales_bytes(k));
     uint32_t* tops_x = c.take<uint32_t>(0);
-    uint32_t* work_y = tops_x + k;
-    const bool columns = dw_dev || db_dev;
-    if (dx_dev) {
-        if (launch_quant8_rows(dy_dev, type, tokens, n, lddy, draw, qr, ldr, sr, columns ? tops_x : nullptr, columns ? k + n : 0, st) != cudaSuccess)
-            return TNG_ERR_CUDA;
-    } else if (columns && cudaMemsetAsync(tops_x, 0, (k + n) * 4, st) != cudaSuccess) {
-        return TNG_ERR_CUDA;
-    }
-    if (columns) {
-        const Quant8Cols jobs[2] = {{dy_dev, tokens, n, lddy, draw, qy, ldc, sy, db_dev, work_y},
-                                    {x_dev, tokens, k, ldx, nullptr, qx, ldc, sx, nullptr, tops_x}};
+    uint32_t* tops_rows = tops_x + k;
+    uint32_t* work_y = tops_rows + tokens;
+    if (dw_dev || db_dev) {
+        if (cudaMemsetAsync(tops_x, 0, (k + tokens + n) * 4, st) != cudaSuccess) return TNG_ERR_CUDA;
+        const Quant8Cols jobs[2] = {{dy_dev, tokens, n, lddy, draw, qy, ldc, sy, db_dev, work_y, dx_dev ? tops_rows : nullptr, dx_dev ? qr : nullptr, ldr, sr},
+                                    {x_dev, tokens, k, ldx, nullptr, qx, ldc, sx, nullptr, tops_x, nullptr, nullptr, 0, nullptr}};
         if (launch_quant8_cols(jobs, dw_dev ? 2 : 1, type, st) != cudaSuccess) return TNG_ERR_CUDA;
+    } else if (dx_dev && launch_quant8_rows(dy_dev, type, tokens, n, lddy, draw, qr, ldr, sr, st) != cudaSuccess) {
+        return TNG_ERR_CUDA;
     }
     if (dx_dev) {
         const Product8 p{qr, wt_dev, ldr, ldwt, sr, swt_dev, nullptr, tokens, k, n, dx_dev, type, lddx};

@@ -13,14 +13,10 @@ namespace {
 template <typename T> constexpr int kHold = 16 / (int)sizeof(T);       // groups of eight elements
 template <typename T, bool VEC, bool DRAW>
 __global__ void quant8_rows_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, int8_t* __restrict__ q,
-                                   uint64_t ldq, float* __restrict__ scale, uint32_t* __restrict__ clear, uint64_t n_clear,
-                                   const __grid_constant__ DrawArgs draw) {
+                                   uint64_t ldq, float* __restrict__ scale, const __grid_constant__ DrawArgs draw) {
     __shared__ uint32_t part[32];
     grid_wait();
     grid_go();
-    // what the launch after this one wants cleared (a gradient's column maxima)
-    const uint32_t threads = blockDim.x * blockDim.y, me = threadIdx.y * blockDim.x + threadIdx.x;
-    for (uint64_t i = (uint64_t)blockIdx.x * threads + me; i < n_clear; i += (uint64_t)gridDim.x * threads) clear[i] = 0u;
     const uint64_t row = (uint64_t)blockIdx.x * blockDim.y + threadIdx.y;
     if (row >= rows) return;                       // whole warps only: with blockDim.y > 1 there is no block barrier
     const T* src = x + row * ldx;
@@ -64,7 +60,8 @@ __global__ void quant8_rows_kernel(const T* __restrict__ x, uint64_t rows, uint6
 
 // ---- columns -----------------------------------------------------------------------------------------
 // Two passes, the first for the largest |x| and the sum of every column, the second for the codes; up to two matrices of
-// one type a launch (a gradient's dy and x).  (Panels of columns small enough for the L2 cache to hold between the passes
+// one type a launch (a gradient's dy and x), of which the first may have its row codes made on the way (dy: one read
+// less, and the random words of an element serve both its codes; 2048 x 4096 bf16 drawn 36 -> 24 us).  (Panels of columns small enough for the L2 cache to hold between the passes
 // saved the second read but lost as much to the ends of twice as many launches: 16384 x 4096 bf16, 83 us in panels of
 // 64 MB, 76 us whole.)
 template <typename T> struct ColumnJob {
@@ -76,6 +73,10 @@ template <typename T> struct ColumnJob {
     int8_t* q;
     uint64_t ldq;
     float *scale, *colsum;
+    uint32_t* row_tops;            // with row codes too (else nullptr): largest |x| of the rows, cleared before
+    int8_t* row_q;
+    uint64_t ld_row;
+    float* row_scale;
 };
 template <typename T> struct ColumnJobs {
     ColumnJob<T> job[2];
@@ -105,29 +106,31 @@ __global__ void __launch_bounds__(256, 4) column_stats_kernel(const __grid_const
     const uint64_t r1 = r0 + job.rows_per_chunk < rows ? r0 + job.rows_per_chunk : rows;
     uint32_t top[kWords] = {};
     float sum[8] = {};
-    if (c < cols) {
-        const auto take = [&](const Raw8<T>& r) {
-            const uint32_t* w = reinterpret_cast<const uint32_t*>(&r);
+    const auto take = [&](const Raw8<T>& v, uint64_t r) {   // (columns past the end read as zero)
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
 #pragma unroll
-            for (int j = 0; j < kWords; ++j) top[j] = top_word<T>(w[j], top[j]);
-            if (want_sums) {
-                float v[8];
-                widen8(r, v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] += v[j];
-            }
-        };
-        uint64_t r = r0 + lane;
-        constexpr int kAhead = 8 / (int)sizeof(T);          // 64 bytes a thread in flight
-        for (; r + (kAhead - 1) * kStatLanes < r1; r += kAhead * kStatLanes) {
-            Raw8<T> v[kAhead];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) v[i] = fetch_raw8<T, VEC>(x + (r + i * kStatLanes) * ldx, c, cols);
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) take(v[i]);
+        for (int j = 0; j < kWords; ++j) top[j] = top_word<T>(w[j], top[j]);
+        if (job.row_tops) {                                // a warp has 256 columns of one row
+            const uint32_t m = __reduce_max_sync(kFullMask, top_of_halves<T>(top_raw8<T>(v, 0u)));
+            if (cg == 0) atomicMax(job.row_tops + r, top_bits<T>(m));
         }
-        for (; r < r1; r += kStatLanes) take(fetch_raw8<T, VEC>(x + r * ldx, c, cols));
+        if (want_sums) {
+            float f[8];
+            widen8(v, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += f[j];
+        }
+    };
+    uint64_t r = r0 + lane;
+    constexpr int kAhead = 8 / (int)sizeof(T);              // 64 bytes a thread in flight
+    for (; r + (kAhead - 1) * kStatLanes < r1; r += kAhead * kStatLanes) {
+        Raw8<T> v[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) v[i] = fetch_raw8<T, VEC>(x + (r + i * kStatLanes) * ldx, c, cols);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) take(v[i], r + i * kStatLanes);
     }
+    for (; r < r1; r += kStatLanes) take(fetch_raw8<T, VEC>(x + r * ldx, c, cols), r);
 #pragma unroll
     for (int j = 0; j < kWords; ++j) sh_top[lane][cg * kWords + j] = top[j];
     if (want_sums) {
@@ -156,10 +159,10 @@ __global__ void __launch_bounds__(256, 4) column_stats_kernel(const __grid_const
 // cross the CTA through shared memory so that a warp writes 128 contiguous bytes of one column.  The next 128
 // rows' loads are issued before that.
 constexpr int kColTile = 64, kRowTile = 128, kRowsPerCta = 256;
-template <typename T, bool VEC, bool DRAW>
-__global__ void __launch_bounds__(256, DRAW ? 3 : 4) quant8_cols_kernel(const __grid_constant__ ColumnJobs<T> jobs, const __grid_constant__ DrawArgs draw) {
+template <typename T, bool VEC, bool DRAW, bool ROWS>
+__global__ void __launch_bounds__(256, DRAW ? (ROWS ? 2 : 3) : (ROWS ? 3 : 4)) quant8_cols_kernel(const __grid_constant__ ColumnJobs<T> jobs, const __grid_constant__ DrawArgs draw) {
     __shared__ uint32_t words[2][kColTile][kRowTile / 4 + 1];
-    __shared__ float sh_inv[kColTile], sh_sum[4][kColTile];
+    __shared__ float sh_inv[kColTile], sh_sum[4][kColTile], sh_row_inv[ROWS ? kRowsPerCta : 1];
     grid_wait();
     grid_go();
     const bool second = blockIdx.x >= jobs.first2;
@@ -198,6 +201,16 @@ __global__ void __launch_bounds__(256, DRAW ? 3 : 4) quant8_cols_kernel(const __
         sh_inv[threadIdx.x] = s.inv;
         if (slab == 0 && col < cols) job.scale[col] = s.scale;
     }
+    const bool rows_too = ROWS && job.row_q;
+    if (rows_too) {
+        static_assert(kRowsPerCta == 256, "a thread a row");
+        const uint64_t r = first + threadIdx.x;
+        const uint32_t top = r < last ? __ldg(job.row_tops + r) : 0u;
+        const LineScale s = line_scale(top);
+        bad = bad || top >= kInfBits;
+        sh_row_inv[threadIdx.x] = s.inv;
+        if (c0 == 0 && r < last) job.row_scale[r] = s.scale;
+    }
     if (slab == 0 && job.colsum) {                         // the chunks' sums: a quarter to a thread, the quarters in order
         const uint32_t lc = threadIdx.x & 63, quarter = threadIdx.x >> 6;
         float a = 0.f;
@@ -235,6 +248,18 @@ __global__ void __launch_bounds__(256, DRAW ? 3 : 4) quant8_cols_kernel(const __
                 // (rows past the end read as zero, a zero column has inv = 0: code zero, with a draw too, since floor(0 + u) = 0)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) b[i][j] = code_bits<DRAW>(f[j], inv[j], w[j]);
+                if (rows_too) {
+                    const uint32_t at = rg * 4 + 2 * h + i;            // of these 128 rows
+                    const uint64_t r = r0 + at;
+                    const float inv_r = sh_row_inv[(uint32_t)(r0 - first) + at];
+                    uint32_t e[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) e[j] = code_bits<DRAW>(f[j], inv_r, w[j]);
+                    uint2 out = make_uint2(pack_bytes(e[0], e[1], e[2], e[3]), pack_bytes(e[4], e[5], e[6], e[7]));
+                    if (any_bad && inv_r == 0.f) out = make_uint2(0u, 0u);
+                    // (zeros up to the next multiple of 16, like the columns past the end that they are)
+                    if (r < last && (wide || c < (cols + 15) / 16 * 16)) *reinterpret_cast<uint2*>(job.row_q + r * job.ld_row + c) = out;
+                }
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -274,7 +299,7 @@ uint32_t column_chunks(uint64_t rows, uint64_t cols) {
 
 template <typename T, bool VEC, bool DRAW>
 cudaError_t rows_launch(const void* x, uint64_t rows, uint64_t cols, uint64_t ldx, const DrawArgs& d, int8_t* q, uint64_t ldq,
-                        float* scale, uint32_t* clear, uint64_t n_clear, cudaStream_t st) {
+                        float* scale, cudaStream_t st) {
     // a warp a row while it can hold one, eight rows a CTA; above, as many threads as hold the row
     const uint64_t groups = (cols + 7) / 8;
     dim3 block(32, 8);
@@ -283,17 +308,18 @@ cudaError_t rows_launch(const void* x, uint64_t rows, uint64_t cols, uint64_t ld
         block = dim3((unsigned)(t > 1024 ? 1024 : t), 1);
     }
     const unsigned grid = (unsigned)((rows + block.y - 1) / block.y);
-    return launch_layer(quant8_rows_kernel<T, VEC, DRAW>, grid, block, 0, 1, st, static_cast<const T*>(x), rows, cols, ldx, q, ldq, scale, clear, n_clear, d);
+    return launch_layer(quant8_rows_kernel<T, VEC, DRAW>, grid, block, 0, 1, st, static_cast<const T*>(x), rows, cols, ldx, q, ldq, scale, d);
 }
 
-template <typename T, bool VEC> cudaError_t cols_launch(const ColumnJobs<T>& jobs, const DrawArgs* draw, uint64_t ctas1, uint64_t ctas2, cudaStream_t st) {
+template <typename T, bool VEC, bool ROWS>
+cudaError_t cols_launch(const ColumnJobs<T>& jobs, const DrawArgs* draw, uint64_t ctas1, uint64_t ctas2, cudaStream_t st) {
     ColumnJobs<T> j = jobs;
     j.first2 = (uint32_t)((uint64_t)j.job[0].blocks * j.job[0].chunks);
     cudaError_t e = launch_layer(column_stats_kernel<T, VEC>, j.first2 + j.job[1].blocks * j.job[1].chunks, 256, 0, 1, st, j);
     if (e != cudaSuccess) return e;
     j.first2 = (uint32_t)ctas1;
-    return draw ? launch_layer(quant8_cols_kernel<T, VEC, true>, (unsigned)(ctas1 + ctas2), 256, 0, 1, st, j, *draw)
-                : launch_layer(quant8_cols_kernel<T, VEC, false>, (unsigned)(ctas1 + ctas2), 256, 0, 1, st, j, DrawArgs{});
+    return draw ? launch_layer(quant8_cols_kernel<T, VEC, true, ROWS>, (unsigned)(ctas1 + ctas2), 256, 0, 1, st, j, *draw)
+                : launch_layer(quant8_cols_kernel<T, VEC, false, ROWS>, (unsigned)(ctas1 + ctas2), 256, 0, 1, st, j, DrawArgs{});
 }
 
 template <typename T> bool rows_aligned(const void* x, uint64_t rows, uint64_t ldx) {
@@ -303,19 +329,19 @@ template <typename T> bool rows_aligned(const void* x, uint64_t rows, uint64_t l
 }  // namespace
 
 cudaError_t launch_quant8_rows(const void* x, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx, const tng_draw* draw,
-                               int8_t* q, uint64_t ldq, float* scale, uint32_t* clear, uint64_t n_clear, cudaStream_t st) {
+                               int8_t* q, uint64_t ldq, float* scale, cudaStream_t st) {
     return with_type(type, [&](auto t) {
         using T = decltype(t);
         const DrawArgs d = draw ? make_draw(*draw, kTagRounding) : DrawArgs{};
         const auto launch = rows_aligned<T>(x, rows, ldx) ? (draw ? rows_launch<T, true, true> : rows_launch<T, true, false>)
                                                           : (draw ? rows_launch<T, false, true> : rows_launch<T, false, false>);
-        return launch(x, rows, cols, ldx, d, q, ldq, scale, clear, n_clear, st);
+        return launch(x, rows, cols, ldx, d, q, ldq, scale, st);
     });
 }
 
 uint64_t quant8_cols_scratch(uint64_t rows, uint64_t cols, bool sums) { return (1 + (sums ? (uint64_t)column_chunks(rows, cols) : 0)) * cols; }
 
-// Jobs of one type whose maxima (the first words of their scratch) are clear.  Two of them share the launches where
+// Jobs of one type whose maxima (the first words of their scratch, row_tops) are clear; only the first may have row codes.  Two of them share the launches where
 // they are alike in alignment and neither is drawn.
 cudaError_t launch_quant8_cols(const Quant8Cols* jobs, int n, tng_dtype type, cudaStream_t st) {
     return with_type(type, [&](auto t) {
@@ -335,13 +361,16 @@ cudaError_t launch_quant8_cols(const Quant8Cols* jobs, int n, tng_dtype type, cu
             o.tops = in.scratch;
             o.sums = in.colsum ? reinterpret_cast<float*>(in.scratch + in.cols) : nullptr;
             o.q = in.q; o.ldq = in.ldq; o.scale = in.scale; o.colsum = in.colsum;
+            o.row_tops = in.row_tops; o.row_q = in.row_q; o.ld_row = in.ld_row; o.row_scale = in.row_scale;
             ctas[i] = o.tiles * ((in.rows + kRowsPerCta - 1) / kRowsPerCta);
             vec[i] = rows_aligned<T>(in.x, in.rows, in.ldx);
         }
         if (ctas[0] + ctas[1] >= (1ull << 31)) return cudaErrorInvalidValue;
         const auto one = [&](const ColumnJobs<T>& k, const tng_draw* draw, bool v, uint64_t c1, uint64_t c2) {
             const DrawArgs d = draw ? make_draw(*draw, kTagRounding) : DrawArgs{};
-            return v ? cols_launch<T, true>(k, draw ? &d : nullptr, c1, c2, st) : cols_launch<T, false>(k, draw ? &d : nullptr, c1, c2, st);
+            const auto launch = k.job[0].row_q ? (v ? cols_launch<T, true, true> : cols_launch<T, false, true>)
+                                               : (v ? cols_launch<T, true, false> : cols_launch<T, false, false>);
+            return launch(k, draw ? &d : nullptr, c1, c2, st);
         };
         if (n == 1) return one(j, jobs[0].draw, vec[0], ctas[0], 0);
         if (vec[0] == vec[1] && !jobs[0].draw && !jobs[1].draw) return one(j, nullptr, vec[0], ctas[0], ctas[1]);
@@ -368,7 +397,7 @@ tng_status tng_quant8_rows(const void* x_dev, tng_dtype type, uint64_t rows, uin
     if (!type_ok(type) || cols < 1 || !dims_ok(rows, cols) || (draw && !draw_ok(draw, rows))) return TNG_ERR_INVALID_ARG;
     if (rows == 0) return TNG_OK;
     if (!matrix_ok(x_dev, type, cols, ldx) || !codes_ok(q_dev, cols, ldq) || !scale_dev || !aligned(scale_dev, 4)) return TNG_ERR_INVALID_ARG;
-    return launch_quant8_rows(x_dev, type, rows, cols, ldx, draw, q_dev, ldq, scale_dev, nullptr, 0, static_cast<cudaStream_t>(stream)) == cudaSuccess
+    return launch_quant8_rows(x_dev, type, rows, cols, ldx, draw, q_dev, ldq, scale_dev, static_cast<cudaStream_t>(stream)) == cudaSuccess
                ? TNG_OK : TNG_ERR_CUDA;
 }
 
@@ -390,7 +419,7 @@ tng_status tng_quant8_cols(const void* x_dev, tng_dtype type, uint64_t rows, uin
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint32_t* scratch = static_cast<uint32_t*>(scratch_dev);
     if (cudaMemsetAsync(scratch, 0, cols * 4, st) != cudaSuccess) return TNG_ERR_CUDA;
-    const Quant8Cols job{x_dev, rows, cols, ldx, draw, q_dev, ldq, scale_dev, colsum_dev, scratch};
+    const Quant8Cols job{x_dev, rows, cols, ldx, draw, q_dev, ldq, scale_dev, colsum_dev, scratch, nullptr, nullptr, 0, nullptr};
     return launch_quant8_cols(&job, 1, type, st) == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
 }
 
