@@ -373,8 +373,8 @@ tng_status tng_product8(const int8_t* a_dev, uint64_t lda, const float* sa_dev, 
                         tng_dtype type, uint64_t ldo, void* stream);
 /* y = x W^T + bias for T tokens: codes of x by row (nearest), then the product with the codes of
  * W (n x k, a scale per output channel: tng_quant8_rows of W).  y has x's type.  scratch_dev:
- * tng_linear8_scratch_bytes, 256-byte aligned (codes and scales of x); 0 bytes for up to 16 tokens that
- * the product codes itself, scratch_dev may then be NULL. */
+ * tng_linear8_scratch_bytes, 256-byte aligned (codes and scales of x); 0 bytes for a few short
+ * tokens, which the product codes itself: scratch_dev may then be NULL. */
 size_t tng_linear8_scratch_bytes(uint64_t tokens, uint64_t k);
 tng_status tng_linear8(const void* x_dev, tng_dtype type, uint64_t tokens, uint64_t k, uint64_t ldx, const int8_t* w_dev,
                        uint64_t ldw, const float* sw_dev, uint64_t n, const float* bias_dev, void* y_dev, uint64_t ldy,

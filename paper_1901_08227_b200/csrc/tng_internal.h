@@ -127,9 +127,9 @@ struct Product8 {
     uint64_t ldo;
 };
 cudaError_t launch_product8(const Product8& p, cudaStream_t st);
-// Whether a product with this many rows of a takes the kernel that streams b past them, and that kernel with rows
-// of p.type (p.a and p.sa unused) which it codes itself.
-bool product8_streams(uint64_t tokens, uint64_t k);
+// Whether a linear layer with this many tokens is one launch that streams the weights past tokens it codes itself, and
+// that launch: x has rows of p.type, p.a and p.sa are unused.
+bool product8_codes_tokens(uint64_t tokens, uint64_t k);
 cudaError_t launch_linear8_stream(const void* x, uint64_t ldx, const Product8& p, cudaStream_t st);
 
 }  // namespace tng

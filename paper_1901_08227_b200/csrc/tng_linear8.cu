@@ -24,7 +24,7 @@ struct Carver {
 extern "C" {
 
 size_t tng_linear8_scratch_bytes(uint64_t tokens, uint64_t k) {
-    return product8_streams(tokens, k) ? 0 : (size_t)(codes_bytes(tokens, k) + scales_bytes(tokens));
+    return product8_codes_tokens(tokens, k) ? 0 : (size_t)(codes_bytes(tokens, k) + scales_bytes(tokens));
 }
 
 tng_status tng_linear8(const void* x_dev, tng_dtype type, uint64_t tokens, uint64_t k, uint64_t ldx, const int8_t* w_dev,
@@ -36,7 +36,7 @@ tng_status tng_linear8(const void* x_dev, tng_dtype type, uint64_t tokens, uint6
         !matrix_ok(y_dev, type, n, ldy))
         return TNG_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (product8_streams(tokens, k)) {
+    if (product8_codes_tokens(tokens, k)) {
         const Product8 p{nullptr, w_dev, 0, ldw, nullptr, sw_dev, bias_dev, tokens, n, k, y_dev, type, ldy};
         return launch_linear8_stream(x_dev, ldx, p, st) == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
     }

@@ -17,108 +17,128 @@ __device__ __forceinline__ float scaled(int acc, float sa, float sb, bool has_bi
     return has_bias ? __fadd_rn(v, bias) : v;
 }
 
-// ---- at most 16 tokens: the weights are streamed past them ----------------------------------------------
-// Bound by reading b once.  The tokens' codes stay in shared memory; a CTA goes over tiles of eight rows of b, KS
-// warps sharing a tile along the contraction, 512 codes a warp and step: eight 16-byte loads a lane, the next
-// step's issued before this one's are used.  A warp-wide m16n8k32 instruction takes the tokens as its 16 rows and
-// the weights as its 8 columns straight from the loaded words: the contraction may run in any order as long as
-// both sides agree, so a lane's 16 consecutive codes serve as its words of two instructions.  (The tensor-memory
-// kernel below needs its operands in shared memory and takes 2.5x the time here: set-up and barriers, not traffic.)
+// ---- at most 8 tokens: the weights are streamed past them ------------------------------------------------
+// Bound by reading b once.  The tokens' codes stay in shared memory; a CTA goes over tiles of sixteen rows of b, KS warps
+// sharing a tile along the contraction, 256 codes a warp and step: a lane has every fourth 16 bytes of two rows, eight
+// loads of them, the next step's issued before this one's are used.  A warp-wide m16n8k32 instruction takes the weights as
+// its 16 rows straight from the loaded words and the tokens as its 8 columns: the contraction may run in any order as
+// long as both sides agree, so a lane's 16 consecutive codes serve as its words of two instructions.  These instructions are
+// slow here (270 cycles where one waits for another, hence four chains; byte products on the integer pipe took 7 cycles
+// each, three times as long at 8 tokens), but they keep up with memory; the tensor-memory kernel below needs its operands in
+// shared memory, and its set-up and barriers cost 5 us.
 // X = int8_t: codes with scales; a floating type: the CTA codes the tokens itself, while its first weights travel.
-constexpr int kStreamThreads = 256, kStreamTokens = 16;
+constexpr int kStreamThreads = 256, kStreamTokens = 8, kStreamHold = 8;
 constexpr uint32_t kStreamSmem = 96 * 1024;
-__host__ __device__ inline uint32_t stream_pitch(uint64_t k) { return (uint32_t)((k + 511) / 512 * 512 + 64); }   // 64 mod 128: no bank conflicts
+__host__ __device__ inline uint32_t stream_pitch(uint64_t k) { return (uint32_t)((k + 255) / 256 * 256 + 64); }   // 64 mod 128: no bank conflicts
+// Threads a token while its line is coded: all 256 over the tokens' next power of two.
+__host__ __device__ inline uint32_t stream_share(uint64_t tokens) { return kStreamThreads / (tokens > 4 ? 8 : tokens > 2 ? 4 : tokens > 1 ? 2 : 1); }
 
 __device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// The tokens' codes and scales into shared memory, zero up to a multiple of 512 codes.  TPT threads a token.
+// The tokens' codes and scales into shared memory, zero up to the pitch.
 template <typename X>
 __device__ __forceinline__ void stream_tokens(const X* x, uint64_t ldx, const float* sa, uint32_t tokens, uint32_t k, int8_t* codes, uint32_t pitch,
                                               float* scales, uint32_t* part) {
-    const uint32_t groups = (k + 7) / 8, all = (k + 511) / 512 * 64;
-    uint32_t tpt = kStreamThreads;                          // threads a token: a power of two, a warp at least
-    while (tpt > 32 && (uint64_t)tpt * tokens > kStreamThreads) tpt >>= 1;
-    const uint32_t at_once = kStreamThreads / tpt, me = threadIdx.x / tpt, lane = threadIdx.x & (tpt - 1);
-    for (uint32_t t0 = 0; t0 < tokens; t0 += at_once) {
-        const uint32_t t = t0 + me;
-        const bool live = t < tokens;
-        const X* row = x + (uint64_t)(live ? t : 0) * ldx;
-        uint2* dst = reinterpret_cast<uint2*>(codes + (live ? t : 0) * pitch);
-        if constexpr (sizeof(X) == 1) {
-            if (live) {
-#pragma unroll 8
-                for (uint32_t g = lane; g < all / 2; g += tpt) {
-                    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                    if (g * 16 < k) w = __ldg(reinterpret_cast<const uint4*>(row) + g);
-                    if (g * 16 + 16 > k) {                  // what follows a line does not count
-                        const uint32_t n = g * 16 < k ? k - g * 16 : 0;
-                        const auto cut = [n](uint32_t v, uint32_t first) { return n >= first + 4 ? v : n <= first ? 0u : v & ((1u << (8 * (n - first))) - 1u); };
-                        w = make_uint4(cut(w.x, 0), cut(w.y, 4), cut(w.z, 8), cut(w.w, 12));
-                    }
-                    reinterpret_cast<uint4*>(dst)[g] = w;
-                }
-                if (lane == 0) scales[t] = __ldg(sa + t);
+    const uint32_t groups = (k + 7) / 8, all = pitch / 8;
+    if constexpr (sizeof(X) == 1) {
+        const uint32_t per = pitch / 16, total = tokens * per;
+        for (uint32_t i0 = threadIdx.x; i0 < total; i0 += 8 * kStreamThreads) {
+            uint4 w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t i = i0 + j * kStreamThreads, t = i / per, g = i - t * per;
+                w[j] = i < total && g * 16 < k ? __ldg(reinterpret_cast<const uint4*>(x + (uint64_t)t * ldx) + g) : make_uint4(0u, 0u, 0u, 0u);
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t i = i0 + j * kStreamThreads, t = i / per, g = i - t * per;
+                if (i >= total) break;
+                if (g * 16 + 16 > k) {                      // what follows a line does not count
+                    const uint32_t n = g * 16 < k ? k - g * 16 : 0;
+                    const auto cut = [n](uint32_t v, uint32_t first) { return n >= first + 4 ? v : n <= first ? 0u : v & ((1u << (8 * (n - first))) - 1u); };
+                    w[j] = make_uint4(cut(w[j].x, 0), cut(w[j].y, 4), cut(w[j].z, 8), cut(w[j].w, 12));
+                }
+                reinterpret_cast<uint4*>(codes)[i] = w[j];
+            }
+        }
+        if (threadIdx.x < tokens) scales[threadIdx.x] = __ldg(sa + threadIdx.x);
+    } else {                                                // (at most kStreamHold groups of eight a thread: all loads at once)
+        const uint32_t share = stream_share(tokens), t = threadIdx.x / share, lane = threadIdx.x & (share - 1);
+        const X* row = x + (uint64_t)(t < tokens ? t : 0) * ldx;
+        const bool vec = aligned16(row) && k % 8 == 0;
+        Raw8<X> v[kStreamHold];
+        uint32_t m = 0;
+        if (vec) {
+#pragma unroll
+            for (int h = 0; h < kStreamHold; ++h) v[h] = lane + h * share < groups ? load_raw8(row + (lane + h * share) * 8) : zero_raw8<X>();
         } else {
-            const bool vec = aligned16(row);
-            const auto fetch = [&](uint32_t g) { return vec ? fetch_raw8<X, true>(row, (uint64_t)g * 8, k) : fetch_raw8<X, false>(row, (uint64_t)g * 8, k); };
-            uint32_t m = 0;
-            if (live) {
-#pragma unroll 4
-                for (uint32_t g = lane; g < groups; g += tpt) m = top_raw8<X>(fetch(g), m);
-            }
-            m = __reduce_max_sync(kFullMask, top_bits<X>(top_of_halves<X>(m)));
-            if (tpt > 32) {
-                if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
-                __syncthreads();
-                const uint32_t w = tpt >> 5;
-                for (uint32_t i = 0; i < w; ++i) m = max(m, part[me * w + i]);
-                __syncthreads();
-            }
+#pragma unroll
+            for (int h = 0; h < kStreamHold; ++h)
+                v[h] = lane + h * share < groups ? fetch_raw8<X, false>(row, (lane + h * share) * 8, k) : zero_raw8<X>();
+        }
+#pragma unroll
+        for (int h = 0; h < kStreamHold; ++h) m = top_raw8<X>(v[h], m);
+        m = __reduce_max_sync(kFullMask, top_bits<X>(top_of_halves<X>(m)));
+        if (share > 32) {
+            if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
+            __syncthreads();
+            const uint32_t w = share >> 5;
+            for (uint32_t i = 0; i < w; ++i) m = max(m, part[t * w + i]);
+        }
+        if (t < tokens) {
             const LineScale s = line_scale(m);
-            if (live) {
-                if (lane == 0) scales[t] = s.scale;
-#pragma unroll 4
-                for (uint32_t g = lane; g < all; g += tpt) {
-                    uint2 w = make_uint2(0u, 0u);
-                    if (g < groups) {
-                        float v[8];
-                        widen8(fetch(g), v);
-                        w = code8<false>(v, s.inv, DrawArgs{}, DrawRow{}, 0);
-                    }
-                    dst[g] = w;
-                }
+            if (lane == 0) scales[t] = s.scale;
+            uint2* dst = reinterpret_cast<uint2*>(codes + t * pitch);
+#pragma unroll
+            for (int h = 0; h < kStreamHold; ++h) {
+                const uint32_t g = lane + h * share;
+                if (g >= all) break;
+                float f[8];
+                widen8(v[h], f);
+                dst[g] = code8<false>(f, s.inv, DrawArgs{}, DrawRow{}, 0);
             }
+            for (uint32_t g = lane + kStreamHold * share; g < all; g += share) dst[g] = make_uint2(0u, 0u);
         }
     }
 }
 
-template <typename X, typename T, bool WIDE>               // WIDE: more than 8 tokens
+template <typename X, typename T>
 __global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(const X* __restrict__ x, uint64_t ldx, const __grid_constant__ Product8 p) {
     extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ float scales[kStreamTokens];
     __shared__ uint32_t part[8];
-    __shared__ int red[2][8][32][4];
+    __shared__ int red[2][8][kStreamTokens][17];           // [half][warp][token][row]
     int8_t* codes = reinterpret_cast<int8_t*>(dyn);
-    const uint32_t k = (uint32_t)p.k, pitch = stream_pitch(k), kparts = (k + 511) / 512, tokens = (uint32_t)p.m;
+    const uint32_t k = (uint32_t)p.k, pitch = stream_pitch(k), kparts = (k + 255) / 256, tokens = (uint32_t)p.m;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const uint32_t ks = kparts >= 5 ? 8u : kparts >= 3 ? 4u : kparts;          // warps sharing a tile
-    const uint32_t per_round = 8 / ks, sub = warp / ks, kp0 = warp & (ks - 1);
-    const uint32_t steps = (kparts + ks - 1) / ks;          // of 512 codes, for a warp that has the most
-    const uint64_t rounds = ((p.n + 7) / 8 + per_round - 1) / per_round;
+    const uint32_t per_round = 8 / ks, sub = warp / ks, kp0 = warp & (ks - 1), chans = per_round * 16;
+    const uint32_t steps = (kparts + ks - 1) / ks;          // of 256 codes, for a warp that has the most
+    const uint64_t rounds = ((p.n + 15) / 16 + per_round - 1) / per_round;
     const uint64_t mine = blockIdx.x < rounds ? (rounds - 1 - blockIdx.x) / gridDim.x + 1 : 0;
 
-    uint4 buf[8];
+    uint4 buf[8];                                           // [four chunks][row g, row g + 8]
     const auto load = [&](uint64_t round, uint32_t step) {
-        const uint64_t row = (round * per_round + sub) * 8 + g;
-        const uint32_t c = (kp0 + step * ks) * 512 + q * 16;
-        const int8_t* src = p.b + row * p.ldb + c;
+        const uint64_t row = (round * per_round + sub) * 16 + g;
+        const uint32_t c = (kp0 + step * ks) * 256 + q * 16;
+        const int8_t *src = p.b + row * p.ldb + c, *src8 = src + 8 * p.ldb;
+        if (row + 8 < p.n && c + 192 < k) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            buf[i] = row < p.n && c + 64 * i < k ? __ldcs(reinterpret_cast<const uint4*>(src + 64 * i)) : make_uint4(0u, 0u, 0u, 0u);
+            for (int i = 0; i < 4; ++i) {
+                buf[2 * i] = __ldcs(reinterpret_cast<const uint4*>(src + 64 * i));
+                buf[2 * i + 1] = __ldcs(reinterpret_cast<const uint4*>(src8 + 64 * i));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+                buf[2 * i] = row < p.n && c + 64 * i < k ? __ldcs(reinterpret_cast<const uint4*>(src + 64 * i)) : zero;
+                buf[2 * i + 1] = row + 8 < p.n && c + 64 * i < k ? __ldcs(reinterpret_cast<const uint4*>(src8 + 64 * i)) : zero;
+            }
+        }
     };
     grid_wait();
     grid_go();
@@ -129,37 +149,38 @@ __global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(cons
     T* out = static_cast<T*>(p.out);
     for (uint64_t j = 0; j < mine; ++j) {
         const uint64_t round = blockIdx.x + j * gridDim.x;
-        const uint32_t chans = per_round * 8;
-        const uint64_t first = round * chans + threadIdx.x % chans;     // (blockDim is a multiple of chans: every output of this thread)
+        const uint64_t first = round * chans + threadIdx.x % chans;     // the channel of this thread's outputs (chans divides 256)
         const float sb = first < p.n ? __ldg(p.sb + first) : 0.f, bias = first < p.n && p.bias ? __ldg(p.bias + first) : 0.f;
-        int acc[4] = {}, odd[4] = {};                       // two chains
+        int acc[4][4] = {};
         for (uint32_t step = 0; step < steps; ++step) {
             uint4 w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = buf[i];
             if (step + 1 < steps) load(round, step + 1);
             else if (j + 1 < mine) load(round + gridDim.x, 0);
-            const uint32_t c = (kp0 + step * ks) * 512 + q * 16;
+            const uint32_t c = (kp0 + step * ks) * 256 + q * 16;
             if (kp0 + step * ks < kparts) {
+                uint4 a[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-                    const uint4 lo = g < tokens ? *reinterpret_cast<const uint4*>(codes + g * pitch + c + 64 * i) : zero;
-                    const uint4 hi = WIDE && g + 8 < tokens ? *reinterpret_cast<const uint4*>(codes + (g + 8) * pitch + c + 64 * i) : zero;
-                    mma_s8(acc, lo.x, hi.x, lo.y, hi.y, w[i].x, w[i].y);
-                    mma_s8(odd, lo.z, hi.z, lo.w, hi.w, w[i].z, w[i].w);
+                for (int i = 0; i < 4; ++i)
+                    a[i] = g < tokens ? *reinterpret_cast<const uint4*>(codes + g * pitch + c + 64 * i) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    mma_s8(acc[(2 * i) & 3], w[2 * i].x, w[2 * i + 1].x, w[2 * i].y, w[2 * i + 1].y, a[i].x, a[i].y);
+                    mma_s8(acc[(2 * i + 1) & 3], w[2 * i].z, w[2 * i + 1].z, w[2 * i].w, w[2 * i + 1].w, a[i].z, a[i].w);
                 }
             }
         }
-        int(*mem)[32][4] = red[j & 1];
-        *reinterpret_cast<int4*>(mem[warp][lane]) = make_int4(acc[0] + odd[0], acc[1] + odd[1], acc[2] + odd[2], acc[3] + odd[3]);
+        int(*mem)[kStreamTokens][17] = red[j & 1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)                         // element e: row g (+ 8 from 2 on), token 2 q + (e & 1)
+            mem[warp][2 * q + (e & 1)][g + (e & 2) * 4] = (acc[0][e] + acc[1][e]) + (acc[2][e] + acc[3][e]);
         __syncthreads();                                    // the other half of `red` is free: its readers passed this barrier last round
         for (uint32_t i = threadIdx.x; i < chans * tokens; i += kStreamThreads) {
-            const uint32_t tok = i / chans, ch = i - tok * chans;
             if (first >= p.n) break;
-            const uint32_t tile = ch >> 3, in = ch & 7, from = (tok & 7) * 4 + (in >> 1), reg = (tok >> 3) * 2 + (in & 1);
+            const uint32_t tok = i / chans, ch = i - tok * chans;
             int a = 0;
-            for (uint32_t s = 0; s < ks; ++s) a += mem[tile * ks + s][from][reg];
+            for (uint32_t s = 0; s < ks; ++s) a += mem[(ch >> 4) * ks + s][tok][ch & 15];
             out[(uint64_t)tok * p.ldo + first] = from_f32<T>(scaled(a, scales[tok], sb, p.bias, bias));
         }
     }
@@ -772,22 +793,22 @@ template <int NT, typename T> cudaError_t launch_slim(const Product8& p, uint32_
     return launch_layer(kernel, (unsigned)ctas, kSlimThreads, G::kSmem, split, st, mb, ma, p, split, tiles_n);
 }
 
-template <typename X, typename T, bool WIDE> cudaError_t launch_stream_one(const X* x, uint64_t ldx, const Product8& p, cudaStream_t st) {
+template <typename X, typename T> cudaError_t launch_stream(const X* x, uint64_t ldx, const Product8& p, cudaStream_t st) {
     static PerDevice<bool> done;
-    const auto kernel = product8_stream_kernel<X, T, WIDE>;
+    const auto kernel = product8_stream_kernel<X, T>;
     const cudaError_t e = allow_smem(kernel, kStreamSmem, done);
     if (e != cudaSuccess) return e;
-    const uint64_t kparts = (p.k + 511) / 512, ks = kparts >= 5 ? 8 : kparts >= 3 ? 4 : kparts;
-    const uint64_t rounds = ((p.n + 7) / 8 * ks + 7) / 8, most = 2ull * sm_count_now();
+    const uint64_t kparts = (p.k + 255) / 256, ks = kparts >= 5 ? 8 : kparts >= 3 ? 4 : kparts;
+    const uint64_t rounds = ((p.n + 15) / 16 * ks + 7) / 8, most = 2ull * sm_count_now();
     return launch_layer(kernel, (unsigned)(rounds < most ? rounds : most), kStreamThreads, p.m * stream_pitch(p.k), 1, st, x, ldx, p);
-}
-template <typename X, typename T> cudaError_t launch_stream(const X* x, uint64_t ldx, const Product8& p, cudaStream_t st) {
-    return p.m > 8 ? launch_stream_one<X, T, true>(x, ldx, p, st) : launch_stream_one<X, T, false>(x, ldx, p, st);
 }
 
 }  // namespace
 
+// The codes of the tokens have to fit beside another CTA's; coding them in every CTA pays as long as their lines fit its
+// registers (8 x 2048: 1 us, against a launch of its own).
 bool product8_streams(uint64_t tokens, uint64_t k) { return tokens <= kStreamTokens && tokens * stream_pitch(k) <= kStreamSmem; }
+bool product8_codes_tokens(uint64_t tokens, uint64_t k) { return product8_streams(tokens, k) && k <= 8ull * kStreamHold * stream_share(tokens); }
 
 cudaError_t launch_linear8_stream(const void* x, uint64_t ldx, const Product8& p, cudaStream_t st) {
     return with_type(p.type, [&](auto t) {
