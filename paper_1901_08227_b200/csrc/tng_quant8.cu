@@ -68,6 +68,7 @@ template <typename T> struct ColumnJob {
     const T* x;
     uint64_t rows, cols, ldx, rows_per_chunk;
     uint32_t blocks, tiles, chunks;   // CTA columns of the first pass and of the second, row chunks of the first
+    uint32_t per_cta;              // rows a CTA of the second pass: kRowsPerCta, or kRowTile where that leaves SMs idle
     uint32_t* tops;                // largest |x| as bit patterns, cleared before
     float* sums;                   // chunks x cols, or nullptr
     int8_t* q;
@@ -173,8 +174,8 @@ __global__ void __launch_bounds__(256, DRAW ? (ROWS ? 2 : 3) : (ROWS ? 3 : 4)) q
     const uint64_t c0 = (uint64_t)(cta - slab * job.tiles) * kColTile;
     const uint32_t cg = threadIdx.x & 7, rg = threadIdx.x >> 3;       // eight columns, four rows
     const uint64_t c = c0 + cg * 8;
-    const uint64_t first = (uint64_t)slab * kRowsPerCta;
-    const uint64_t last = first + kRowsPerCta < rows ? first + kRowsPerCta : rows;
+    const uint64_t first = (uint64_t)slab * job.per_cta;
+    const uint64_t last = first + job.per_cta < rows ? first + job.per_cta : rows;
     const bool wide = VEC && c0 + kColTile <= cols;      // all 64 columns: vector loads, no tests on columns
     Raw8<T> v[4];
     const T* px = x + (first + rg * 4) * ldx + c;
@@ -288,11 +289,11 @@ __global__ void __launch_bounds__(256, DRAW ? (ROWS ? 2 : 3) : (ROWS ? 3 : 4)) q
     }
 }
 
-// Row chunks of the statistics: about four CTAs an SM, 64 rows at least.
+// Row chunks of the statistics: about four CTAs an SM, 32 rows at least.
 uint32_t column_chunks(uint64_t rows, uint64_t cols) {
     const uint64_t blocks = (cols + kStatCols - 1) / kStatCols;
     uint64_t chunks = (4 * 148 + blocks - 1) / blocks;
-    const uint64_t most = (rows + 63) / 64;
+    const uint64_t most = (rows + 31) / 32;
     if (chunks > most) chunks = most;
     return chunks < 1 ? 1u : (uint32_t)chunks;
 }
@@ -363,6 +364,8 @@ cudaError_t launch_quant8_cols(const Quant8Cols* jobs, int n, tng_dtype type, cu
             o.q = in.q; o.ldq = in.ldq; o.scale = in.scale; o.colsum = in.colsum;
             o.row_tops = in.row_tops; o.row_q = in.row_q; o.ld_row = in.ld_row; o.row_scale = in.row_scale;
             ctas[i] = o.tiles * ((in.rows + kRowsPerCta - 1) / kRowsPerCta);
+            o.per_cta = ctas[i] < 2ull * sm_count_now() ? kRowTile : kRowsPerCta;
+            ctas[i] = o.tiles * ((in.rows + o.per_cta - 1) / o.per_cta);
             vec[i] = rows_aligned<T>(in.x, in.rows, in.ldx);
         }
         if (ctas[0] + ctas[1] >= (1ull << 31)) return cudaErrorInvalidValue;
