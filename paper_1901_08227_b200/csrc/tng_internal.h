@@ -127,6 +127,8 @@ struct Product8 {
     uint64_t ldo;
 };
 cudaError_t launch_product8(const Product8& p, cudaStream_t st);
+// Two independent products, the second with fp32 outputs.
+cudaError_t launch_product8_two(const Product8& p, const Product8& fp32, cudaStream_t st);
 // Whether a linear layer with this many tokens is one launch that streams the weights past tokens it codes itself, and
 // that launch: x has rows of p.type, p.a and p.sa are unused.
 bool product8_codes_tokens(uint64_t tokens, uint64_t k);

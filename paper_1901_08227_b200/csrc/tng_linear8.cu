@@ -74,7 +74,7 @@ tng_status tng_linear8_grad(const void* dy_dev, uint64_t lddy, const void* x_dev
     if (dx_dev && (!matrix_ok(dx_dev, type, k, lddx) || !codes_ok(wt_dev, n, ldwt) || !swt_dev || !aligned(swt_dev, 4)))
         return TNG_ERR_INVALID_ARG;
     // With a sum over the tokens to form, dy's row and column codes come from the same passes, and x's columns share their
-    // launches: clear the maxima (side by side), maxima, codes, two products.  dx alone needs the rows only.
+    // launches: clear the maxima (side by side), maxima, codes, products.  dx alone needs the rows only.
     Carver c{static_cast<unsigned char*>(scratch_dev)};
     const uint64_t ldr = tng_code_stride(n), ldc = tng_code_stride(tokens);
     int8_t* qr = c.take<int8_t>(codes_bytes(tokens, n));
@@ -94,14 +94,10 @@ tng_status tng_linear8_grad(const void* dy_dev, uint64_t lddy, const void* x_dev
     } else if (dx_dev && launch_quant8_rows(dy_dev, type, tokens, n, lddy, draw, qr, ldr, sr, st) != cudaSuccess) {
         return TNG_ERR_CUDA;
     }
-    if (dx_dev) {
-        const Product8 p{qr, wt_dev, ldr, ldwt, sr, swt_dev, nullptr, tokens, k, n, dx_dev, type, lddx};
-        if (launch_product8(p, st) != cudaSuccess) return TNG_ERR_CUDA;
-    }
-    if (dw_dev) {
-        const Product8 p{qy, qx, ldc, ldc, sy, sx, nullptr, n, k, tokens, dw_dev, TNG_F32, lddw};
-        if (launch_product8(p, st) != cudaSuccess) return TNG_ERR_CUDA;
-    }
+    const Product8 to_x{qr, wt_dev, ldr, ldwt, sr, swt_dev, nullptr, tokens, k, n, dx_dev, type, lddx};
+    const Product8 to_w{qy, qx, ldc, ldc, sy, sx, nullptr, n, k, tokens, dw_dev, TNG_F32, lddw};
+    const cudaError_t e = dx_dev && dw_dev ? launch_product8_two(to_x, to_w, st) : dx_dev ? launch_product8(to_x, st) : dw_dev ? launch_product8(to_w, st) : cudaSuccess;
+    if (e != cudaSuccess) return TNG_ERR_CUDA;
     return TNG_OK;
 }
 

@@ -203,13 +203,78 @@ constexpr uint32_t kPairStages = 6, kPairHalf = 128 * 128, kPairStage = 2 * kPai
 static_assert(128 * kPairTile * 4 <= kPairStages * kPairStage, "the stages also hold the sums");
 constexpr uint32_t kPairSmem = 1024 + kPairStages * kPairStage + 16 * kStageStride + 256;
 
-struct TileWalk {                                          // tile order: groups of eight tile rows, columns outside
-    uint32_t tiles_m, tiles_n;
-    __device__ __forceinline__ void at(uint32_t t, uint32_t& tm, uint32_t& tn) const {
-        const uint32_t per = 8 * tiles_n, g = t / per, first = g * 8;
-        const uint32_t rows = tiles_m - first < 8 ? tiles_m - first : 8, r = t - g * per;
+// What one launch computes: one product, or two independent ones (a gradient's dx and dw, which together leave fewer
+// pairs idle at the end than one after the other).
+struct PairArgs {
+    Product8 p[2];
+};
+struct PairMaps {
+    CUtensorMap a, b, o;
+};
+
+// A pair's tiles, the same sequence for each of its roles.  Within a product: groups of eight tile rows, columns outside.
+// Of two products the one with the longer contraction (job `first`) goes first, tile by tile over the pairs; the pairs that
+// get one tile of it less then take as many of the other's as that is worth, and the rest goes over all pairs again.
+struct TileWalk {
+    struct Job {
+        uint32_t tiles_m, tiles_n, kblocks;
+    } job[2];
+    uint32_t first, pair, pairs, spare, extra, phase, next, cur, tm, tn;
+
+    __device__ __forceinline__ static Job shape(const Product8& p) { return {(uint32_t)((p.m + 255) / 256), (uint32_t)((p.n + 255) / 256), (uint32_t)((p.k + 127) / 128)}; }
+    __device__ __forceinline__ uint32_t count(uint32_t j) const { return job[j].tiles_m * job[j].tiles_n; }
+    template <bool DUAL> __device__ __forceinline__ void start(const PairArgs& args, uint32_t pair_, uint32_t pairs_) {
+        pair = pair_;
+        pairs = pairs_;
+        job[0] = shape(args.p[0]);
+        if (DUAL) job[1] = shape(args.p[1]);
+        first = DUAL && job[1].kblocks > job[0].kblocks;
+        phase = 0;
+        next = pair;
+        spare = extra = 0;
+        if (DUAL) {
+            spare = count(first) % pairs;                  // pairs with one more of the first job's tiles
+            const uint32_t worth = spare ? job[first].kblocks / job[first ^ 1].kblocks : 0;
+            const uint32_t all = worth * (pairs - spare), have = count(first ^ 1);
+            extra = all < have ? all : have;
+        }
+    }
+    // The next tile into cur (job), tm, tn; false when there is none.
+    template <bool DUAL> __device__ __forceinline__ bool step() {
+        uint32_t t = next;
+        cur = first;
+        if (phase == 0) {
+            if (t < count(first)) {
+                next = t + pairs;
+            } else if (!DUAL) {
+                return false;
+            } else {
+                phase = 1;
+                next = pair >= spare ? pair - spare : extra;
+            }
+        }
+        if (DUAL && phase == 1) {
+            cur = first ^ 1;
+            t = next;
+            if (t < extra) {
+                next = t + (pairs - spare);
+            } else {
+                phase = 2;
+                next = extra + (pair >= spare ? pair - spare : pair + pairs - spare);
+            }
+        }
+        if (DUAL && phase == 2) {
+            cur = first ^ 1;
+            t = next;
+            if (t >= count(cur)) return false;
+            next = t + pairs;
+        }
+        const Job& j = job[cur];
+        const uint32_t per = 8 * j.tiles_n, g = t / per, top = g * 8;
+        const uint32_t rows = j.tiles_m - top < 8 ? j.tiles_m - top : 8, r = t - g * per;
         tn = r / rows;
-        tm = first + (r - tn * rows);
+        tm = top + (r - tn * rows);
+        return true;
     }
 };
 
@@ -315,10 +380,12 @@ __device__ __forceinline__ void finish_columns(const Product8& p, const CUtensor
     }
 }
 
-template <typename T, bool SPLIT, bool TILES>
+// T: element type of the (first) output; DUAL: the second one's is fp32.
+template <typename T, bool SPLIT, bool TILES, bool DUAL>
 __global__ void __launch_bounds__(kPairThreads, 1)
     product8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_o,
-                         const __grid_constant__ Product8 p, uint32_t split) {
+                         const __grid_constant__ PairMaps maps2, const __grid_constant__ PairArgs args, uint32_t split) {
+    static_assert(!(SPLIT && DUAL) && (TILES || !DUAL), "two products are whole tiles, by tiled copies");
     extern __shared__ unsigned char dyn[];
     __shared__ uint32_t sh_tmem;
     __shared__ volatile uint32_t sh_failed;
@@ -332,10 +399,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const uint32_t rank = in_cluster & 1u, even = in_cluster & ~1u;            // the pair's CTA that issues
     const uint32_t part = SPLIT ? in_cluster >> 1 : 0, parts = SPLIT ? split : 1;
     const uint32_t pair = (blockIdx.x >> 1) / parts, pairs = (gridDim.x >> 1) / parts;
-    const uint32_t all_blocks = (uint32_t)((p.k + 127) / 128);
-    const uint32_t kb0 = SPLIT ? all_blocks * part / parts : 0, kb1 = SPLIT ? all_blocks * (part + 1) / parts : all_blocks;
-    const TileWalk walk{(uint32_t)((p.m + 255) / 256), (uint32_t)((p.n + 255) / 256)};
-    const uint32_t tiles = walk.tiles_m * walk.tiles_n;
+    TileWalk walk = {};
+    walk.start<DUAL>(args, pair, pairs);
+    const auto k_first = [&] { return SPLIT ? walk.job[0].kblocks * part / parts : 0u; };
+    const auto k_last = [&] { return SPLIT ? walk.job[0].kblocks * (part + 1) / parts : walk.job[DUAL ? walk.cur : 0].kblocks; };
 
     if (threadIdx.x == 0) {
         sh_failed = 0;
@@ -363,19 +430,19 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 
     if (warp == 16 && lane == 0) {
         // ---- feed: this CTA's rows of either operand, completion counted on the even CTA's barrier
-        uint32_t it = 0;
+        uint32_t it = 0, s = 0, parity = 1;                // parity of the stage's last release (the first use waits for none)
         bool ok = true;
-        for (uint32_t t = pair; t < tiles && ok; t += pairs) {
-            uint32_t tm, tn;
-            walk.at(t, tm, tn);
-            const int32_t ya = (int32_t)(tm * kPairTile + rank * 128), yb = (int32_t)(tn * kPairTile + rank * 128);
-            for (uint32_t kb = kb0; kb < kb1; ++kb, ++it) {
-                const uint32_t s = it % kPairStages, use = it / kPairStages;
-                if (use > 0 && !mbar_wait(empty(s), (use - 1) & 1u)) { ok = false; break; }
+        while (ok && walk.step<DUAL>()) {
+            const int32_t ya = (int32_t)(walk.tm * kPairTile + rank * 128), yb = (int32_t)(walk.tn * kPairTile + rank * 128);
+            const CUtensorMap *from_a = DUAL && walk.cur ? &maps2.a : &map_a, *from_b = DUAL && walk.cur ? &maps2.b : &map_b;
+            const int32_t x1 = (int32_t)(k_last() * 128);
+            for (int32_t x = (int32_t)(k_first() * 128); x < x1; x += 128, ++it) {
+                if (it >= kPairStages && !mbar_wait(empty(s), parity)) { ok = false; break; }
                 if (rank == 0) mbar_expect_tx(full(s), 2 * kPairStage);
                 const uint32_t dst = data + s * kPairStage, bar = cluster_map(full(s), even);
-                tile_load<2>(dst, &map_a, (int32_t)(kb * 128), ya, bar);
-                tile_load<2>(dst + kPairHalf, &map_b, (int32_t)(kb * 128), yb, bar);
+                tile_load<2>(dst, from_a, x, ya, bar);
+                tile_load<2>(dst + kPairHalf, from_b, x, yb, bar);
+                if (++s == kPairStages) { s = 0; parity ^= 1u; }
             }
         }
         if (!ok) {                                         // the odd CTA cannot see its copies land: leave them a millisecond
@@ -389,21 +456,28 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         // ---- issue
         constexpr uint32_t idesc = umma_idesc_s8(256, kPairTile);
         const uint16_t both = (uint16_t)(3u << even);
-        uint32_t it = 0, n_acc = 0;
+        uint32_t s = 0, parity = 0, n_acc = 0;
         bool ok = true;
-        for (uint32_t t = pair; t < tiles && ok; t += pairs, ++n_acc) {
-            const uint32_t acc = n_acc & 1u, use = n_acc >> 1;
+        for (; ok && walk.step<DUAL>(); ++n_acc) {
+            const uint32_t acc = n_acc & 1u, use = n_acc >> 1, blocks = k_last() - k_first(), into = tmem + acc * kPairTile;
+            // instructions of the last block: 32 codes each
+            const uint32_t rest = (uint32_t)((args.p[DUAL ? walk.cur : 0].k + 31) / 32) - (k_last() - 1) * 4, last_steps = rest < 4 ? rest : 4;
             if (use > 0 && !mbar_wait(acc_empty + 8 * acc, (use - 1) & 1u)) { ok = false; break; }
             umma_fence_after();
-            for (uint32_t kb = kb0; kb < kb1; ++kb, ++it) {
-                const uint32_t s = it % kPairStages;
-                if (!mbar_wait(full(s), (it / kPairStages) & 1u)) { ok = false; break; }
+            for (uint32_t kb = 0; kb < blocks; ++kb) {
+                if (!mbar_wait(full(s), parity)) { ok = false; break; }
                 umma_fence_after();
                 const uint64_t da = umma_desc(data + s * kPairStage), db = umma_desc(data + s * kPairStage + kPairHalf);
-                const uint64_t left = p.k - (uint64_t)kb * 128;
-                const uint32_t steps = left >= 128 ? 4u : (uint32_t)((left + 31) / 32);
-                for (uint32_t j = 0; j < steps; ++j) umma_s8<2>(tmem + acc * kPairTile, da + 2 * j, db + 2 * j, idesc, kb > kb0 || j > 0);
+                if (kb + 1 < blocks || last_steps == 4) {
+                    umma_s8<2>(into, da, db, idesc, kb > 0);
+                    umma_s8<2>(into, da + 2, db + 2, idesc, true);
+                    umma_s8<2>(into, da + 4, db + 4, idesc, true);
+                    umma_s8<2>(into, da + 6, db + 6, idesc, true);
+                } else {
+                    for (uint32_t j = 0; j < last_steps; ++j) umma_s8<2>(into, da + 2 * j, db + 2 * j, idesc, kb > 0 || j > 0);
+                }
                 umma_commit_pair(empty(s), both);
+                if (++s == kPairStages) { s = 0; parity ^= 1u; }
             }
             if (ok) umma_commit_pair(acc_full + 8 * acc, both);
         }
@@ -422,21 +496,23 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             // ---- write out: rows 32 quad + lane of this CTA's 128, 64 columns
             uint32_t n_acc = 0;
             bool ok = true;
-            for (uint32_t t = pair; t < tiles; t += pairs, ++n_acc) {
+            for (; walk.step<DUAL>(); ++n_acc) {
                 const uint32_t acc = n_acc & 1u, use = n_acc >> 1;
-                uint32_t tm, tn;
-                walk.at(t, tm, tn);
-                const uint64_t row0 = (uint64_t)tm * kPairTile + row_in, col0 = (uint64_t)tn * kPairTile + group * 64;
+                const Product8& p = args.p[DUAL ? walk.cur : 0];
+                const uint64_t row0 = (uint64_t)walk.tm * kPairTile + row_in, col0 = (uint64_t)walk.tn * kPairTile + group * 64;
                 const float sa = row0 + lane < p.m ? __ldg(p.sa + row0 + lane) : 0.f;
                 const ColumnScale cs[2] = {column_scale(p, col0 + lane), column_scale(p, col0 + 32 + lane)};
                 if (ok && !mbar_wait(acc_full + 8 * acc, use & 1u)) ok = false;
                 ok = __all_sync(kFullMask, ok && !sh_failed);
                 umma_fence_after();
-                finish_columns<T, kWidth, TILES>(p, &map_o, tmem + ((quad * 32) << 16) + acc * kPairTile + group * 64, ok, sa, cs, row0, col0, stage, lane, [&] {
+                const uint32_t from = tmem + ((quad * 32) << 16) + acc * kPairTile + group * 64;
+                const auto done = [&] {
                     umma_fence_before();                   // everything read: the next tile may overwrite it
                     __syncwarp();
                     if (lane == 0) cluster_arrive(cluster_map(acc_empty + 8 * acc, even));
-                });
+                };
+                if (DUAL && walk.cur) finish_columns<float, 16, true>(p, &maps2.o, from, ok, sa, cs, row0, col0, stage, lane, done);
+                else finish_columns<T, kWidth, TILES>(p, &map_o, from, ok, sa, cs, row0, col0, stage, lane, done);
             }
             if (TILES && lane == 0) tile_store_wait_all();
         }
@@ -450,9 +526,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         const uint32_t cols = kPairTile / parts, mine = part * cols;
         int4* sums = reinterpret_cast<int4*>(stages);      // [four columns][row]: a warp's access is contiguous; every copy
         bool ok = true;                                    // has landed and every instruction has read its operands
-        uint32_t tm, tn;
-        walk.at(pair, tm, tn);
-        const uint64_t row0 = (uint64_t)tm * kPairTile + row_in, col0 = (uint64_t)tn * kPairTile + mine + group * 32;
+        const Product8& p = args.p[0];
+        (void)walk.step<DUAL>();
+        const uint64_t row0 = (uint64_t)walk.tm * kPairTile + row_in, col0 = (uint64_t)walk.tn * kPairTile + mine + group * 32;
         const bool own = group * 32 < cols;                // 32 columns a warp, of one's own
         float sa = 0.f;
         ColumnScale cs = {};
@@ -526,6 +602,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 // their int32 sums in shared memory and each write out a part of the columns, summed over the cluster's shared
 // memories.  Warps: 0-3 write out, 4 feeds, 5 issues.
 constexpr int kSlimThreads = 192;
+constexpr uint64_t kSlimRows = 128;                        // rows of a up to which this kernel is taken
 template <int NT> struct SlimGeom {
     static constexpr uint32_t kA = 128 * 128, kB = NT * 128, kStage = kA + kB;
     static constexpr uint32_t kStages = NT == 128 ? 3 : 4;
@@ -732,24 +809,31 @@ template <typename K> cudaError_t allow_smem(K kernel, uint32_t bytes, PerDevice
     return e;
 }
 
-template <typename T, bool SPLIT, bool TILES> cudaError_t launch_pair_as(const Product8& p, uint32_t split, cudaStream_t st) {
+template <typename T, bool SPLIT, bool TILES, bool DUAL>
+cudaError_t launch_pair_as(const Product8& p, const Product8* p2, uint32_t split, cudaStream_t st) {
     static PerDevice<bool> done;
-    const auto kernel = product8_pair_kernel<T, SPLIT, TILES>;
+    const auto kernel = product8_pair_kernel<T, SPLIT, TILES, DUAL>;
     cudaError_t e = allow_smem(kernel, kPairSmem, done);
     if (e != cudaSuccess) return e;
-    CUtensorMap ma, mb, mo;
-    if (!make_map(&ma, p.a, p.m, p.k, p.lda, 128) || !make_map(&mb, p.b, p.n, p.k, p.ldb, 128)) return cudaErrorNotSupported;
-    mo = ma;
-    if (TILES && !make_out_map(&mo, p, sizeof(T))) return cudaErrorNotSupported;
-    const uint64_t tiles = (p.m + 255) / 256 * ((p.n + 255) / 256), pairs = (uint64_t)sm_count_now() / 2;
+    PairArgs args = {};
+    PairMaps maps[2] = {};
+    uint64_t tiles = 0;
+    for (int i = 0; i < (DUAL ? 2 : 1); ++i) {
+        const Product8& q = args.p[i] = i ? *p2 : p;
+        if (!make_map(&maps[i].a, q.a, q.m, q.k, q.lda, 128) || !make_map(&maps[i].b, q.b, q.n, q.k, q.ldb, 128)) return cudaErrorNotSupported;
+        if (TILES && !make_out_map(&maps[i].o, q, i ? 4 : sizeof(T))) return cudaErrorNotSupported;
+        tiles += (q.m + 255) / 256 * ((q.n + 255) / 256);
+    }
+    const uint64_t pairs = (uint64_t)sm_count_now() / 2;
     if (tiles >= (1ull << 31)) return cudaErrorInvalidValue;
     return launch_layer(kernel, (unsigned)(2 * (SPLIT ? tiles * split : tiles < pairs ? tiles : pairs)), kPairThreads, kPairSmem, 2 * split, st,
-                        ma, mb, mo, p, split);
+                        maps[0].a, maps[0].b, maps[0].o, maps[1], args, split);
 }
+bool rows_by_tiles(const Product8& p) { return (reinterpret_cast<uintptr_t>(p.out) | p.ldo * type_bytes(p.type)) % 16 == 0; }
 template <typename T> cudaError_t launch_pair(const Product8& p, uint32_t split, cudaStream_t st) {
-    const bool tiles = (reinterpret_cast<uintptr_t>(p.out) | p.ldo * sizeof(T)) % 16 == 0;
-    if (split > 1) return tiles ? launch_pair_as<T, true, true>(p, split, st) : launch_pair_as<T, true, false>(p, split, st);
-    return tiles ? launch_pair_as<T, false, true>(p, 1, st) : launch_pair_as<T, false, false>(p, 1, st);
+    const bool tiles = rows_by_tiles(p);
+    if (split > 1) return tiles ? launch_pair_as<T, true, true, false>(p, nullptr, split, st) : launch_pair_as<T, true, false, false>(p, nullptr, split, st);
+    return tiles ? launch_pair_as<T, false, true, false>(p, nullptr, 1, st) : launch_pair_as<T, false, false, false>(p, nullptr, 1, st);
 }
 
 // Clusters of `split` pairs that run at once on this device.
@@ -759,7 +843,7 @@ template <typename T> uint64_t resident_clusters(uint32_t split) {
     PerDevice<int>& table = known[split == 2 ? 0 : 1];
     if (slot >= 0 && table.v[slot] > 0) return (uint64_t)table.v[slot] - 1;
     static PerDevice<bool> done;
-    const auto kernel = product8_pair_kernel<T, true, true>;
+    const auto kernel = product8_pair_kernel<T, true, true, false>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * split);
     cfg.blockDim = dim3(kPairThreads);
@@ -777,6 +861,15 @@ template <typename T> uint64_t resident_clusters(uint32_t split) {
     }
     if (slot >= 0) table.v[slot] = n + 1;
     return (uint64_t)n;
+}
+
+// Tiles that leave pairs idle: split the contraction, four stages of it at least to a part, as long as all clusters run
+// at once (512 x 4096 x 4096, 32 tiles: 18.3 us whole, 15.2 in two parts, 35.1 in four, where clusters of eight queue).
+template <typename T> uint32_t pair_split(const Product8& p) {
+    const uint64_t tiles = (p.m + 255) / 256 * ((p.n + 255) / 256), kblocks = (p.k + 127) / 128;
+    uint32_t split = 1;
+    while (split < 4 && kblocks >= split * 8 && tiles <= resident_clusters<T>(split * 2)) split *= 2;
+    return split;
 }
 
 template <int NT, typename T> cudaError_t launch_slim(const Product8& p, uint32_t split, cudaStream_t st) {
@@ -822,7 +915,7 @@ cudaError_t launch_product8(const Product8& p, cudaStream_t st) {
     return with_type(p.type, [&](auto t) {
         using T = decltype(t);
         if (product8_streams(p.m, p.k)) return launch_stream<int8_t, T>(p.a, p.lda, p, st);
-        if (p.m <= 128) {
+        if (p.m <= kSlimRows) {
             const uint64_t nt = p.m <= 16 ? 16 : p.m <= 32 ? 32 : p.m <= 64 ? 64 : 128;
             const uint64_t tiles = (p.n + 127) / 128 * ((p.m + nt - 1) / nt);
             uint32_t split = 1;
@@ -832,13 +925,19 @@ cudaError_t launch_product8(const Product8& p, cudaStream_t st) {
             if (nt == 64) return launch_slim<64, T>(p, split, st);
             return launch_slim<128, T>(p, split, st);
         }
-        // Tiles that leave pairs idle: split the contraction, four stages of it at least to a part, as long as all
-        // clusters run at once (512 x 4096 x 4096, 32 tiles: 18.3 us whole, 15.2 in two parts, 35.1 in four, where
-        // clusters of eight queue).
-        const uint64_t tiles = (p.m + 255) / 256 * ((p.n + 255) / 256);
-        uint32_t split = 1;
-        while (split < 4 && kblocks >= split * 8 && tiles <= resident_clusters<T>(split * 2)) split *= 2;
+        const uint32_t split = pair_split<T>(p);
         return launch_pair<T>(p, split, st);
+    });
+}
+
+cudaError_t launch_product8_two(const Product8& p, const Product8& fp32, cudaStream_t st) {
+    return with_type(p.type, [&](auto t) {
+        using T = decltype(t);
+        // one launch where each would be whole tiles anyway
+        if (p.m > kSlimRows && fp32.m > kSlimRows && rows_by_tiles(p) && rows_by_tiles(fp32) && pair_split<T>(p) == 1 && pair_split<float>(fp32) == 1)
+            return launch_pair_as<T, false, true, true>(p, &fp32, 1, st);
+        const cudaError_t e = launch_product8(p, st);
+        return e != cudaSuccess ? e : launch_product8(fp32, st);
     });
 }
 

@@ -436,3 +436,18 @@ def test_refusals():
     assert L.tng_dropout(x.data_ptr(), tng.BF16, 8, 64, 63, None, 0, 0.5, d, x.data_ptr(), 64, st) == tng.ERR_INVALID_ARG
     assert L.tng_quant8_cols(x.data_ptr(), tng.BF16, 8, 64, 64, None, a.data_ptr(), 16, sa.data_ptr(), None, None, st) == tng.ERR_INVALID_ARG
     assert L.tng_linear8(x20.data_ptr(), tng.BF16, 20, 64, 64, w.data_ptr(), 64, sw.data_ptr(), 32, None, x.data_ptr(), 32, None, st) == tng.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,K,N", [(129, 129 * 4, 136), (2048, 512, 520), (640, 8192, 6000), (5000, 1024, 1032), (300, 2600, 2600), (9000, 768, 2900), (1500, 5000, 20000)])
+def test_linear_gradients_of_many_tiles(dtype, T, K, N):
+    """dx and dw in one launch where both are whole tiles: every order of the two, all tiles written once.  The reference
+    runs on the GPU in 64 bits."""
+    x, dy = values((T, K), dtype, 1), values((T, N), dtype, 2, 1e-2)
+    wt, swt = tng.quant8_cols(values((N, K), torch.float32, 3, K ** -0.5))
+    dx = torch.full((T, K), float("nan"), dtype=dtype, device="cuda")
+    dw = torch.full((N, K), float("nan"), device="cuda")
+    tng.linear8_grad(dy, x, wt, swt, dx=dx, dw=dw)
+    for out, (a, sa), (b, sb) in ((dx, tng.quant8_rows(dy), (wt, swt)), (dw, tng.quant8_cols(dy), tng.quant8_cols(x))):
+        y = (a.double() @ b.double().t()).round().float() * sa[:, None] * sb[None, :]
+        assert torch.equal(out, y.to(out.dtype))
