@@ -59,12 +59,12 @@ template <typename T, bool VEC> __device__ __forceinline__ Raw8<T> fetch_raw8(co
     uint32_t* w = reinterpret_cast<uint32_t*>(&r);
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = c + j < cols ? __ldg(reinterpret_cast<const uint32_t*>(row) + c + j) : 0u;
+        for (int j = 0; j < 8; ++j) w[j] = c + j < cols ? load4_bits(row + c + j) : 0u;
     } else {
         const uint16_t* h = reinterpret_cast<const uint16_t*>(row) + c;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t lo = c + 2 * j < cols ? __ldg(h + 2 * j) : 0u, hi = c + 2 * j + 1 < cols ? __ldg(h + 2 * j + 1) : 0u;
+            const uint32_t lo = c + 2 * j < cols ? load2_bits(h + 2 * j) : 0u, hi = c + 2 * j + 1 < cols ? load2_bits(h + 2 * j + 1) : 0u;
             w[j] = lo | hi << 16;
         }
     }

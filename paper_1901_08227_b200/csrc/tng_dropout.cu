@@ -31,7 +31,7 @@ __device__ __forceinline__ float kept(float x, uint32_t word, const DropArgs& a)
 template <typename T> __device__ __forceinline__ Raw8<T> load_stream8(const T* p) {
     Raw8<T> r;
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.w[i] = load16_once(reinterpret_cast<const uint4*>(p) + i);
     return r;
 }
 

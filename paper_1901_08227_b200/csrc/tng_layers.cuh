@@ -67,6 +67,37 @@ __device__ __forceinline__ uint4 draw_words(const DrawArgs& a, const DrawRow& r,
     return make_uint4(c0, c1, c2, c3);
 }
 
+// The layer kernels are launched so that one may be set up while the one before it on the stream ends (a few
+// microseconds a launch, in chains of short kernels).  Every thread calls grid_wait() before it touches global memory:
+// it returns when all earlier work on the stream is complete and visible; grid_go() lets the next launch begin its set-up.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// Loads of what an earlier launch may have written.  Not the read-only path (__ldg, or a const __restrict__ parameter): that
+// one is for data that nobody writes while the kernel exists, and here the launch before may still be writing when
+// this one starts to wait; volatile, so that none moves ahead of grid_wait().
+__device__ __forceinline__ uint4 load16(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint4 load16_once(const void* p) {              // read once: first to leave the caches
+    uint4 v;
+    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t load4_bits(const void* p) {
+    uint32_t v;
+    asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t load2_bits(const void* p) {
+    uint16_t v;
+    asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float load_f32(const float* p) { return __uint_as_float(load4_bits(p)); }
+
 template <typename T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32(float v) { return v; }
 template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -101,7 +132,7 @@ template <typename T> struct Raw8 {
 template <typename T> __device__ __forceinline__ Raw8<T> load_raw8(const T* p) {   // p 16-byte aligned
     Raw8<T> r;
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.w[i] = load16(reinterpret_cast<const uint4*>(p) + i);
     return r;
 }
 template <typename T> __device__ __forceinline__ void widen8(const Raw8<T>& r, float (&v)[8]) {
@@ -129,11 +160,6 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float (
 
 __device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// The layer kernels are launched so that one may be set up while the one before it on the stream ends (a few
-// microseconds a launch, in chains of short kernels).  Every thread calls grid_wait() before it touches global memory:
-// it returns when all earlier work on the stream is complete and visible; grid_go() lets the next launch begin its set-up.
-__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void grid_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <typename... P, typename... A>
 cudaError_t launch_layer(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, unsigned cluster, cudaStream_t st, const A&... args) {
     cudaLaunchConfig_t cfg = {};

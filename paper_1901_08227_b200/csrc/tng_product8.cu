@@ -50,7 +50,7 @@ __device__ __forceinline__ void stream_tokens(const X* x, uint64_t ldx, const fl
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t i = i0 + j * kStreamThreads, t = i / per, g = i - t * per;
-                w[j] = i < total && g * 16 < k ? __ldg(reinterpret_cast<const uint4*>(x + (uint64_t)t * ldx) + g) : make_uint4(0u, 0u, 0u, 0u);
+                w[j] = i < total && g * 16 < k ? load16(reinterpret_cast<const uint4*>(x + (uint64_t)t * ldx) + g) : make_uint4(0u, 0u, 0u, 0u);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -64,7 +64,7 @@ __device__ __forceinline__ void stream_tokens(const X* x, uint64_t ldx, const fl
                 reinterpret_cast<uint4*>(codes)[i] = w[j];
             }
         }
-        if (threadIdx.x < tokens) scales[threadIdx.x] = __ldg(sa + threadIdx.x);
+        if (threadIdx.x < tokens) scales[threadIdx.x] = load_f32(sa + threadIdx.x);
     } else {                                                // (at most kStreamHold groups of eight a thread: all loads at once)
         const uint32_t share = stream_share(tokens), t = threadIdx.x / share, lane = threadIdx.x & (share - 1);
         const X* row = x + (uint64_t)(t < tokens ? t : 0) * ldx;
@@ -106,7 +106,7 @@ __device__ __forceinline__ void stream_tokens(const X* x, uint64_t ldx, const fl
 }
 
 template <typename X, typename T>
-__global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(const X* __restrict__ x, uint64_t ldx, const __grid_constant__ Product8 p) {
+__global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(const X* x, uint64_t ldx, const __grid_constant__ Product8 p) {
     extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ float scales[kStreamTokens];
     __shared__ uint32_t part[8];
@@ -128,15 +128,15 @@ __global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(cons
         if (row + 8 < p.n && c + 192 < k) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                buf[2 * i] = __ldcs(reinterpret_cast<const uint4*>(src + 64 * i));
-                buf[2 * i + 1] = __ldcs(reinterpret_cast<const uint4*>(src8 + 64 * i));
+                buf[2 * i] = load16_once(src + 64 * i);
+                buf[2 * i + 1] = load16_once(src8 + 64 * i);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-                buf[2 * i] = row < p.n && c + 64 * i < k ? __ldcs(reinterpret_cast<const uint4*>(src + 64 * i)) : zero;
-                buf[2 * i + 1] = row + 8 < p.n && c + 64 * i < k ? __ldcs(reinterpret_cast<const uint4*>(src8 + 64 * i)) : zero;
+                buf[2 * i] = row < p.n && c + 64 * i < k ? load16_once(src + 64 * i) : zero;
+                buf[2 * i + 1] = row + 8 < p.n && c + 64 * i < k ? load16_once(src8 + 64 * i) : zero;
             }
         }
     };
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(cons
     for (uint64_t j = 0; j < mine; ++j) {
         const uint64_t round = blockIdx.x + j * gridDim.x;
         const uint64_t first = round * chans + threadIdx.x % chans;     // the channel of this thread's outputs (chans divides 256)
-        const float sb = first < p.n ? __ldg(p.sb + first) : 0.f, bias = first < p.n && p.bias ? __ldg(p.bias + first) : 0.f;
+        const float sb = first < p.n ? load_f32(p.sb + first) : 0.f, bias = first < p.n && p.bias ? load_f32(p.bias + first) : 0.f;
         int acc[4][4] = {};
         for (uint32_t step = 0; step < steps; ++step) {
             uint4 w[8];
@@ -284,7 +284,7 @@ struct ColumnScale {
 };
 __device__ __forceinline__ ColumnScale column_scale(const Product8& p, uint64_t col) {
     const bool in = col < p.n;
-    return {in ? __ldg(p.sb + col) : 0.f, in && p.bias ? __ldg(p.bias + col) : 0.f};
+    return {in ? load_f32(p.sb + col) : 0.f, in && p.bias ? load_f32(p.bias + col) : 0.f};
 }
 
 // Scales W columns of a warp's 32 rows and writes them out through the warp's 2 KB of staging.  ok = false: NaN.
@@ -500,7 +500,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                 const uint32_t acc = n_acc & 1u, use = n_acc >> 1;
                 const Product8& p = args.p[DUAL ? walk.cur : 0];
                 const uint64_t row0 = (uint64_t)walk.tm * kPairTile + row_in, col0 = (uint64_t)walk.tn * kPairTile + group * 64;
-                const float sa = row0 + lane < p.m ? __ldg(p.sa + row0 + lane) : 0.f;
+                const float sa = row0 + lane < p.m ? load_f32(p.sa + row0 + lane) : 0.f;
                 const ColumnScale cs[2] = {column_scale(p, col0 + lane), column_scale(p, col0 + 32 + lane)};
                 if (ok && !mbar_wait(acc_full + 8 * acc, use & 1u)) ok = false;
                 ok = __all_sync(kFullMask, ok && !sh_failed);
@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         float sa = 0.f;
         ColumnScale cs = {};
         if (warp < 16) {
-            if (row0 + lane < p.m) sa = __ldg(p.sa + row0 + lane);
+            if (row0 + lane < p.m) sa = load_f32(p.sa + row0 + lane);
             if (own) cs = column_scale(p, col0 + lane);
             ok = mbar_wait(acc_full, 0);
             umma_fence_after();
@@ -696,14 +696,14 @@ __global__ void __launch_bounds__(kSlimThreads)
     }
     float sb = 0.f, bias = 0.f;
     if (warp < 4 && chan < p.n) {
-        sb = __ldg(p.sb + chan);
-        if (p.bias) bias = __ldg(p.bias + chan);
+        sb = load_f32(p.sb + chan);
+        if (p.bias) bias = load_f32(p.bias + chan);
     }
     T* out = static_cast<T*>(p.out);
     const auto put = [&](uint32_t c, int acc, bool good) {
         const uint64_t tok = tok0 + c;
         if (chan < p.n && tok < p.m)
-            out[tok * p.ldo + chan] = from_f32<T>(good ? scaled(acc, __ldg(p.sa + tok), sb, p.bias, bias) : CUDART_NAN_F);
+            out[tok * p.ldo + chan] = from_f32<T>(good ? scaled(acc, load_f32(p.sa + tok), sb, p.bias, bias) : CUDART_NAN_F);
     };
     if (split == 1) {
         if (warp < 4) {

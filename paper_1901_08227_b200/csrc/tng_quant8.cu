@@ -12,8 +12,8 @@ namespace {
 // longer rows (above 1024 threads' worth) are read twice.
 template <typename T> constexpr int kHold = 16 / (int)sizeof(T);       // groups of eight elements
 template <typename T, bool VEC, bool DRAW>
-__global__ void quant8_rows_kernel(const T* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ldx, int8_t* __restrict__ q,
-                                   uint64_t ldq, float* __restrict__ scale, const __grid_constant__ DrawArgs draw) {
+__global__ void quant8_rows_kernel(const T* x, uint64_t rows, uint64_t cols, uint64_t ldx, int8_t* q,
+                                   uint64_t ldq, float* scale, const __grid_constant__ DrawArgs draw) {
     __shared__ uint32_t part[32];
     grid_wait();
     grid_go();
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(256, DRAW ? (ROWS ? 2 : 3) : (ROWS ? 3 : 4)) q
     bool bad = false;                                      // a column with a NaN or infinity: rare, its codes are zero
     if (threadIdx.x < kColTile) {
         const uint64_t col = c0 + threadIdx.x;
-        const uint32_t top = col < cols ? __ldg(job.tops + col) : 0u;
+        const uint32_t top = col < cols ? load4_bits(job.tops + col) : 0u;
         const LineScale s = line_scale(top);
         bad = top >= kInfBits;
         sh_inv[threadIdx.x] = s.inv;
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(256, DRAW ? (ROWS ? 2 : 3) : (ROWS ? 3 : 4)) q
     if (rows_too) {
         static_assert(kRowsPerCta == 256, "a thread a row");
         const uint64_t r = first + threadIdx.x;
-        const uint32_t top = r < last ? __ldg(job.row_tops + r) : 0u;
+        const uint32_t top = r < last ? load4_bits(job.row_tops + r) : 0u;
         const LineScale s = line_scale(top);
         bad = bad || top >= kInfBits;
         sh_row_inv[threadIdx.x] = s.inv;
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(256, DRAW ? (ROWS ? 2 : 3) : (ROWS ? 3 : 4)) q
         float a = 0.f;
         if (c0 + lc < cols) {
 #pragma unroll 8
-            for (uint32_t k = job.chunks * quarter / 4; k < job.chunks * (quarter + 1) / 4; ++k) a += __ldg(job.sums + (uint64_t)k * cols + c0 + lc);
+            for (uint32_t k = job.chunks * quarter / 4; k < job.chunks * (quarter + 1) / 4; ++k) a += load_f32(job.sums + (uint64_t)k * cols + c0 + lc);
         }
         sh_sum[quarter][lc] = a;
     }
