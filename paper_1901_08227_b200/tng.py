@@ -421,9 +421,9 @@ _DTYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _device = torch._C._cuda_getDevice
 
 
-def _matrix(t, name, dtype=None, shape=None):
-    """A 2-D CUDA tensor of the current device with unit column stride -> (pointer, row stride)."""
-    if t.get_device() != _device() or (t.dtype not in _DTYPE if dtype is None else t.dtype != dtype):
+def _matrix(t, name, dtype=None, shape=None, dev=None):
+    """A 2-D CUDA tensor of the current device (dev) with unit column stride -> (pointer, row stride)."""
+    if t.get_device() != (_device() if dev is None else dev) or (t.dtype not in _DTYPE if dtype is None else t.dtype != dtype):
         raise TypeError(f"{name} must be a tensor on the current CUDA device of type {dtype or 'float32, bfloat16 or float16'}")
     size = t.shape
     if len(size) != 2 or (shape is not None and size != shape):
@@ -435,15 +435,15 @@ def _matrix(t, name, dtype=None, shape=None):
     return t.data_ptr(), ld if rows > 1 or ld > cols else cols
 
 
-def _codes(t, name, shape=None):
-    p, ld = _matrix(t, name, torch.int8, shape)
+def _codes(t, name, shape=None, dev=None):
+    p, ld = _matrix(t, name, torch.int8, shape, dev)
     return p, ld if ld % 16 == 0 or t.shape[0] > 1 else -(-ld // 16) * 16
 
 
-def _vector(t, name, n):
+def _vector(t, name, n, dev=None):
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.get_device() != _device() or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+    if t.dtype != torch.float32 or t.get_device() != (_device() if dev is None else dev) or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
         raise TypeError(f"{name} must be a contiguous float32 vector of {n} elements on the current CUDA device")
     return t.data_ptr()
 
@@ -518,18 +518,22 @@ def product8(a, sa, b, sb, bias=None, dtype=torch.bfloat16, out=None):
 def linear8(x, w, sw, bias=None, out=None, scratch=None):
     """y = x W^T + bias with x (tokens, k) coded by token in the call and W held as codes (n, k) with a
     scale per output channel (`quant8_rows` of W).  y has x's type."""
-    px, ldx = _matrix(x, "x")
+    dev = _device()
+    px, ldx = _matrix(x, "x", None, None, dev)
     tokens, k = x.shape
     n = w.shape[0]
-    pw, ldw = _codes(w, "w", (n, k))
+    pw, ldw = _codes(w, "w", (n, k), dev)
     if out is None:
         out = x.new_empty((tokens, n))
         po, ldo = out.data_ptr(), n
     else:
-        po, ldo = _matrix(out, "out", x.dtype, (tokens, n))
-    ps, _keep = _scratch(scratch, _linear8_scratch(tokens, k), x)
-    _check(lib().tng_linear8(px, _DTYPE[x.dtype], tokens, k, ldx, pw, ldw, _vector(sw, "sw", n), n, _vector(bias, "bias", n), po, ldo,
-                             ps, _stream()), "tng_linear8")
+        po, ldo = _matrix(out, "out", x.dtype, (tokens, n), dev)
+    nbytes = _linear8_scratch(tokens, k)
+    ps, _keep = _scratch(scratch, nbytes, x) if nbytes else (None, None)
+    status = lib().tng_linear8(px, _DTYPE[x.dtype], tokens, k, ldx, pw, ldw, _vector(sw, "sw", n, dev), n, _vector(bias, "bias", n, dev), po, ldo,
+                               ps, torch._C._cuda_getCurrentRawStream(dev))
+    if status:
+        raise TngError(status, "tng_linear8")
     return out
 
 
@@ -537,36 +541,47 @@ def linear8_grad(dy, x, wt, swt, draw=None, dx=None, dw=None, db=None, scratch=N
     """Gradients of y = x W^T + bias: (dx, dw, db) from dy (tokens, n) and x (tokens, k).  `wt` (k, n) and
     `swt` (k) hold W by column (`quant8_cols` of W); with `draw` dy is rounded stochastically.  `dw` may be a
     strided float32 view, such as a part of a worker's row of gradients."""
-    py, ldy = _matrix(dy, "dy")
+    dev = _device()
+    py, ldy = _matrix(dy, "dy", None, None, dev)
     tokens, n = dy.shape
     k = x.shape[1]
-    px, ldx = _matrix(x, "x", dy.dtype, (tokens, k))
-    pw, ldw = _codes(wt, "wt", (k, n))
+    px, ldx = _matrix(x, "x", dy.dtype, (tokens, k), dev)
+    pw, ldw = _codes(wt, "wt", (k, n), dev)
     if dx is None:
-        dx = torch.empty_like(x) if x.is_contiguous() else x.new_empty((tokens, k))
+        dx = dy.new_empty((tokens, k))
+        pdx, lddx = dx.data_ptr(), k
+    else:
+        pdx, lddx = _matrix(dx, "dx", dy.dtype, (tokens, k), dev)
     if dw is None:
         dw = dy.new_empty((n, k), dtype=torch.float32)
+        pdw, lddw = dw.data_ptr(), k
+    else:
+        pdw, lddw = _matrix(dw, "dw", torch.float32, (n, k), dev)
     if db is None:
         db = dy.new_empty(n, dtype=torch.float32)
-    pdx, lddx = _matrix(dx, "dx", dy.dtype, (tokens, k))
-    pdw, lddw = _matrix(dw, "dw", torch.float32, (n, k))
+        pdb = db.data_ptr()
+    else:
+        pdb = _vector(db, "db", n, dev)
     ps, _keep = _scratch(scratch, _linear8_grad_scratch(tokens, k, n), dy)
-    _check(lib().tng_linear8_grad(py, ldy, px, ldx, _DTYPE[dy.dtype], tokens, k, n, pw, ldw, _vector(swt, "swt", k), draw,
-                                  pdx, lddx, pdw, lddw, _vector(db, "db", n), ps, _stream()), "tng_linear8_grad")
+    _check(lib().tng_linear8_grad(py, ldy, px, ldx, _DTYPE[dy.dtype], tokens, k, n, pw, ldw, _vector(swt, "swt", k, dev), draw,
+                                  pdx, lddx, pdw, lddw, pdb, ps, torch._C._cuda_getCurrentRawStream(dev)), "tng_linear8_grad")
     return dx, dw, db
 
 
 def dropout(x, p, draw, residual=None, out=None):
     """residual + dropout(x): kept elements are scaled by 1/(1-p); the mask follows from `draw` alone."""
-    px, ldx = _matrix(x, "x")
+    dev = _device()
+    px, ldx = _matrix(x, "x", None, None, dev)
     rows, cols = x.shape
     if out is None:
         out = torch.empty_like(x)
         po, ldo = out.data_ptr(), cols if rows == 1 else out.stride(0)
     else:
-        po, ldo = _matrix(out, "out", x.dtype, x.shape)
-    pr, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, x.shape)
-    _check(lib().tng_dropout(px, _DTYPE[x.dtype], rows, cols, ldx, pr, ldr, p, draw, po, ldo, _stream()), "tng_dropout")
+        po, ldo = _matrix(out, "out", x.dtype, x.shape, dev)
+    pr, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, x.shape, dev)
+    status = lib().tng_dropout(px, _DTYPE[x.dtype], rows, cols, ldx, pr, ldr, p, draw, po, ldo, torch._C._cuda_getCurrentRawStream(dev))
+    if status:
+        raise TngError(status, "tng_dropout")
     return out
 
 
