@@ -17,18 +17,18 @@ __device__ __forceinline__ float scaled(int acc, float sa, float sb, bool has_bi
     return has_bias ? __fadd_rn(v, bias) : v;
 }
 
-// ---- at most 8 tokens: the weights are streamed past them ------------------------------------------------
-// Bound by reading b once.  The tokens' codes stay in shared memory; a CTA goes over tiles of sixteen rows of b, KS warps
+// ---- a linear layer of at most 8 tokens in one launch: the weights are streamed past them -------------------
+// Bound by reading b once (1 x 4096 x 4096 bf16 6.3 us, 8 x 16384 x 2048 11.2 us, launches included).  Every CTA codes the
+// tokens itself while its first weights travel, one group of registers a thread: at most 16384 elements with the tokens
+// counted as a power of two.  (Codes by a launch of their own and the tensor-memory kernel below: 7.6 and 10.5 us, and
+// 3.5 us more of the host's time; 8 x 512 x 512 3.5 us against 5.5.)  The tokens' codes stay in shared memory; a CTA goes over tiles of sixteen rows of b, KS warps
 // sharing a tile along the contraction, 256 codes a warp and step: a lane has every fourth 16 bytes of two rows, eight
 // loads of them, the next step's issued before this one's are used.  A warp-wide m16n8k32 instruction takes the weights as
 // its 16 rows straight from the loaded words and the tokens as its 8 columns: the contraction may run in any order as
 // long as both sides agree, so a lane's 16 consecutive codes serve as its words of two instructions.  These instructions are
 // slow here (270 cycles where one waits for another, hence four chains; byte products on the integer pipe took 7 cycles
-// each, three times as long at 8 tokens), but they keep up with memory; the tensor-memory kernel below needs its operands in
-// shared memory, and its set-up and barriers cost 5 us.
-// X = int8_t: codes with scales; a floating type: the CTA codes the tokens itself, while its first weights travel.
+// each, three times as long at 8 tokens), but they keep up with memory.
 constexpr int kStreamThreads = 256, kStreamTokens = 8, kStreamHold = 8;
-constexpr uint32_t kStreamSmem = 96 * 1024;
 __host__ __device__ inline uint32_t stream_pitch(uint64_t k) { return (uint32_t)((k + 255) / 256 * 256 + 64); }   // 64 mod 128: no bank conflicts
 // Threads a token while its line is coded: all 256 over the tokens' next power of two.
 __host__ __device__ inline uint32_t stream_share(uint64_t tokens) { return kStreamThreads / (tokens > 4 ? 8 : tokens > 2 ? 4 : tokens > 1 ? 2 : 1); }
@@ -40,73 +40,50 @@ __device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, ui
 
 // The tokens' codes and scales into shared memory, zero up to the pitch.
 template <typename X>
-__device__ __forceinline__ void stream_tokens(const X* x, uint64_t ldx, const float* sa, uint32_t tokens, uint32_t k, int8_t* codes, uint32_t pitch,
+__device__ __forceinline__ void stream_tokens(const X* x, uint64_t ldx, uint32_t tokens, uint32_t k, int8_t* codes, uint32_t pitch,
                                               float* scales, uint32_t* part) {
     const uint32_t groups = (k + 7) / 8, all = pitch / 8;
-    if constexpr (sizeof(X) == 1) {
-        const uint32_t per = pitch / 16, total = tokens * per;
-        for (uint32_t i0 = threadIdx.x; i0 < total; i0 += 8 * kStreamThreads) {
-            uint4 w[8];
+    // (at most kStreamHold groups of eight a thread: all loads at once)
+    const uint32_t share = stream_share(tokens), t = threadIdx.x / share, lane = threadIdx.x & (share - 1);
+    const X* row = x + (uint64_t)(t < tokens ? t : 0) * ldx;
+    const bool vec = aligned16(row) && k % 8 == 0;
+    Raw8<X> v[kStreamHold];
+    uint32_t m = 0;
+    if (vec) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t i = i0 + j * kStreamThreads, t = i / per, g = i - t * per;
-                w[j] = i < total && g * 16 < k ? load16(reinterpret_cast<const uint4*>(x + (uint64_t)t * ldx) + g) : make_uint4(0u, 0u, 0u, 0u);
-            }
+        for (int h = 0; h < kStreamHold; ++h) v[h] = lane + h * share < groups ? load_raw8(row + (lane + h * share) * 8) : zero_raw8<X>();
+    } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t i = i0 + j * kStreamThreads, t = i / per, g = i - t * per;
-                if (i >= total) break;
-                if (g * 16 + 16 > k) {                      // what follows a line does not count
-                    const uint32_t n = g * 16 < k ? k - g * 16 : 0;
-                    const auto cut = [n](uint32_t v, uint32_t first) { return n >= first + 4 ? v : n <= first ? 0u : v & ((1u << (8 * (n - first))) - 1u); };
-                    w[j] = make_uint4(cut(w[j].x, 0), cut(w[j].y, 4), cut(w[j].z, 8), cut(w[j].w, 12));
-                }
-                reinterpret_cast<uint4*>(codes)[i] = w[j];
-            }
+        for (int h = 0; h < kStreamHold; ++h)
+            v[h] = lane + h * share < groups ? fetch_raw8<X, false>(row, (lane + h * share) * 8, k) : zero_raw8<X>();
+    }
+#pragma unroll
+    for (int h = 0; h < kStreamHold; ++h) m = top_raw8<X>(v[h], m);
+    m = __reduce_max_sync(kFullMask, top_bits<X>(top_of_halves<X>(m)));
+    if (share > 32) {
+        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
+        __syncthreads();
+        const uint32_t w = share >> 5;
+        for (uint32_t i = 0; i < w; ++i) m = max(m, part[t * w + i]);
+    }
+    if (t < tokens) {
+        const LineScale s = line_scale(m);
+        if (lane == 0) scales[t] = s.scale;
+        uint2* dst = reinterpret_cast<uint2*>(codes + t * pitch);
+#pragma unroll
+        for (int h = 0; h < kStreamHold; ++h) {
+            const uint32_t g = lane + h * share;
+            if (g >= all) break;
+            float f[8];
+            widen8(v[h], f);
+            dst[g] = code8<false>(f, s.inv, DrawArgs{}, DrawRow{}, 0);
         }
-        if (threadIdx.x < tokens) scales[threadIdx.x] = load_f32(sa + threadIdx.x);
-    } else {                                                // (at most kStreamHold groups of eight a thread: all loads at once)
-        const uint32_t share = stream_share(tokens), t = threadIdx.x / share, lane = threadIdx.x & (share - 1);
-        const X* row = x + (uint64_t)(t < tokens ? t : 0) * ldx;
-        const bool vec = aligned16(row) && k % 8 == 0;
-        Raw8<X> v[kStreamHold];
-        uint32_t m = 0;
-        if (vec) {
-#pragma unroll
-            for (int h = 0; h < kStreamHold; ++h) v[h] = lane + h * share < groups ? load_raw8(row + (lane + h * share) * 8) : zero_raw8<X>();
-        } else {
-#pragma unroll
-            for (int h = 0; h < kStreamHold; ++h)
-                v[h] = lane + h * share < groups ? fetch_raw8<X, false>(row, (lane + h * share) * 8, k) : zero_raw8<X>();
-        }
-#pragma unroll
-        for (int h = 0; h < kStreamHold; ++h) m = top_raw8<X>(v[h], m);
-        m = __reduce_max_sync(kFullMask, top_bits<X>(top_of_halves<X>(m)));
-        if (share > 32) {
-            if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
-            __syncthreads();
-            const uint32_t w = share >> 5;
-            for (uint32_t i = 0; i < w; ++i) m = max(m, part[t * w + i]);
-        }
-        if (t < tokens) {
-            const LineScale s = line_scale(m);
-            if (lane == 0) scales[t] = s.scale;
-            uint2* dst = reinterpret_cast<uint2*>(codes + t * pitch);
-#pragma unroll
-            for (int h = 0; h < kStreamHold; ++h) {
-                const uint32_t g = lane + h * share;
-                if (g >= all) break;
-                float f[8];
-                widen8(v[h], f);
-                dst[g] = code8<false>(f, s.inv, DrawArgs{}, DrawRow{}, 0);
-            }
-            for (uint32_t g = lane + kStreamHold * share; g < all; g += share) dst[g] = make_uint2(0u, 0u);
-        }
+        for (uint32_t g = lane + kStreamHold * share; g < all; g += share) dst[g] = make_uint2(0u, 0u);
     }
 }
 
-template <typename X, typename T>
-__global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(const X* x, uint64_t ldx, const __grid_constant__ Product8 p) {
+template <typename T>
+__global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(const T* x, uint64_t ldx, const __grid_constant__ Product8 p) {
     extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ float scales[kStreamTokens];
     __shared__ uint32_t part[8];
@@ -143,7 +120,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(cons
     grid_wait();
     grid_go();
     if (mine) load(blockIdx.x, 0);
-    stream_tokens<X>(x, ldx, p.sa, tokens, k, codes, pitch, scales, part);
+    stream_tokens<T>(x, ldx, tokens, k, codes, pitch, scales, part);
     __syncthreads();
 
     T* out = static_cast<T*>(p.out);
@@ -188,7 +165,8 @@ __global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(cons
 
 // ---- pairs of CTAs: 256 x 256 outputs a tile ------------------------------------------------------------
 // Two CTAs (two SMs) work on one tile: each holds 128 rows of a and 128 rows of b per stage, and the matrix
-// instruction of the even CTA reads both shared memories; the accumulators are 128 rows x 256 columns in each
+// instruction of the even CTA reads both shared memories (8192^3, bf16 out: 334 us, 3290 TOP/s, the tensor pipe 89% busy;
+// 390 us once the power limit holds the clock); the accumulators are 128 rows x 256 columns in each
 // CTA's tensor memory, twice, so that one tile is written out while the next is summed.  A stage of 128 codes
 // takes 513 cycles where the instruction rate allows 512 (measured with the feed running); 256 x 128 tiles take 470
 // for half the work, so small outputs split the contraction instead of the tile:
@@ -600,12 +578,15 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 // The 128 rows are rows of b, the NT columns rows of a (tokens): with few tokens the weights are the long side, and an
 // output row then runs along the lanes.  The CTAs of a cluster take consecutive parts of the contraction, leave
 // their int32 sums in shared memory and each write out a part of the columns, summed over the cluster's shared
-// memories.  Warps: 0-3 write out, 4 feeds, 5 issues.
+// memories.  Bound by the weights' traffic and 3.5 us of launch, set-up and last meeting: 8 x 16384 x 2048 8.6 us (3.9 TB/s).
+// Warps: 0-3 write out, 4 feeds, 5 issues.
 constexpr int kSlimThreads = 192;
-constexpr uint64_t kSlimRows = 128;                        // rows of a up to which this kernel is taken
+// Rows of a up to which this kernel is taken.  64 x 4096 x 4096: 8.0 us, the pairs 10.8; 64 x 16384 x 2048: 12.8 and 10.9;
+// 100 rows: 10.2 and 10.9, 16.7 and 11.4.
+constexpr uint64_t kSlimRows = 64;
 template <int NT> struct SlimGeom {
     static constexpr uint32_t kA = 128 * 128, kB = NT * 128, kStage = kA + kB;
-    static constexpr uint32_t kStages = NT == 128 ? 3 : 4;
+    static constexpr uint32_t kStages = 4;
     static constexpr uint32_t kColumns = NT < 32 ? 32 : NT;
     static constexpr uint32_t kSmem = 1024 + kStages * kStage + 256;
     static_assert(kStages * kStage >= 128 * NT * 4, "the stages also hold the sums");
@@ -614,10 +595,11 @@ template <int NT> struct SlimGeom {
 template <int NT, typename T>
 __global__ void __launch_bounds__(kSlimThreads)
     product8_slim_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ Product8 p,
-                         uint32_t split, uint32_t tiles_n) {
+                         uint32_t split) {
     using G = SlimGeom<NT>;
     extern __shared__ unsigned char dyn[];
     __shared__ uint32_t sh_tmem;
+    __shared__ float sh_sa[NT];
     __shared__ volatile uint32_t sh_failed;
     const uint32_t data = (smem_u32(dyn) + 1023u) & ~1023u;
     int4* sums = reinterpret_cast<int4*>(dyn + (data - smem_u32(dyn)));     // [four columns][row]: a warp's access is contiguous
@@ -626,8 +608,7 @@ __global__ void __launch_bounds__(kSlimThreads)
     const auto empty = [&](uint32_t s) { return bars + 16u * s + 8u; };
     const uint32_t acc_full = bars + 16u * G::kStages, drain = acc_full + 8u;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t part = blockIdx.x % split, tile = blockIdx.x / split;
-    const uint32_t tm = tile / tiles_n, tn = tile - tm * tiles_n;
+    const uint32_t part = blockIdx.x % split, tn = blockIdx.x / split;
     const uint32_t kblocks = (uint32_t)((p.k + 127) / 128);
     const uint32_t kb0 = (uint32_t)((uint64_t)kblocks * part / split), kb1 = (uint32_t)((uint64_t)kblocks * (part + 1) / split);
     const uint32_t n = kb1 - kb0;
@@ -651,7 +632,7 @@ __global__ void __launch_bounds__(kSlimThreads)
     grid_go();
 
     if (warp == 4 && lane == 0) {
-        const int32_t yb = (int32_t)(tn * 128), ya = (int32_t)(tm * NT);
+        const int32_t yb = (int32_t)(tn * 128);
         uint32_t i = 0;
         for (; i < n; ++i) {
             const uint32_t s = i % G::kStages, use = i / G::kStages;
@@ -659,7 +640,7 @@ __global__ void __launch_bounds__(kSlimThreads)
             mbar_expect_tx(full(s), G::kStage);
             const uint32_t dst = data + s * G::kStage;
             tile_load<1>(dst, &map_b, (int32_t)((kb0 + i) * 128), yb, full(s));
-            tile_load<1>(dst + G::kA, &map_a, (int32_t)((kb0 + i) * 128), ya, full(s));
+            tile_load<1>(dst + G::kA, &map_a, (int32_t)((kb0 + i) * 128), 0, full(s));
         }
         for (uint32_t j = i > G::kStages ? i - G::kStages : 0; j < i; ++j) (void)mbar_wait(full(j % G::kStages), (j / G::kStages) & 1u);
     } else if (warp == 5 && lane == 0) {
@@ -689,21 +670,21 @@ __global__ void __launch_bounds__(kSlimThreads)
 
     bool ok = true;
     const uint64_t chan = (uint64_t)tn * 128 + warp * 32 + lane;
-    const uint64_t tok0 = (uint64_t)tm * NT;
-    if (warp < 4) {
+    float sb = 0.f, bias = 0.f;
+    if (warp < 4) {                                        // scales ahead of the sums: a load between two stores costs its whole latency
+        if (threadIdx.x < NT) sh_sa[threadIdx.x] = threadIdx.x < p.m ? load_f32(p.sa + threadIdx.x) : 0.f;
+        if (chan < p.n) {
+            sb = load_f32(p.sb + chan);
+            if (p.bias) bias = load_f32(p.bias + chan);
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
         ok = mbar_wait(acc_full, 0);
         umma_fence_after();
     }
-    float sb = 0.f, bias = 0.f;
-    if (warp < 4 && chan < p.n) {
-        sb = load_f32(p.sb + chan);
-        if (p.bias) bias = load_f32(p.bias + chan);
-    }
     T* out = static_cast<T*>(p.out);
     const auto put = [&](uint32_t c, int acc, bool good) {
-        const uint64_t tok = tok0 + c;
-        if (chan < p.n && tok < p.m)
-            out[tok * p.ldo + chan] = from_f32<T>(good ? scaled(acc, load_f32(p.sa + tok), sb, p.bias, bias) : CUDART_NAN_F);
+        if (chan < p.n && c < p.m)
+            out[c * p.ldo + chan] = from_f32<T>(good ? scaled(acc, sh_sa[c], sb, p.bias, bias) : CUDART_NAN_F);
     };
     if (split == 1) {
         if (warp < 4) {
@@ -711,7 +692,7 @@ __global__ void __launch_bounds__(kSlimThreads)
 #pragma unroll 1
             for (uint32_t c = 0; c < NT; c += 16) {
                 uint32_t r[16];
-                if (tok0 + c >= p.m) break;
+                if (c >= p.m) break;
                 tmem_ld16(tmem + ((warp * 32) << 16) + c, r);
                 tmem_wait_ld();
 #pragma unroll
@@ -740,7 +721,7 @@ __global__ void __launch_bounds__(kSlimThreads)
             const uint32_t cols = NT / split < 4 ? 4 : NT / split, c0 = cols * part;
             const uint32_t at = data + (warp * 32 + lane) * 16;
 #pragma unroll 1
-            for (uint32_t c = c0; c < c0 + cols && c < NT && tok0 + c < p.m; c += 4) {
+            for (uint32_t c = c0; c < c0 + cols && c < NT && c < p.m; c += 4) {
                 int4 v[8];
 #pragma unroll
                 for (uint32_t q = 0; q < 8; ++q) v[q] = q < split ? cluster_ld4(cluster_map(at + c / 4 * 2048, q)) : make_int4(0, 0, 0, 0);
@@ -880,33 +861,22 @@ template <int NT, typename T> cudaError_t launch_slim(const Product8& p, uint32_
     if (e != cudaSuccess) return e;
     CUtensorMap ma, mb;
     if (!make_map(&mb, p.b, p.n, p.k, p.ldb, 128) || !make_map(&ma, p.a, p.m, p.k, p.lda, NT)) return cudaErrorNotSupported;
-    const uint32_t tiles_n = (uint32_t)((p.n + 127) / 128);
-    const uint64_t ctas = (p.m + NT - 1) / NT * tiles_n * split;
+    const uint64_t ctas = (p.n + 127) / 128 * split;
     if (ctas >= (1ull << 31)) return cudaErrorInvalidValue;
-    return launch_layer(kernel, (unsigned)ctas, kSlimThreads, G::kSmem, split, st, mb, ma, p, split, tiles_n);
-}
-
-template <typename X, typename T> cudaError_t launch_stream(const X* x, uint64_t ldx, const Product8& p, cudaStream_t st) {
-    static PerDevice<bool> done;
-    const auto kernel = product8_stream_kernel<X, T>;
-    const cudaError_t e = allow_smem(kernel, kStreamSmem, done);
-    if (e != cudaSuccess) return e;
-    const uint64_t kparts = (p.k + 255) / 256, ks = kparts >= 5 ? 8 : kparts >= 3 ? 4 : kparts;
-    const uint64_t rounds = ((p.n + 15) / 16 * ks + 7) / 8, most = 2ull * sm_count_now();
-    return launch_layer(kernel, (unsigned)(rounds < most ? rounds : most), kStreamThreads, p.m * stream_pitch(p.k), 1, st, x, ldx, p);
+    return launch_layer(kernel, (unsigned)ctas, kSlimThreads, G::kSmem, split, st, mb, ma, p, split);
 }
 
 }  // namespace
 
-// The codes of the tokens have to fit beside another CTA's; coding them in every CTA pays as long as their lines fit its
-// registers (8 x 2048: 1 us, against a launch of its own).
-bool product8_streams(uint64_t tokens, uint64_t k) { return tokens <= kStreamTokens && tokens * stream_pitch(k) <= kStreamSmem; }
-bool product8_codes_tokens(uint64_t tokens, uint64_t k) { return product8_streams(tokens, k) && k <= 8ull * kStreamHold * stream_share(tokens); }
+bool product8_codes_tokens(uint64_t tokens, uint64_t k) { return tokens <= kStreamTokens && k <= 8ull * kStreamHold * stream_share(tokens); }
 
 cudaError_t launch_linear8_stream(const void* x, uint64_t ldx, const Product8& p, cudaStream_t st) {
     return with_type(p.type, [&](auto t) {
         using T = decltype(t);
-        return launch_stream<T, T>(static_cast<const T*>(x), ldx, p, st);
+        const uint64_t kparts = (p.k + 255) / 256, ks = kparts >= 5 ? 8 : kparts >= 3 ? 4 : kparts;
+        const uint64_t rounds = ((p.n + 15) / 16 * ks + 7) / 8, most = 2ull * sm_count_now();
+        return launch_layer(product8_stream_kernel<T>, (unsigned)(rounds < most ? rounds : most), kStreamThreads, p.m * stream_pitch(p.k), 1, st,
+                            static_cast<const T*>(x), ldx, p);
     });
 }
 
@@ -914,16 +884,14 @@ cudaError_t launch_product8(const Product8& p, cudaStream_t st) {
     const uint64_t sms = (uint64_t)sm_count_now(), kblocks = (p.k + 127) / 128;
     return with_type(p.type, [&](auto t) {
         using T = decltype(t);
-        if (product8_streams(p.m, p.k)) return launch_stream<int8_t, T>(p.a, p.lda, p, st);
         if (p.m <= kSlimRows) {
-            const uint64_t nt = p.m <= 16 ? 16 : p.m <= 32 ? 32 : p.m <= 64 ? 64 : 128;
-            const uint64_t tiles = (p.n + 127) / 128 * ((p.m + nt - 1) / nt);
+            const uint64_t nt = p.m <= 16 ? 16 : p.m <= 32 ? 32 : 64;
+            const uint64_t tiles = (p.n + 127) / 128;
             uint32_t split = 1;
             while (split < 8 && tiles * split * 2 <= sms && kblocks >= split * 4) split *= 2;
             if (nt == 16) return launch_slim<16, T>(p, split, st);
             if (nt == 32) return launch_slim<32, T>(p, split, st);
-            if (nt == 64) return launch_slim<64, T>(p, split, st);
-            return launch_slim<128, T>(p, split, st);
+            return launch_slim<64, T>(p, split, st);
         }
         const uint32_t split = pair_split<T>(p);
         return launch_pair<T>(p, split, st);
