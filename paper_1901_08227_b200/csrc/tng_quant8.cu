@@ -217,9 +217,15 @@ __global__ void __launch_bounds__(256, DRAW ? (ROWS ? 2 : 3) : (ROWS ? 3 : 4)) q
     if (slab == 0 && job.colsum) {                         // the chunks' sums: a quarter to a thread, the quarters in order
         const uint32_t lc = threadIdx.x & 63, quarter = threadIdx.x >> 6;
         float a = 0.f;
-        if (c0 + lc < cols) {
-#pragma unroll 8
-            for (uint32_t k = job.chunks * quarter / 4; k < job.chunks * (quarter + 1) / 4; ++k) a += load_f32(job.sums + (uint64_t)k * cols + c0 + lc);
+        if (c0 + lc < cols) {                              // eight loads under way at a time
+            const uint32_t k0 = job.chunks * quarter / 4, k1 = job.chunks * (quarter + 1) / 4;
+            for (uint32_t k = k0; k < k1; k += 8) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = load_f32(job.sums + (uint64_t)(k + i < k1 ? k + i : k1 - 1) * cols + c0 + lc);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) a += k + i < k1 ? v[i] : 0.f;
+            }
         }
         sh_sum[quarter][lc] = a;
     }
