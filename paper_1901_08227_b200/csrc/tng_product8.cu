@@ -427,9 +427,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             sh_failed = 1;
             for (int i = 0; i < 1000; ++i) __nanosleep(1000);
         }
-        // no CTA of the pair may leave before its copies have landed
-        if (rank == 0)
-            for (uint32_t j = it > kPairStages ? it - kPairStages : 0; j < it; ++j) (void)mbar_wait(full(j % kPairStages), (j / kPairStages) & 1u);
+        // no CTA of the pair may leave before its copies have landed and the last releases of its stages have arrived
+        for (uint32_t j = it > kPairStages ? it - kPairStages : 0; j < it; ++j) {
+            if (rank == 0) (void)mbar_wait(full(j % kPairStages), (j / kPairStages) & 1u);
+            if (ok && !mbar_wait(empty(j % kPairStages), (j / kPairStages) & 1u)) ok = false;
+        }
     } else if (warp == 17 && lane == 0 && rank == 0) {
         // ---- issue
         constexpr uint32_t idesc = umma_idesc_s8(256, kPairTile);
@@ -461,9 +463,12 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
         if (!ok) {
             sh_failed = 1;
-            umma_commit_pair(drain, both);
+            umma_commit_pair(drain, (uint16_t)(1u << even));
             (void)mbar_wait(drain, 0);
         }
+        // the hand-backs that no further tile waits for come from the other CTA too: they arrive before this one may leave
+        if (!SPLIT)
+            for (uint32_t j = n_acc > 2 ? n_acc - 2 : 0; j < n_acc; ++j) (void)mbar_wait(acc_empty + 8 * (j & 1u), (j >> 1) & 1u);
     }
     __syncwarp();
     unsigned char* stage = stages + kPairStages * kPairStage + warp * kStageStride;
@@ -487,7 +492,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                 const auto done = [&] {
                     umma_fence_before();                   // everything read: the next tile may overwrite it
                     __syncwarp();
-                    if (lane == 0) cluster_arrive(cluster_map(acc_empty + 8 * acc, even));
+                    if (lane == 0 && ok) cluster_arrive(cluster_map(acc_empty + 8 * acc, even));   // (a failure hands nothing back)
                 };
                 if (DUAL && walk.cur) finish_columns<float, 16, true>(p, &maps2.o, from, ok, sa, cs, row0, col0, stage, lane, done);
                 else finish_columns<T, kWidth, TILES>(p, &map_o, from, ok, sa, cs, row0, col0, stage, lane, done);
@@ -507,7 +512,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         const Product8& p = args.p[0];
         (void)walk.step<DUAL>();
         const uint64_t row0 = (uint64_t)walk.tm * kPairTile + row_in, col0 = (uint64_t)walk.tn * kPairTile + mine + group * 32;
-        const bool own = group * 32 < cols;                // 32 columns a warp, of one's own
+        const bool own = warp < 16 && group * 32 < cols && row0 < p.m && col0 < p.n;   // 32 columns a warp, of one's own, in the matrix
         float sa = 0.f;
         ColumnScale cs = {};
         if (warp < 16) {
@@ -530,7 +535,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             umma_fence_before();
         }
         cluster_sync_all();
-        if (warp < 16 && own) {
+        uint32_t r[32];
+        if (own) {
             umma_fence_after();
             const uint32_t c = mine + group * 32;
             const auto fetch = [&](uint32_t q, int4 (&v)[8]) {
@@ -541,7 +547,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             int4 v[8];
             fetch(1, v);
             ok = cluster_all_zero(smem_u32((const void*)&sh_failed), 2 * parts);
-            uint32_t r[32];
             tmem_ld32(tmem + ((quad * 32) << 16) + c, r);
             tmem_wait_ld();
 #pragma unroll 1
@@ -555,6 +560,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                 }
                 if (q + 1 < parts) fetch(q + 1, v);
             }
+        }
+        __syncwarp();
+        cluster_arrive_all();                              // done with the others' sums
+        if (own) {
             if constexpr (kWidth == 32) {
                 finish_chunk<T, 32, TILES>(p, &map_o, r, ok, sa, cs, 0, row0, col0, stage, lane);
             } else {
@@ -569,7 +578,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             if (TILES && lane == 0) tile_store_wait_all();
         }
         __syncwarp();
-        cluster_meet_all();                                // nobody leaves while its sums are being read
+        cluster_wait_all();                                // nobody leaves while its sums are being read
     }
     if (warp == 17) tmem_free<2>(tmem, 2 * kPairTile);
 }
@@ -593,7 +602,7 @@ template <int NT> struct SlimGeom {
 };
 
 template <int NT, typename T>
-__global__ void __launch_bounds__(kSlimThreads)
+__global__ void __launch_bounds__(kSlimThreads, 2)
     product8_slim_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ Product8 p,
                          uint32_t split) {
     using G = SlimGeom<NT>;
@@ -642,7 +651,11 @@ __global__ void __launch_bounds__(kSlimThreads)
             tile_load<1>(dst, &map_b, (int32_t)((kb0 + i) * 128), yb, full(s));
             tile_load<1>(dst + G::kA, &map_a, (int32_t)((kb0 + i) * 128), 0, full(s));
         }
-        for (uint32_t j = i > G::kStages ? i - G::kStages : 0; j < i; ++j) (void)mbar_wait(full(j % G::kStages), (j / G::kStages) & 1u);
+        // every copy has landed and every release has arrived before the CTA may leave
+        for (uint32_t j = i > G::kStages ? i - G::kStages : 0; j < i; ++j) {
+            (void)mbar_wait(full(j % G::kStages), (j / G::kStages) & 1u);
+            if (!sh_failed && !mbar_wait(empty(j % G::kStages), (j / G::kStages) & 1u)) sh_failed = 1;
+        }
     } else if (warp == 5 && lane == 0) {
         constexpr uint32_t idesc = umma_idesc_s8(128, NT);
         bool ok = true;
@@ -716,30 +729,45 @@ __global__ void __launch_bounds__(kSlimThreads)
         }
         umma_fence_before();
         cluster_sync_all();                                // every part's sums are in place
-        if (warp < 4) {
-            const bool good = cluster_all_zero(smem_u32((const void*)&sh_failed), split);
-            const uint32_t cols = NT / split < 4 ? 4 : NT / split, c0 = cols * part;
-            const uint32_t at = data + (warp * 32 + lane) * 16;
-#pragma unroll 1
-            for (uint32_t c = c0; c < c0 + cols && c < NT && c < p.m; c += 4) {
+        constexpr uint32_t kMost = NT / 2;                 // columns of a part, of two at least
+        const uint32_t cols = NT / split < 4 ? 4 : NT / split, c0 = cols * part;
+        const uint32_t end = c0 >= p.m ? 0 : p.m - c0 < cols ? (uint32_t)p.m - c0 : cols;
+        const bool mine = warp < 4 && (uint64_t)tn * 128 + warp * 32 < p.n;
+        int4 a[kMost / 4];
+        bool good = false;
+        if (mine) {
+            good = cluster_all_zero(smem_u32((const void*)&sh_failed), split);
+            const uint32_t at = data + (c0 / 4 * 128 + warp * 32 + lane) * 16;
+#pragma unroll
+            for (uint32_t i = 0; i < kMost / 4; ++i) {
+                if (4 * i >= end) break;
                 int4 v[8];
 #pragma unroll
-                for (uint32_t q = 0; q < 8; ++q) v[q] = q < split ? cluster_ld4(cluster_map(at + c / 4 * 2048, q)) : make_int4(0, 0, 0, 0);
-                int4 a = v[0];
+                for (uint32_t q = 0; q < 8; ++q) v[q] = q < split ? cluster_ld4(cluster_map(at + i * 2048, q)) : make_int4(0, 0, 0, 0);
+                a[i] = v[0];
 #pragma unroll
                 for (int q = 1; q < 8; ++q) {
-                    a.x += v[q].x;
-                    a.y += v[q].y;
-                    a.z += v[q].z;
-                    a.w += v[q].w;
+                    a[i].x += v[q].x;
+                    a[i].y += v[q].y;
+                    a[i].z += v[q].z;
+                    a[i].w += v[q].w;
                 }
-                put(c, a.x, good);
-                put(c + 1, a.y, good);
-                put(c + 2, a.z, good);
-                put(c + 3, a.w, good);
             }
         }
-        cluster_meet_all();                                // nobody leaves while its sums are being read
+        __syncwarp();
+        cluster_arrive_all();                              // done with the others' sums
+        if (mine) {
+#pragma unroll
+            for (uint32_t i = 0; i < kMost / 4; ++i) {
+                if (4 * i >= end) break;
+                put(c0 + 4 * i, a[i].x, good);
+                put(c0 + 4 * i + 1, a[i].y, good);
+                put(c0 + 4 * i + 2, a[i].z, good);
+                put(c0 + 4 * i + 3, a[i].w, good);
+            }
+        }
+        __syncwarp();
+        cluster_wait_all();                                // nobody leaves while its sums are being read
     }
     if (warp == 5) tmem_free<1>(tmem, G::kColumns);
 }

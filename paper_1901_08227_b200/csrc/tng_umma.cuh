@@ -117,7 +117,11 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// The same as a mere meeting point: what the threads wrote is not made visible (no wait for their stores).
+// Its two halves: the release orders this thread's accesses, reads of other CTAs' memories among them, before the
+// arrival, so that past the wait nobody's are under way.  (Stores to global memory between the halves are not waited for.)
+__device__ __forceinline__ void cluster_arrive_all() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait_all() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// A mere meeting point: nothing is made visible or waited for (no wait for stores).
 __device__ __forceinline__ void cluster_meet_all() {
     asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
