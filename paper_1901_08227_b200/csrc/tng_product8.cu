@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const uint32_t bars = data + kPairStages * kPairStage + 16 * kStageStride;
     const auto full = [&](uint32_t s) { return bars + 16u * s; };
     const auto empty = [&](uint32_t s) { return bars + 16u * s + 8u; };
-    const uint32_t acc_full = bars + 16u * kPairStages, acc_empty = acc_full + 16u, drain = acc_full + 32u;
+    const uint32_t acc_full = bars + 16u * kPairStages, acc_empty = acc_full + 16u, drain = acc_full + 32u, ready = acc_full + 40u;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, in_cluster = cluster_rank();
     const uint32_t rank = in_cluster & 1u, even = in_cluster & ~1u;            // the pair's CTA that issues
     const uint32_t part = SPLIT ? in_cluster >> 1 : 0, parts = SPLIT ? split : 1;
@@ -393,18 +393,26 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             mbar_init(acc_empty + 8 * i, 32);              // sixteen warps of either CTA
         }
         mbar_init(drain, 1);
+        mbar_init(ready, 1);
         mbar_init_fence();
         map_prefetch(&map_a);
         map_prefetch(&map_b);
     }
-    if (warp == 17) tmem_alloc<2>(smem_u32(&sh_tmem), 2 * kPairTile);
-    umma_fence_before();
-    __syncthreads();
     cluster_sync_all();
-    umma_fence_after();
-    const uint32_t tmem = sh_tmem;
     grid_wait();
-    grid_go();
+    // Tensor memory is taken only now: a launch that held it while it waits could keep the one it waits for (which need not
+    // be this library's) from ever getting its own.  The first copies travel meanwhile.
+    if (warp == 17) {
+        tmem_alloc<2>(smem_u32(&sh_tmem), 2 * kPairTile);
+        if (rank == 1 && lane == 0) cluster_arrive(cluster_map(ready, even));
+    }
+    if (warp != 16) {
+        umma_fence_before();
+        asm volatile("bar.sync 1, 544;" ::: "memory");     // the seventeen warps that use it
+        umma_fence_after();
+        grid_go();
+    }
+    const uint32_t tmem = sh_tmem;
 
     if (warp == 16 && lane == 0) {
         // ---- feed: this CTA's rows of either operand, completion counted on the even CTA's barrier
@@ -437,7 +445,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         constexpr uint32_t idesc = umma_idesc_s8(256, kPairTile);
         const uint16_t both = (uint16_t)(3u << even);
         uint32_t s = 0, parity = 0, n_acc = 0;
-        bool ok = true;
+        bool ok = mbar_wait(ready, 0);                     // the odd CTA has its tensor memory
         for (; ok && walk.step<DUAL>(); ++n_acc) {
             const uint32_t acc = n_acc & 1u, use = n_acc >> 1, blocks = k_last() - k_first(), into = tmem + acc * kPairTile;
             // instructions of the last block: 32 codes each
@@ -632,13 +640,16 @@ __global__ void __launch_bounds__(kSlimThreads, 2)
         mbar_init(drain, 1);
         mbar_init_fence();
     }
-    if (warp == 5) tmem_alloc<1>(smem_u32(&sh_tmem), G::kColumns);
-    umma_fence_before();
     __syncthreads();
-    umma_fence_after();
-    const uint32_t tmem = sh_tmem;
     grid_wait();
-    grid_go();
+    if (warp == 5) tmem_alloc<1>(smem_u32(&sh_tmem), G::kColumns);         // only now: see the pair kernel
+    if (warp != 4) {
+        umma_fence_before();
+        asm volatile("bar.sync 2, 160;" ::: "memory");
+        umma_fence_after();
+        grid_go();
+    }
+    const uint32_t tmem = sh_tmem;
 
     if (warp == 4 && lane == 0) {
         const int32_t yb = (int32_t)(tn * 128);
