@@ -359,7 +359,8 @@ size_t tng_code_stride(uint64_t n);
  * tng_quant8_cols: a line is a column (a scale per channel) and the codes come transposed: q is
  *   cols x rows, so that a product can contract over the rows of x.  colsum (may be NULL) receives
  *   the column sums of x in fp32.  scratch_dev: tng_quant8_cols_scratch_bytes, 256-byte aligned.
- * Bytes between a line's end and the next multiple of 16 are written as zero. */
+ * Bytes between a line's end and the next multiple of 16 are written as zero, the last line's too: q_dev
+ * has to hold them.  (Calls that take codes may read those bytes; what they hold makes no difference.) */
 tng_status tng_quant8_rows(const void* x_dev, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx,
                            const tng_draw* draw, int8_t* q_dev, uint64_t ldq, float* scale_dev, void* stream);
 size_t tng_quant8_cols_scratch_bytes(uint64_t rows, uint64_t cols);

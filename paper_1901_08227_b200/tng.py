@@ -436,8 +436,19 @@ def _matrix(t, name, dtype=None, shape=None, dev=None):
 
 
 def _codes(t, name, shape=None, dev=None):
+    """Codes to be read.  (What follows a line's end may be read up to the next multiple of 16, never used.)"""
     p, ld = _matrix(t, name, torch.int8, shape, dev)
     return p, ld if ld % 16 == 0 or t.shape[0] > 1 else -(-ld // 16) * 16
+
+
+def _codes_out(t, name, shape):
+    """Codes to be written, with zeros from each line's end to the next multiple of 16: the tensor has to own those bytes."""
+    p, ld = _matrix(t, name, torch.int8, shape)
+    lines, n = shape
+    if lines and n and (lines == 1 and ld % 16 != 0 or
+                        t.storage_offset() + (lines - 1) * ld + -(-n // 16) * 16 > t.untyped_storage().nbytes()):
+        raise ValueError(f"{name} must hold every line up to the next multiple of 16 bytes (see empty_codes)")
+    return p, ld
 
 
 def _vector(t, name, n, dev=None):
@@ -476,12 +487,13 @@ def empty_codes(lines, n, device="cuda"):
 
 
 def quant8_rows(x, draw=None, q=None, scale=None):
-    """Codes of x by row and a scale per row: (rows, cols) int8, (rows,) float32."""
+    """Codes of x by row and a scale per row: (rows, cols) int8, (rows,) float32.  Given a `q`, zeros are written
+    from the end of each of its lines to the next multiple of 16 bytes."""
     p, ld = _matrix(x, "x")
     rows, cols = x.shape
     q = empty_codes(rows, cols, x.device) if q is None else q
     scale = torch.empty(rows, device=x.device) if scale is None else scale
-    pq, ldq = _codes(q, "q", (rows, cols))
+    pq, ldq = _codes_out(q, "q", (rows, cols))
     _check(lib().tng_quant8_rows(p, _DTYPE[x.dtype], rows, cols, ld, draw, pq, ldq, _vector(scale, "scale", rows), _stream()),
            "tng_quant8_rows")
     return q, scale
@@ -489,12 +501,12 @@ def quant8_rows(x, draw=None, q=None, scale=None):
 
 def quant8_cols(x, draw=None, q=None, scale=None, colsum=None, scratch=None):
     """Codes of x by column, transposed, and a scale per column: (cols, rows) int8, (cols,) float32.
-    `colsum` (cols float32) receives the column sums of x."""
+    `colsum` (cols float32) receives the column sums of x.  A `q` is filled up as by `quant8_rows`."""
     p, ld = _matrix(x, "x")
     rows, cols = x.shape
     q = empty_codes(cols, rows, x.device) if q is None else q
     scale = torch.empty(cols, device=x.device) if scale is None else scale
-    pq, ldq = _codes(q, "q", (cols, rows))
+    pq, ldq = _codes_out(q, "q", (cols, rows))
     ps, _keep = _scratch(scratch, lib().tng_quant8_cols_scratch_bytes(rows, cols), x)
     _check(lib().tng_quant8_cols(p, _DTYPE[x.dtype], rows, cols, ld, draw, pq, ldq, _vector(scale, "scale", cols),
                                  _vector(colsum, "colsum", cols), ps, _stream()), "tng_quant8_cols")

@@ -41,3 +41,13 @@ def test_whole_tiles_back_to_back(m, n, k):
     for out in outs:
         tng.product8(a, sa, b, sb, out=out)
     assert all(torch.equal(out, want) for out in outs)
+
+
+@pytest.mark.parametrize("make,shape", [(tng.quant8_rows, (1, 1001)), (tng.quant8_cols, (1001, 1))])
+def test_codes_of_one_line_leave_what_follows_alone(make, shape):
+    pool = torch.full((2048,), 7, dtype=torch.int8, device="cuda")
+    x = torch.randn(shape, device="cuda")
+    with pytest.raises(ValueError):
+        make(x, q=pool[:1001].view(1, 1001))
+    make(x, q=pool.as_strided((1, 1001), (1008, 1)))
+    assert not pool[1001:1008].any() and bool((pool[1008:] == 7).all())
