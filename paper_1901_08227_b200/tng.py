@@ -139,8 +139,16 @@ def _check(status, what):
         raise TngError(status, what)
 
 
-def _stream() -> int:
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())   # current_stream() builds an object: 3 us a call
+def _device() -> int:
+    return torch.cuda.current_device()
+
+
+def _stream(dev=None) -> int:
+    """Handle of the current stream (of device `dev`).  current_stream() builds an object, 3 us a call: it serves where torch lacks
+    the direct call."""
+    dev = _device() if dev is None else dev
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(dev) if raw is not None else torch.cuda.current_stream(dev).cuda_stream
 
 
 def _dev(t, dtype=torch.float32):
@@ -418,9 +426,6 @@ F32, BF16, F16 = 0, 1, 2
 _DTYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 
-_device = torch._C._cuda_getDevice
-
-
 def _matrix(t, name, dtype=None, shape=None, dev=None):
     """A 2-D CUDA tensor of the current device (dev) with unit column stride -> (pointer, row stride)."""
     if t.get_device() != (_device() if dev is None else dev) or (t.dtype not in _DTYPE if dtype is None else t.dtype != dtype):
@@ -543,7 +548,7 @@ def linear8(x, w, sw, bias=None, out=None, scratch=None):
     nbytes = _linear8_scratch(tokens, k)
     ps, _keep = _scratch(scratch, nbytes, x) if nbytes else (None, None)
     status = lib().tng_linear8(px, _DTYPE[x.dtype], tokens, k, ldx, pw, ldw, _vector(sw, "sw", n, dev), n, _vector(bias, "bias", n, dev), po, ldo,
-                               ps, torch._C._cuda_getCurrentRawStream(dev))
+                               ps, _stream(dev))
     if status:
         raise TngError(status, "tng_linear8")
     return out
@@ -576,7 +581,7 @@ def linear8_grad(dy, x, wt, swt, draw=None, dx=None, dw=None, db=None, scratch=N
         pdb = _vector(db, "db", n, dev)
     ps, _keep = _scratch(scratch, _linear8_grad_scratch(tokens, k, n), dy)
     _check(lib().tng_linear8_grad(py, ldy, px, ldx, _DTYPE[dy.dtype], tokens, k, n, pw, ldw, _vector(swt, "swt", k, dev), draw,
-                                  pdx, lddx, pdw, lddw, pdb, ps, torch._C._cuda_getCurrentRawStream(dev)), "tng_linear8_grad")
+                                  pdx, lddx, pdw, lddw, pdb, ps, _stream(dev)), "tng_linear8_grad")
     return dx, dw, db
 
 
@@ -591,7 +596,7 @@ def dropout(x, p, draw, residual=None, out=None):
     else:
         po, ldo = _matrix(out, "out", x.dtype, x.shape, dev)
     pr, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, x.shape, dev)
-    status = lib().tng_dropout(px, _DTYPE[x.dtype], rows, cols, ldx, pr, ldr, p, draw, po, ldo, torch._C._cuda_getCurrentRawStream(dev))
+    status = lib().tng_dropout(px, _DTYPE[x.dtype], rows, cols, ldx, pr, ldr, p, draw, po, ldo, _stream(dev))
     if status:
         raise TngError(status, "tng_dropout")
     return out

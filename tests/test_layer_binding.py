@@ -1,8 +1,14 @@
 """What the binding of the training-layer operators accepts and passes on (CPU only: the library is a stand-in that records its calls)."""
+import subprocess
+import sys
+from pathlib import Path
+
 import pytest
 import torch
 
 from paper_1901_08227_b200 import tng
+
+ROOT = Path(__file__).resolve().parent.parent
 
 
 class Recorder:
@@ -70,3 +76,29 @@ def test_codes_that_own_their_padding_are_accepted(library, make, name, x):
 def test_codes_of_nothing_are_accepted(library):
     tng.quant8_rows(torch.zeros((0, 20)), q=torch.zeros((0, 20), dtype=torch.int8))
     tng.quant8_cols(torch.zeros((0, 20)), q=torch.zeros((20, 0), dtype=torch.int8))
+
+
+def test_the_package_imports_where_torch_has_no_cuda():
+    """A build of torch without CUDA lacks the names that find the current device and stream."""
+    code = ("import torch\n"
+            "for n in ('_cuda_getDevice', '_cuda_getCurrentRawStream'):\n"
+            "    delattr(torch._C, n)\n"
+            "import paper_1901_08227_b200\n"
+            "from paper_1901_08227_b200 import distributed, tng, workloads\n"
+            "assert tng.empty_codes(2, 20, 'cpu').shape == (2, 20)\n")
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+
+
+def test_the_current_stream_is_asked_for_as_torch_does(monkeypatch):
+    """CUDA is brought up first (and a forked process told that it cannot be), and torch's own call serves where the short cut is missing."""
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    asked = []
+
+    class Stream:
+        cuda_stream = 77
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: asked.append("device") or 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: asked.append(device) or Stream)
+    assert tng._stream() == 77 and asked == ["device", 3]
+    assert tng._device() == 3
