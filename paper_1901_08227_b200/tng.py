@@ -497,7 +497,7 @@ def quant8_rows(x, draw=None, q=None, scale=None):
     p, ld = _matrix(x, "x")
     rows, cols = x.shape
     q = empty_codes(rows, cols, x.device) if q is None else q
-    scale = torch.empty(rows, device=x.device) if scale is None else scale
+    scale = torch.empty(rows, dtype=torch.float32, device=x.device) if scale is None else scale
     pq, ldq = _codes_out(q, "q", (rows, cols))
     _check(lib().tng_quant8_rows(p, _DTYPE[x.dtype], rows, cols, ld, draw, pq, ldq, _vector(scale, "scale", rows), _stream()),
            "tng_quant8_rows")
@@ -510,7 +510,7 @@ def quant8_cols(x, draw=None, q=None, scale=None, colsum=None, scratch=None):
     p, ld = _matrix(x, "x")
     rows, cols = x.shape
     q = empty_codes(cols, rows, x.device) if q is None else q
-    scale = torch.empty(cols, device=x.device) if scale is None else scale
+    scale = torch.empty(cols, dtype=torch.float32, device=x.device) if scale is None else scale
     pq, ldq = _codes_out(q, "q", (cols, rows))
     ps, _keep = _scratch(scratch, lib().tng_quant8_cols_scratch_bytes(rows, cols), x)
     _check(lib().tng_quant8_cols(p, _DTYPE[x.dtype], rows, cols, ld, draw, pq, ldq, _vector(scale, "scale", cols),

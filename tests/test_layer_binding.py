@@ -102,3 +102,14 @@ def test_the_current_stream_is_asked_for_as_torch_does(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: asked.append(device) or Stream)
     assert tng._stream() == 77 and asked == ["device", 3]
     assert tng._device() == 3
+
+
+@pytest.mark.parametrize("default", [torch.float64, torch.bfloat16])
+def test_scales_are_single_precision_whatever_the_default_type(library, default):
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(default)
+    try:
+        x = torch.zeros((3, 20), dtype=torch.float32)
+        assert tng.quant8_rows(x)[1].dtype == tng.quant8_cols(x)[1].dtype == torch.float32
+    finally:
+        torch.set_default_dtype(before)
