@@ -229,5 +229,5 @@ extern "C" tng_status tng_dropout(const void* x_dev, tng_dtype type, uint64_t ro
     const cudaError_t e = with_type(type, [&](auto t) {
         return launch_dropout<decltype(t)>(x_dev, residual_dev, y_dev, a, static_cast<cudaStream_t>(stream));
     });
-    return e == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
+    return layer_status(e);
 }

@@ -178,6 +178,13 @@ cudaError_t launch_layer(void (*kernel)(P...), dim3 grid, dim3 block, size_t sme
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 
+// What a call returns for the last step of its work.  The runtime remembers an error until it is asked for, and calls that
+// ask after their launch would take it for their own: it is cleared here.
+inline tng_status layer_status(cudaError_t e) {
+    if (e == cudaSuccess) return TNG_OK;
+    (void)cudaGetLastError();
+    return TNG_ERR_CUDA;
+}
 // Calls f(T()) for the element type of `type`.
 template <class F> inline cudaError_t with_type(tng_dtype type, F&& f) {
     switch (type) {

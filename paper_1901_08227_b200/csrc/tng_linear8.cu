@@ -38,16 +38,17 @@ tng_status tng_linear8(const void* x_dev, tng_dtype type, uint64_t tokens, uint6
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (product8_codes_tokens(tokens, k)) {
         const Product8 p{nullptr, w_dev, 0, ldw, nullptr, sw_dev, bias_dev, tokens, n, k, y_dev, type, ldy};
-        return launch_linear8_stream(x_dev, ldx, p, st) == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
+        return layer_status(launch_linear8_stream(x_dev, ldx, p, st));
     }
     if (!scratch_dev || !aligned(scratch_dev, 256)) return TNG_ERR_INVALID_ARG;
     Carver c{static_cast<unsigned char*>(scratch_dev)};
     int8_t* q = c.take<int8_t>(codes_bytes(tokens, k));
     float* s = c.take<float>(scales_bytes(tokens));
     const uint64_t ldq = tng_code_stride(k);
-    if (launch_quant8_rows(x_dev, type, tokens, k, ldx, nullptr, q, ldq, s, st) != cudaSuccess) return TNG_ERR_CUDA;
+    const cudaError_t e = launch_quant8_rows(x_dev, type, tokens, k, ldx, nullptr, q, ldq, s, st);
+    if (e != cudaSuccess) return layer_status(e);
     const Product8 p{q, w_dev, ldq, ldw, s, sw_dev, bias_dev, tokens, n, k, y_dev, type, ldy};
-    return launch_product8(p, st) == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
+    return layer_status(launch_product8(p, st));
 }
 
 size_t tng_linear8_grad_scratch_bytes(uint64_t tokens, uint64_t k, uint64_t n) {
@@ -65,9 +66,9 @@ tng_status tng_linear8_grad(const void* dy_dev, uint64_t lddy, const void* x_dev
     if ((dw_dev && !matrix_ok(dw_dev, TNG_F32, k, lddw)) || !aligned(db_dev, 4)) return TNG_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (tokens == 0) {                             // an empty batch has zero gradients
-        if (dw_dev && cudaMemset2DAsync(dw_dev, lddw * 4, 0, k * 4, n, st) != cudaSuccess) return TNG_ERR_CUDA;
-        if (db_dev && cudaMemsetAsync(db_dev, 0, n * 4, st) != cudaSuccess) return TNG_ERR_CUDA;
-        return TNG_OK;
+        cudaError_t e = dw_dev ? cudaMemset2DAsync(dw_dev, lddw * 4, 0, k * 4, n, st) : cudaSuccess;
+        if (e == cudaSuccess && db_dev) e = cudaMemsetAsync(db_dev, 0, n * 4, st);
+        return layer_status(e);
     }
     if (!matrix_ok(dy_dev, type, n, lddy) || !scratch_dev || !aligned(scratch_dev, 256)) return TNG_ERR_INVALID_ARG;
     if (dw_dev && !matrix_ok(x_dev, type, k, ldx)) return TNG_ERR_INVALID_ARG;
@@ -86,19 +87,20 @@ tng_status tng_linear8_grad(const void* dy_dev, uint64_t lddy, const void* x_dev
     uint32_t* tops_x = c.take<uint32_t>(0);
     uint32_t* tops_rows = tops_x + k;
     uint32_t* work_y = tops_rows + tokens;
+    cudaError_t e = cudaSuccess;
     if (dw_dev || db_dev) {
-        if (cudaMemsetAsync(tops_x, 0, (k + tokens + n) * 4, st) != cudaSuccess) return TNG_ERR_CUDA;
+        e = cudaMemsetAsync(tops_x, 0, (k + tokens + n) * 4, st);
         const Quant8Cols jobs[2] = {{dy_dev, tokens, n, lddy, draw, qy, ldc, sy, db_dev, work_y, dx_dev ? tops_rows : nullptr, dx_dev ? qr : nullptr, ldr, sr},
                                     {x_dev, tokens, k, ldx, nullptr, qx, ldc, sx, nullptr, tops_x, nullptr, nullptr, 0, nullptr}};
-        if (launch_quant8_cols(jobs, dw_dev ? 2 : 1, type, st) != cudaSuccess) return TNG_ERR_CUDA;
-    } else if (dx_dev && launch_quant8_rows(dy_dev, type, tokens, n, lddy, draw, qr, ldr, sr, st) != cudaSuccess) {
-        return TNG_ERR_CUDA;
+        if (e == cudaSuccess) e = launch_quant8_cols(jobs, dw_dev ? 2 : 1, type, st);
+    } else if (dx_dev) {
+        e = launch_quant8_rows(dy_dev, type, tokens, n, lddy, draw, qr, ldr, sr, st);
     }
+    if (e != cudaSuccess) return layer_status(e);
     const Product8 to_x{qr, wt_dev, ldr, ldwt, sr, swt_dev, nullptr, tokens, k, n, dx_dev, type, lddx};
     const Product8 to_w{qy, qx, ldc, ldc, sy, sx, nullptr, n, k, tokens, dw_dev, TNG_F32, lddw};
-    const cudaError_t e = dx_dev && dw_dev ? launch_product8_two(to_x, to_w, st) : dx_dev ? launch_product8(to_x, st) : dw_dev ? launch_product8(to_w, st) : cudaSuccess;
-    if (e != cudaSuccess) return TNG_ERR_CUDA;
-    return TNG_OK;
+    e = dx_dev && dw_dev ? launch_product8_two(to_x, to_w, st) : dx_dev ? launch_product8(to_x, st) : dw_dev ? launch_product8(to_w, st) : cudaSuccess;
+    return layer_status(e);
 }
 
 }  // extern "C"

@@ -961,5 +961,5 @@ extern "C" tng_status tng_product8(const int8_t* a_dev, uint64_t lda, const floa
         !aligned(bias_dev, 4) || !matrix_ok(out_dev, type, n, ldo))
         return TNG_ERR_INVALID_ARG;
     const Product8 p{a_dev, b_dev, lda, ldb, sa_dev, sb_dev, bias_dev, m, n, k, out_dev, type, ldo};
-    return launch_product8(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
+    return layer_status(launch_product8(p, static_cast<cudaStream_t>(stream)));
 }

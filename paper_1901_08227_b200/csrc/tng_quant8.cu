@@ -408,8 +408,7 @@ tng_status tng_quant8_rows(const void* x_dev, tng_dtype type, uint64_t rows, uin
     if (!type_ok(type) || cols < 1 || !dims_ok(rows, cols) || (draw && !draw_ok(draw, rows))) return TNG_ERR_INVALID_ARG;
     if (rows == 0) return TNG_OK;
     if (!matrix_ok(x_dev, type, cols, ldx) || !codes_ok(q_dev, cols, ldq) || !scale_dev || !aligned(scale_dev, 4)) return TNG_ERR_INVALID_ARG;
-    return launch_quant8_rows(x_dev, type, rows, cols, ldx, draw, q_dev, ldq, scale_dev, static_cast<cudaStream_t>(stream)) == cudaSuccess
-               ? TNG_OK : TNG_ERR_CUDA;
+    return layer_status(launch_quant8_rows(x_dev, type, rows, cols, ldx, draw, q_dev, ldq, scale_dev, static_cast<cudaStream_t>(stream)));
 }
 
 size_t tng_quant8_cols_scratch_bytes(uint64_t rows, uint64_t cols) {
@@ -422,16 +421,18 @@ tng_status tng_quant8_cols(const void* x_dev, tng_dtype type, uint64_t rows, uin
     if (!scale_dev || !aligned(scale_dev, 4) || !aligned(colsum_dev, 4)) return TNG_ERR_INVALID_ARG;
     if (rows == 0) {                               // columns of nothing: scale and sum zero
         cudaStream_t st = static_cast<cudaStream_t>(stream);
-        if (cudaMemsetAsync(scale_dev, 0, cols * 4, st) != cudaSuccess) return TNG_ERR_CUDA;
-        return !colsum_dev || cudaMemsetAsync(colsum_dev, 0, cols * 4, st) == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
+        cudaError_t e = cudaMemsetAsync(scale_dev, 0, cols * 4, st);
+        if (e == cudaSuccess && colsum_dev) e = cudaMemsetAsync(colsum_dev, 0, cols * 4, st);
+        return layer_status(e);
     }
     if (!matrix_ok(x_dev, type, cols, ldx) || !codes_ok(q_dev, rows, ldq) || !scratch_dev || !aligned(scratch_dev, 256))
         return TNG_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint32_t* scratch = static_cast<uint32_t*>(scratch_dev);
-    if (cudaMemsetAsync(scratch, 0, cols * 4, st) != cudaSuccess) return TNG_ERR_CUDA;
+    const cudaError_t e = cudaMemsetAsync(scratch, 0, cols * 4, st);
+    if (e != cudaSuccess) return layer_status(e);
     const Quant8Cols job{x_dev, rows, cols, ldx, draw, q_dev, ldq, scale_dev, colsum_dev, scratch, nullptr, nullptr, 0, nullptr};
-    return launch_quant8_cols(&job, 1, type, st) == cudaSuccess ? TNG_OK : TNG_ERR_CUDA;
+    return layer_status(launch_quant8_cols(&job, 1, type, st));
 }
 
 }  // extern "C"

@@ -51,3 +51,41 @@ def test_codes_of_one_line_leave_what_follows_alone(make, shape):
         make(x, q=pool[:1001].view(1, 1001))
     make(x, q=pool.as_strided((1, 1001), (1008, 1)))
     assert not pool[1001:1008].any() and bool((pool[1008:] == 7).all())
+
+
+def test_an_empty_batch_clears_rows_that_are_far_apart():
+    ld = (1 << 29) + 64                                     # rows 2 GB apart
+    buf = torch.full((ld + 64,), 5.0, device="cuda")
+    dw = buf.as_strided((2, 20), (ld, 1))
+    wt, swt = tng.quant8_cols(torch.randn(2, 20, device="cuda"))
+    tng.linear8_grad(torch.empty((0, 2), device="cuda"), torch.empty((0, 20), device="cuda"), wt, swt, dw=dw)
+    assert not dw.any() and bool((buf[20:64] == 5).all()) and bool((buf[ld + 20:] == 5).all())
+
+
+@pytest.mark.parametrize("call", ["quant8_rows", "quant8_cols", "product8", "linear8", "dropout"])
+def test_a_call_that_fails_leaves_no_error_behind(call):
+    """Enqueueing on the legacy stream while a stream that it synchronises with is captured is refused by the runtime; the next
+    call must not report it again."""
+    rt = pytest.importorskip("cuda.bindings.runtime")
+    x = torch.randn(20, 64, device="cuda")
+    q, s = tng.quant8_rows(x)
+    qc, sc = tng.quant8_cols(x)
+    y, scratch = torch.empty(20, 20, device="cuda"), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    w, v = torch.zeros(64, device="cuda"), torch.ones(64, device="cuda")
+    make = {"quant8_rows": lambda: tng.quant8_rows(x, q=q, scale=s), "quant8_cols": lambda: tng.quant8_cols(x, q=qc, scale=sc, scratch=scratch),
+            "product8": lambda: tng.product8(q, s, q, s, out=y), "linear8": lambda: tng.linear8(x, q, s, out=y, scratch=scratch),
+            "dropout": lambda: tng.dropout(x, 0.5, tng.Draw(), out=x)}[call]
+    make()
+    torch.cuda.synchronize()
+    assert torch.cuda.current_stream().cuda_stream == 0
+    error, stream = rt.cudaStreamCreate()
+    assert error == 0 and rt.cudaStreamBeginCapture(stream, rt.cudaStreamCaptureMode.cudaStreamCaptureModeRelaxed)[0] == 0
+    try:
+        with pytest.raises(tng.TngError) as e:
+            make()
+    finally:
+        rt.cudaStreamEndCapture(stream)
+        rt.cudaStreamDestroy(stream)
+    assert e.value.status == tng.ERR_CUDA
+    tng.sgd_update(w, v, 0.5)                               # (reports whatever error its thread has pending)
+    assert bool((w == -0.5).all())
