@@ -266,7 +266,7 @@ __device__ __forceinline__ ColumnScale column_scale(const Product8& p, uint64_t 
 }
 
 // Scales W columns of a warp's 32 rows and writes them out through the warp's 2 KB of staging.  ok = false: NaN.
-// TILES (rows of 16-byte multiples): W columns are 64 bytes, copied as a box in the 64-byte swizzle (16-byte pieces by
+// TILES (rows that start and end on 16-byte boundaries): W columns are 64 bytes, copied as a box in the 64-byte swizzle (16-byte pieces by
 // lane: no bank conflicts) that clips at the matrix and runs on while the next columns are scaled.  Else W = 16, two rows
 // of 16 elements an access.  (32-byte stores by each lane into its own row cost a cache line an access: 3500 cycles for
 // 32 x 32 fp32 against a stage's 513.)
@@ -849,7 +849,12 @@ cudaError_t launch_pair_as(const Product8& p, const Product8* p2, uint32_t split
     return launch_layer(kernel, (unsigned)(2 * (SPLIT ? tiles * split : tiles < pairs ? tiles : pairs)), kPairThreads, kPairSmem, 2 * split, st,
                         maps[0].a, maps[0].b, maps[0].o, maps[1], args, split);
 }
-bool rows_by_tiles(const Product8& p) { return (reinterpret_cast<uintptr_t>(p.out) | p.ldo * type_bytes(p.type)) % 16 == 0; }
+// Whether the output may leave by tiled copies.  Its rows start on 16-byte boundaries, as the copies need, and end on one: a copy
+// clips at the matrix in pieces of 16 bytes and would clear up to 15 bytes after a row that ends inside one.
+bool rows_by_tiles(const Product8& p) {
+    const uint64_t e = type_bytes(p.type);
+    return (reinterpret_cast<uintptr_t>(p.out) | p.ldo * e | p.n * e) % 16 == 0;
+}
 template <typename T> cudaError_t launch_pair(const Product8& p, uint32_t split, cudaStream_t st) {
     const bool tiles = rows_by_tiles(p);
     if (split > 1) return tiles ? launch_pair_as<T, true, true, false>(p, nullptr, split, st) : launch_pair_as<T, true, false, false>(p, nullptr, split, st);

@@ -94,7 +94,8 @@ template <int GROUP> __device__ __forceinline__ void tile_load(uint32_t dst, con
             "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
             "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
-// This CTA's shared memory into a box of the map, clipped to the matrix; x a multiple of 16 bytes, both >= 0.
+// This CTA's shared memory into a box of the map, clipped to the matrix, whose rows are whole 16-byte pieces; x a multiple of
+// 16 bytes, both >= 0.
 __device__ __forceinline__ void tile_store(const CUtensorMap* map, int32_t x, int32_t y, uint32_t src) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");

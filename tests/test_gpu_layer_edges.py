@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_1901_08227_b200 import tng
-from test_gpu_layers import random_codes
+from test_gpu_layers import DTYPES, SEED, random_codes, values
 
 pytestmark = pytest.mark.gpu
 
@@ -89,3 +89,39 @@ def test_a_call_that_fails_leaves_no_error_behind(call):
     assert e.value.status == tng.ERR_CUDA
     tng.sgd_update(w, v, 0.5)                               # (reports whatever error its thread has pending)
     assert bool((w == -0.5).all())
+
+
+# Rows of the output start on 16-byte boundaries; where they end on one too they leave by tiled copies, else by scalar stores.
+# Neither may touch the padding.  (rows, columns, contraction): split in four, in two, whole tiles, several waves of them
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,n,k", [(200, 301, 4096), (1300, 4093, 2048), (300, 301, 200), (515, 1003, 777), (2570, 5121, 130), (200, 304, 4096), (1300, 4088, 2048), (300, 264, 200), (2570, 5128, 130)])
+def test_products_into_padded_aligned_rows(dtype, m, n, k):
+    a, sa = random_codes(m, k, m)
+    b, sb = random_codes(n, k, n)
+    bias = values((n,), torch.float32, 5)
+    want = (wanted(a, sa, b, sb, torch.float32) + bias).to(dtype)
+    for ld in (-(-n // 8) * 8, -(-n // 8) * 8 + 24):
+        base = torch.full((m + 1, ld), 7.0, dtype=dtype, device="cuda")
+        tng.product8(a, sa, b, sb, bias=bias, out=base[:m, :n])
+        assert torch.equal(base[:m, :n], want) and bool((base[:m, n:] == 7).all()) and bool((base[m] == 7).all())
+    loose = torch.full((m, n + 1), 7.0, dtype=dtype, device="cuda")       # the same by scalar stores
+    if (n + 1) * loose.element_size() % 16 != 0:
+        tng.product8(a, sa, b, sb, bias=bias, out=loose[:, :n])
+        assert torch.equal(loose[:, :n], want) and bool((loose[:, n] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("T,K,N", [(2050, 517, 525), (333, 301, 205), (5000, 1029, 1037), (2050, 520, 528), (333, 304, 205),
+                                   (5000, 1032, 1037)])
+def test_gradients_into_padded_aligned_rows(dtype, drawn, T, K, N):
+    """The reference runs on the GPU in 64 bits, from the quantisers' codes."""
+    x, dy = values((T, K), dtype, 1), values((T, N), dtype, 2, 1e-2)
+    wt, swt = tng.quant8_cols(values((N, K), torch.float32, 3, K ** -0.5))
+    d = tng.Draw(SEED, 4, 8, row0=5) if drawn else None
+    ld = -(-K // 8) * 8 + 8
+    dx = torch.full((T, ld), 7.0, dtype=dtype, device="cuda")
+    dw = torch.full((N, ld), 7.0, device="cuda")
+    tng.linear8_grad(dy, x, wt, swt, draw=d, dx=dx[:, :K], dw=dw[:, :K])
+    assert torch.equal(dx[:, :K], wanted(*tng.quant8_rows(dy, d), wt, swt, dtype)) and bool((dx[:, K:] == 7).all())
+    assert torch.equal(dw[:, :K], wanted(*tng.quant8_cols(dy, d), *tng.quant8_cols(x), torch.float32)) and bool((dw[:, K:] == 7).all())
