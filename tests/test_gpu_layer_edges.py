@@ -2,8 +2,10 @@
 import pytest
 import torch
 
+import layers_ref as ref
+from gpu_util import to_np
 from paper_1901_08227_b200 import tng
-from test_gpu_layers import DTYPES, SEED, random_codes, values
+from test_gpu_layers import DTYPES, SEED, f32, random_codes, rounded, same, values
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +127,83 @@ def test_gradients_into_padded_aligned_rows(dtype, drawn, T, K, N):
     tng.linear8_grad(dy, x, wt, swt, draw=d, dx=dx[:, :K], dw=dw[:, :K])
     assert torch.equal(dx[:, :K], wanted(*tng.quant8_rows(dy, d), wt, swt, dtype)) and bool((dx[:, K:] == 7).all())
     assert torch.equal(dw[:, :K], wanted(*tng.quant8_cols(dy, d), *tng.quant8_cols(x), torch.float32)) and bool((dw[:, K:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,K,N", [(2048, 512, 520), (300, 2600, 2600), (1500, 5000, 20000), (9000, 768, 2900)])
+def test_drawn_gradients_of_many_tiles(dtype, T, K, N):
+    x, dy = values((T, K), dtype, 1), values((T, N), dtype, 2, 1e-2)
+    wt, swt = tng.quant8_cols(values((N, K), torch.float32, 3, K ** -0.5))
+    d = tng.Draw(SEED, 4, 8, row0=5)
+    dx, dw, _ = tng.linear8_grad(dy, x, wt, swt, draw=d)
+    assert torch.equal(dx, wanted(*tng.quant8_rows(dy, d), wt, swt, dtype))
+    assert torch.equal(dw, wanted(*tng.quant8_cols(dy, d), *tng.quant8_cols(x), torch.float32))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("drawn", [False, True])
+def test_gradients_of_lines_that_are_zero_tiny_or_not_finite(dtype, drawn):
+    """dy's row and column codes come from one pass: each line's fate is its own, as when the quantisers code it apart."""
+    T, K, N = 300, 40, 200
+    clean = values((T, N), dtype, 3)
+    x = values((T, K), dtype, 4)
+    wt, swt = tng.quant8_cols(values((N, K), torch.float32, 5))
+    d = tng.Draw(SEED, 6, 7) if drawn else None
+    u = ref.uniforms(T, N, SEED, 6, 7, ref.TAG_ROUNDING) if drawn else None
+    tiny = 2.0 ** -126 if dtype != torch.float16 else 2.0 ** -24
+    for name, spoil in {"nan": lambda y: y[5, 7].fill_(float("nan")), "inf": lambda y: y[129, 65].fill_(float("inf")),
+                        "-inf": lambda y: y[299, 199].fill_(float("-inf")), "rows": lambda y: y[10:20].zero_(), "columns": lambda y: y[:, 60:70].zero_(),
+                        "tiny row": lambda y: y[250].mul_(tiny), "tiny column": lambda y: y[:, 130].mul_(tiny),
+                        "largest": lambda y: y[77].fill_(torch.finfo(dtype).max)}.items():
+        dy = clean.clone()
+        spoil(dy)
+        dx, dw, db = tng.linear8_grad(dy, x, wt, swt, draw=d)
+        wdx, wdw, _ = ref.linear_grad(f32(dy), f32(x), to_np(wt), to_np(swt), u)
+        assert same(f32(dx), rounded(wdx, dtype)), name
+        assert same(to_np(dw), wdw), name
+        row_bad, col_bad = ~torch.isfinite(dy).all(1), ~torch.isfinite(dy).all(0)
+        assert torch.equal(torch.isnan(dx).all(1), row_bad) and torch.equal(torch.isnan(dw).all(1), col_bad)
+        assert torch.equal(~torch.isfinite(db), col_bad)
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+def test_gradients_can_be_captured_in_a_graph(drawn):
+    T, K, N = 300, 512, 260
+    x, dy = values((T, K), torch.bfloat16, 1), values((T, N), torch.bfloat16, 2)
+    wt, swt = tng.quant8_cols(values((N, K), torch.float32, 3))
+    d = tng.Draw(1, 2, 3) if drawn else None
+    dx, dw, db = torch.empty_like(x), torch.empty((N, K), device="cuda"), torch.empty(N, device="cuda")
+    q, s, sums = tng.empty_codes(K, T), torch.empty(K, device="cuda"), torch.empty(K, device="cuda")
+    scratch = torch.empty(tng.lib().tng_linear8_grad_scratch_bytes(T, K, N), dtype=torch.uint8, device="cuda")
+    scratch2 = torch.empty(tng.lib().tng_quant8_cols_scratch_bytes(T, K), dtype=torch.uint8, device="cuda")
+
+    def step():
+        tng.linear8_grad(dy, x, wt, swt, draw=d, dx=dx, dw=dw, db=db, scratch=scratch)
+        tng.quant8_cols(dx, d, q=q, scale=s, colsum=sums, scratch=scratch2)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+        step()                                              # a clear right after a product
+    for seed in (5, 6, 7):
+        dy.copy_(values((T, N), torch.bfloat16, seed))
+        x.copy_(values((T, K), torch.bfloat16, seed + 10))
+        graph.replay()
+        got = [t.clone() for t in (dx, dw, db, q, s, sums)]
+        step()
+        assert all(torch.equal(a, b) for a, b in zip(got, (dx, dw, db, q, s, sums)))
+        assert torch.equal(dx, tng.linear8_grad(dy, x, wt, swt, draw=d)[0])
+
+
+@pytest.mark.parametrize("dtype,cols", [(torch.float32, 40007), (torch.bfloat16, 70001), (torch.float16, 131056), (torch.float32, 131056)])
+def test_rows_longer_than_a_block_holds(dtype, cols):
+    """Rows that the registers of 1024 threads do not hold are read a second time."""
+    x = values((3, cols), dtype, 1)
+    x[1, cols - 1] = 50.0                                   # the largest lies in the part that is not kept
+    for draw in (None, tng.Draw(SEED, 5, 77, row0=3)):
+        u = None if draw is None else ref.uniforms(3, cols, SEED, 5, 77, ref.TAG_ROUNDING, 3)
+        q, s = tng.quant8_rows(x, draw)
+        wq, ws = ref.codes(f32(x), u)
+        assert same(to_np(q), wq) and same(to_np(s), ws)
