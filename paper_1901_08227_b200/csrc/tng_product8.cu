@@ -595,11 +595,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 // The 128 rows are rows of b, the NT columns rows of a (tokens): with few tokens the weights are the long side, and an
 // output row then runs along the lanes.  The CTAs of a cluster take consecutive parts of the contraction, leave
 // their int32 sums in shared memory and each write out a part of the columns, summed over the cluster's shared
-// memories.  Bound by the weights' traffic and 3.5 us of launch, set-up and last meeting: 8 x 16384 x 2048 8.6 us (3.9 TB/s).
-// Warps: 0-3 write out, 4 feeds, 5 issues.
+// memories.  Bound by the weights' traffic and 3.5 us of launch, set-up and last meeting: 9 x 16384 x 2048 10.4 us with the
+// weights from memory (3.3 TB/s).  Warps: 0-3 write out, 4 feeds, 5 issues.
 constexpr int kSlimThreads = 192;
-// Rows of a up to which this kernel is taken.  64 x 4096 x 4096: 8.0 us, the pairs 10.8; 64 x 16384 x 2048: 12.8 and 10.9;
-// 100 rows: 10.2 and 10.9, 16.7 and 11.4.
+// Rows of a that a tile holds at most; which products are taken: see takes_slim.
 constexpr uint64_t kSlimRows = 64;
 template <int NT> struct SlimGeom {
     static constexpr uint32_t kA = 128 * 128, kB = NT * 128, kStage = kA + kB;
@@ -897,6 +896,20 @@ template <typename T> uint32_t pair_split(const Product8& p) {
     return split;
 }
 
+// Which kernel a product of few rows takes.  The slim kernel's time grows with the rows (2 to 3 us from 24 to 64: more output by
+// scalar stores), the pairs' does not: above 32 rows the pairs win where their tiles, whole or in two parts, fill half a wave
+// or more and not more than one.  Slim and pairs, us, weights from memory:
+//   24 rows: 16384 x 2048 11.1, 11.3   8192 x 4096 12.1, 14.2   12288 x 4096 16.2, 18.5   5120 x 1024 6.7, 6.5
+//   48 rows: 16384 x 2048 12.4, 11.1   8192 x 4096 13.9, 12.1   12288 x 4096 17.5, 14.5   5120 x 1024 8.5, 7.1
+//   64 rows, less than half a wave: 1024 x 1024 5.3, 6.2   4096 x 4096 9.1, 10.4   4608 x 8192 13.6, 15.4
+//   64 rows, four parts: 2560 x 2560 7.4, 7.7   more than a wave: 28672 x 4096 26.0, 26.8   28672 x 8192 46.6, 52.4
+//   (but 65536 x 1024 22.9, 19.0)
+template <typename T> bool takes_slim(const Product8& p) {
+    if (p.m > kSlimRows || p.m <= 32) return p.m <= 32;
+    const uint64_t split = pair_split<T>(p), units = (p.n + 255) / 256 * split, pairs = (uint64_t)sm_count_now() / 2;
+    return split > 2 || 2 * units < pairs || units > pairs;
+}
+
 template <int NT, typename T> cudaError_t launch_slim(const Product8& p, uint32_t split, cudaStream_t st) {
     using G = SlimGeom<NT>;
     static PerDevice<bool> done;
@@ -928,7 +941,7 @@ cudaError_t launch_product8(const Product8& p, cudaStream_t st) {
     const uint64_t sms = (uint64_t)sm_count_now(), kblocks = (p.k + 127) / 128;
     return with_type(p.type, [&](auto t) {
         using T = decltype(t);
-        if (p.m <= kSlimRows) {
+        if (takes_slim<T>(p)) {
             const uint64_t nt = p.m <= 16 ? 16 : p.m <= 32 ? 32 : 64;
             const uint64_t tiles = (p.n + 127) / 128;
             uint32_t split = 1;

@@ -33,6 +33,17 @@ def test_split_contractions_with_parts_outside_the_matrix(dtype, m, n, k):
     assert all(torch.equal(out, other if i % 2 else want) for i, out in enumerate(outs))
 
 
+# Around the rule between the two kernels for up to 64 rows: rows 32, 33, 64, 65 with tiles below and above half a wave and a wave.
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [32, 33, 64, 65])
+@pytest.mark.parametrize("n,k", [(9215, 300), (9473, 300), (4863, 1200), (4609, 1200), (18944, 144), (18945, 144), (4096, 4096)])
+def test_products_around_the_choice_of_a_kernel(dtype, m, n, k):
+    a, sa = random_codes(m, k, m + k)
+    b, sb = random_codes(n, k, n + k)
+    bias = values((n,), torch.float32, 5)
+    assert torch.equal(tng.product8(a, sa, b, sb, bias=bias, dtype=dtype), (wanted(a, sa, b, sb, torch.float32) + bias).to(dtype))
+
+
 @pytest.mark.parametrize("m,n,k", [(512, 512, 64), (2600, 5000, 48), (300, 20000, 16)])
 def test_whole_tiles_back_to_back(m, n, k):
     """Tiles of one block of the contraction: a pair's last hand-backs come right before it leaves."""
