@@ -218,3 +218,44 @@ def test_rows_longer_than_a_block_holds(dtype, cols):
         q, s = tng.quant8_rows(x, draw)
         wq, ws = ref.codes(f32(x), u)
         assert same(to_np(q), wq) and same(to_np(s), ws)
+
+
+@pytest.mark.parametrize("n", [264, 261])
+def test_products_of_rows_far_apart(n):
+    """Codes and outputs whose last rows lie beyond 32 bits of bytes: tiled copies and scalar stores."""
+    m, k = 130, 200
+    a, sa = random_codes(m, k, 1)
+    b, sb = random_codes(n, k, 2)
+    want = wanted(a, sa, b, sb, torch.bfloat16)
+    ld = (1 << 25) + 64
+    far = torch.empty((m - 1) * ld + 256, dtype=torch.int8, device="cuda").as_strided((m, k), (ld, 1))
+    far.copy_(a)
+    out = torch.empty((m - 1) * ld + 512, dtype=torch.bfloat16, device="cuda").as_strided((m, n), (ld, 1))
+    tng.product8(far, sa, b, sb, out=out)
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T", [1, 5, 8, 12, 70])
+def test_what_follows_a_line_does_not_count(dtype, T):
+    """Weights that are a part of wider codes, activations and outputs that are parts of wider rows."""
+    K, N = 203, 37
+    wide, sw = random_codes(N, K + 45, 1)
+    x = torch.full((T, K + 5), float("nan"), dtype=dtype, device="cuda")
+    x[:, :K] = values((T, K), dtype, 2)
+    y = torch.full((T, N + 3), 7.0, dtype=dtype, device="cuda")
+    tng.linear8(x[:, :K], wide[:, :K], sw, out=y[:, :N])
+    want = ref.linear(f32(x[:, :K]), to_np(wide[:, :K]), to_np(sw))
+    assert same(f32(y[:, :N]), rounded(want, dtype)) and bool((y[:, N:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(3, 5), (40, 1000), (300, 4097), (2000, 1030)])
+def test_dropout_writes_its_columns_only(dtype, rows, cols):
+    x = values((rows, cols), dtype, 1)
+    d = tng.Draw(SEED, 3, 12)
+    want = tng.dropout(x, 0.3, d, residual=x)
+    for ld in (cols + 1, -(-cols // 8) * 8 + 8):
+        base = torch.full((rows + 1, ld), 7.0, dtype=dtype, device="cuda")
+        tng.dropout(x, 0.3, d, residual=x, out=base[:rows, :cols])
+        assert torch.equal(base[:rows, :cols], want) and bool((base[:rows, cols:] == 7).all()) and bool((base[rows] == 7).all())
