@@ -115,7 +115,7 @@ struct Quant8Cols {
     uint64_t ld_row;
     float* row_scale;
 };
-uint64_t quant8_cols_scratch(uint64_t rows, uint64_t cols, bool sums);
+uint64_t quant8_cols_scratch(uint64_t rows, uint64_t cols);       // words: maxima of the columns, sums of the chunks
 cudaError_t launch_quant8_cols(const Quant8Cols* jobs, int n, tng_dtype type, cudaStream_t st);   // n = 1 or 2
 struct Product8 {
     const int8_t *a, *b;

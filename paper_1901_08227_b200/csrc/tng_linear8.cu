@@ -54,7 +54,7 @@ tng_status tng_linear8(const void* x_dev, tng_dtype type, uint64_t tokens, uint6
 size_t tng_linear8_grad_scratch_bytes(uint64_t tokens, uint64_t k, uint64_t n) {
     if (tokens == 0) return 256;
     return (size_t)(codes_bytes(tokens, n) + scales_bytes(tokens) + codes_bytes(n, tokens) + scales_bytes(n) + codes_bytes(k, tokens) +
-                    scales_bytes(k) + up256(4 * (k + tokens + quant8_cols_scratch(tokens, n, true))));
+                    scales_bytes(k) + up256(4 * (k + tokens + quant8_cols_scratch(tokens, n))));
 }
 
 tng_status tng_linear8_grad(const void* dy_dev, uint64_t lddy, const void* x_dev, uint64_t ldx, tng_dtype type, uint64_t tokens,

@@ -297,10 +297,12 @@ __global__ void __launch_bounds__(256, DRAW ? (ROWS ? 2 : 3) : (ROWS ? 3 : 4)) q
     }
 }
 
-// Row chunks of the statistics: about four CTAs an SM, 32 rows at least.
+// Row chunks of the statistics: about four CTAs an SM, and a chunk for every 32 rows at most (33 rows are two of 17 and 16).  The
+// SMs are a B200's, not those of the current device: the sizes of scratch follow from the chunks.
+constexpr uint64_t kStatCtas = 4 * 148;
 uint32_t column_chunks(uint64_t rows, uint64_t cols) {
     const uint64_t blocks = (cols + kStatCols - 1) / kStatCols;
-    uint64_t chunks = (4 * 148 + blocks - 1) / blocks;
+    uint64_t chunks = (kStatCtas + blocks - 1) / blocks;
     const uint64_t most = (rows + 31) / 32;
     if (chunks > most) chunks = most;
     return chunks < 1 ? 1u : (uint32_t)chunks;
@@ -348,7 +350,7 @@ cudaError_t launch_quant8_rows(const void* x, tng_dtype type, uint64_t rows, uin
     });
 }
 
-uint64_t quant8_cols_scratch(uint64_t rows, uint64_t cols, bool sums) { return (1 + (sums ? (uint64_t)column_chunks(rows, cols) : 0)) * cols; }
+uint64_t quant8_cols_scratch(uint64_t rows, uint64_t cols) { return (1 + (uint64_t)column_chunks(rows, cols)) * cols; }
 
 // Jobs of one type whose maxima (the first words of their scratch, row_tops) are clear; only the first may have row codes.  Two of them share the launches where
 // they are alike in alignment and neither is drawn.
@@ -412,7 +414,7 @@ tng_status tng_quant8_rows(const void* x_dev, tng_dtype type, uint64_t rows, uin
 }
 
 size_t tng_quant8_cols_scratch_bytes(uint64_t rows, uint64_t cols) {
-    return (size_t)((quant8_cols_scratch(rows, cols, true) * 4 + 255) / 256 * 256);
+    return (size_t)((quant8_cols_scratch(rows, cols) * 4 + 255) / 256 * 256);
 }
 
 tng_status tng_quant8_cols(const void* x_dev, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx, const tng_draw* draw,
