@@ -333,7 +333,12 @@ tng_status tng_sgd_update(float* w_dev, const float* v_dev, uint64_t d, float et
  * and their row stride is a multiple of 16 (tng_code_stride).  Scales, bias, dw, db are fp32.
  * Rows and columns are below 2^31, contractions at most TNG_MAX_CONTRACTION long (the int32 sums
  * are exact up to there).  A call with no rows succeeds: sums over the rows (dw, db, column scales and
- * sums) are zero, and there is nothing else to write.  Outputs must not overlap inputs, except where stated. */
+ * sums) are zero, and there is nothing else to write.  Outputs must not overlap inputs, except where stated.
+ *
+ * Errors.  The calls only enqueue work, so a failure that shows on the GPU alone is reported in the output: if a bounded
+ * wait of a product's kernel gives up (tng_product8, tng_linear8, tng_linear8_grad), the outputs that it still owed are
+ * NaN while the call has returned TNG_OK.  A line of inputs that is not finite gives NaN outputs too, but only for its
+ * own row or column.  After such an event every other call works on as before. */
 typedef enum { TNG_F32 = 0, TNG_BF16 = 1, TNG_F16 = 2 } tng_dtype;
 
 /* Where random numbers come from: Philox4x32-10 with key (seed_lo, seed_hi) and counter

@@ -2,6 +2,9 @@
 //   out[i][j] = (float(sum_l a[i][l] b[j][l]) sa[i]) sb[j] + bias[j].
 //
 // The int32 sums are exact, so every variant below gives the same bits whatever order it sums in.
+//
+// Every wait on a barrier has a poll limit.  When one runs out the sums are incomplete: the outputs that the CTAs concerned
+// still owe become NaN (`ok`, `good` below), which is how a call that never waits for the GPU reports it.
 #include <math_constants.h>
 
 #include "tng_codes.cuh"
@@ -10,8 +13,7 @@
 namespace tng {
 namespace {
 
-// A bounded wait gave up: the sums are incomplete and every output the CTA still owes becomes NaN, which is how
-// a call that never waits for the GPU reports it.
+// A sum as an output, each operation one fp32 rounding.
 __device__ __forceinline__ float scaled(int acc, float sa, float sb, bool has_bias, float bias) {
     const float v = __fmul_rn(__fmul_rn((float)acc, sa), sb);
     return has_bias ? __fadd_rn(v, bias) : v;
