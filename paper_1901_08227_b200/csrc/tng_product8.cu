@@ -367,8 +367,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                          const __grid_constant__ PairMaps maps2, const __grid_constant__ PairArgs args, uint32_t split) {
     static_assert(!(SPLIT && DUAL) && (TILES || !DUAL), "two products are whole tiles, by tiled copies");
     extern __shared__ unsigned char dyn[];
-    __shared__ uint32_t sh_tmem;
-    __shared__ volatile uint32_t sh_failed;
+    __shared__ volatile uint32_t sh_tmem, sh_failed;
     const uint32_t data = (smem_u32(dyn) + 1023u) & ~1023u;
     unsigned char* stages = dyn + (data - smem_u32(dyn));
     const uint32_t bars = data + kPairStages * kPairStage + 16 * kStageStride;
@@ -405,7 +404,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     // Tensor memory is taken only now: a launch that held it while it waits could keep the one it waits for (which need not
     // be this library's) from ever getting its own.  The first copies travel meanwhile.
     if (warp == 17) {
-        tmem_alloc<2>(smem_u32(&sh_tmem), 2 * kPairTile);
+        tmem_alloc<2>(smem_u32((const void*)&sh_tmem), 2 * kPairTile);
         if (rank == 1 && lane == 0) cluster_arrive(cluster_map(ready, even));
     }
     if (warp != 16) {
@@ -414,7 +413,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         umma_fence_after();
         grid_go();
     }
-    const uint32_t tmem = sh_tmem;
 
     if (warp == 16 && lane == 0) {
         // ---- feed: this CTA's rows of either operand, completion counted on the even CTA's barrier
@@ -449,7 +447,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         uint32_t s = 0, parity = 0, n_acc = 0;
         bool ok = mbar_wait(ready, 0);                     // the odd CTA has its tensor memory
         for (; ok && walk.step<DUAL>(); ++n_acc) {
-            const uint32_t acc = n_acc & 1u, use = n_acc >> 1, blocks = k_last() - k_first(), into = tmem + acc * kPairTile;
+            const uint32_t acc = n_acc & 1u, use = n_acc >> 1, blocks = k_last() - k_first(), into = sh_tmem + acc * kPairTile;
             // instructions of the last block: 32 codes each
             const uint32_t rest = (uint32_t)((args.p[DUAL ? walk.cur : 0].k + 31) / 32) - (k_last() - 1) * 4, last_steps = rest < 4 ? rest : 4;
             if (use > 0 && !mbar_wait(acc_empty + 8 * acc, (use - 1) & 1u)) { ok = false; break; }
@@ -498,7 +496,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                 if (ok && !mbar_wait(acc_full + 8 * acc, use & 1u)) ok = false;
                 ok = __all_sync(kFullMask, ok && !sh_failed);
                 umma_fence_after();
-                const uint32_t from = tmem + ((quad * 32) << 16) + acc * kPairTile + group * 64;
+                const uint32_t from = sh_tmem + ((quad * 32) << 16) + acc * kPairTile + group * 64;
                 const auto done = [&] {
                     umma_fence_before();                   // everything read: the next tile may overwrite it
                     __syncwarp();
@@ -536,7 +534,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
                 const uint32_t c = group * 64 + ch * 32;
                 if (c >= mine && c < mine + cols) continue;
                 uint32_t r[32];
-                tmem_ld32(tmem + ((quad * 32) << 16) + c, r);
+                tmem_ld32(sh_tmem + ((quad * 32) << 16) + c, r);
                 tmem_wait_ld();
                 int4* to = sums + (c / 4) * 128 + quad * 32 + lane;
 #pragma unroll
@@ -557,7 +555,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
             int4 v[8];
             fetch(1, v);
             ok = cluster_all_zero(smem_u32((const void*)&sh_failed), 2 * parts);
-            tmem_ld32(tmem + ((quad * 32) << 16) + c, r);
+            tmem_ld32(sh_tmem + ((quad * 32) << 16) + c, r);
             tmem_wait_ld();
 #pragma unroll 1
             for (uint32_t q = 1; q < parts; ++q) {
@@ -590,7 +588,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         __syncwarp();
         cluster_wait_all();                                // nobody leaves while its sums are being read
     }
-    if (warp == 17) tmem_free<2>(tmem, 2 * kPairTile);
+    if (warp == 17) tmem_free<2>(sh_tmem, 2 * kPairTile);
 }
 
 // ---- few rows: 128 x NT tiles, the contraction split over a cluster ------------------------------------
