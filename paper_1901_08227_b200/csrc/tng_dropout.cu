@@ -58,7 +58,8 @@ __device__ __forceinline__ void drop8(const Raw8<T>& rx, const Raw8<T>& rr, T* p
 // of 1024 columns and up), so that the distances are constants.  Bound by issue slots as much as by memory: a wide
 // multiply takes three of them, 72 slots of Philox for four elements (after the two hoisted ones), so addresses, the row's
 // part of Philox and the walk over (row, segment) are paid once in 32 elements.  16384 x 8192 bf16 with a residual 128 us
-// (6.3 TB/s), 8192 x 8192 fp16 without 56 us (4.8 TB/s).
+// (6.3 TB/s), 8192 x 8192 fp16 without 56 us (4.8 TB/s), both in short bursts; call after call 145 and 59 us at the
+// power-limited clock.
 template <typename T, bool RES, bool WARP>
 __global__ void __launch_bounds__(kThreads, 3) dropout_kernel(const T* x, const T* res, T* y, const __grid_constant__ DropArgs a) {
     constexpr int kVec = 4;
@@ -116,7 +117,7 @@ __global__ void __launch_bounds__(kThreads, 3) dropout_kernel(const T* x, const 
 // bits a lane drew into four ballots; loads and stores then run over the columns lane by lane, so that they are
 // contiguous across the warp wherever the row starts.  (Eight scalar accesses by one thread would touch every sector of
 // the warp's span once an access.)  VEC = 1 has the shortest path for a thread: the one for small arrays.
-// 4097 x 2501 fp32: 20 us, 4.1 TB/s.
+// 4097 x 2501 fp32: 20 us, 4.1 TB/s (16 us with the arrays in the L2 cache).
 template <typename T, bool RES, bool WHOLE>
 __device__ __forceinline__ void drop128(T* py, uint32_t left, uint32_t lane, uint64_t column, const DrawRow& dr, const float (&v)[4], const float (&r)[4], const DropArgs& a) {
     const uint4 w = draw_words(a.draw, dr, column);

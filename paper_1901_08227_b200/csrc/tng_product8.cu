@@ -20,10 +20,10 @@ __device__ __forceinline__ float scaled(int acc, float sa, float sb, bool has_bi
 }
 
 // ---- a linear layer of at most 8 tokens in one launch: the weights are streamed past them -------------------
-// Bound by reading b once (1 x 4096 x 4096 bf16 6.3 us, 8 x 16384 x 2048 11.2 us, launches included).  Every CTA codes the
+// Bound by reading b once (from memory: 1 x 4096 x 4096 bf16 6.5 us, 8 x 16384 x 2048 11.4 us, launches included).  Every CTA codes the
 // tokens itself while its first weights travel, one group of registers a thread: at most 16384 elements with the tokens
-// counted as a power of two.  (Codes by a launch of their own and the tensor-memory kernel below: 7.6 and 10.5 us, and
-// 3.5 us more of the host's time; 8 x 512 x 512 3.5 us against 5.5.)  The tokens' codes stay in shared memory; a CTA goes over tiles of sixteen rows of b, KS warps
+// counted as a power of two.  (Codes by a launch of their own and the tensor-memory kernel below: 9.3 and 12.7 us, and
+// 3.5 us more of the host's time; 8 x 512 x 512 3.3 us against 5.3.)  The tokens' codes stay in shared memory; a CTA goes over tiles of sixteen rows of b, KS warps
 // sharing a tile along the contraction, 256 codes a warp and step: a lane has every fourth 16 bytes of two rows, eight
 // loads of them, the next step's issued before this one's are used.  A warp-wide m16n8k32 instruction takes the weights as
 // its 16 rows straight from the loaded words and the tokens as its 8 columns: the contraction may run in any order as
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2) product8_stream_kernel(cons
 
 // ---- pairs of CTAs: 256 x 256 outputs a tile ------------------------------------------------------------
 // Two CTAs (two SMs) work on one tile: each holds 128 rows of a and 128 rows of b per stage, and the matrix
-// instruction of the even CTA reads both shared memories (8192^3, bf16 out: 334 us, 3290 TOP/s, the tensor pipe 89% busy;
+// instruction of the even CTA reads both shared memories (8192^3, bf16 out: 318 to 334 us, 3290 TOP/s and up, the tensor pipe 88% busy;
 // 390 us once the power limit holds the clock); the accumulators are 128 rows x 256 columns in each
 // CTA's tensor memory, twice, so that one tile is written out while the next is summed.  A stage of 128 codes
 // takes 513 cycles where the instruction rate allows 512 (measured with the feed running); 256 x 128 tiles take 470
@@ -888,7 +888,8 @@ template <typename T> uint64_t resident_clusters(uint32_t split) {
 }
 
 // Tiles that leave pairs idle: split the contraction, four stages of it at least to a part, as long as all clusters run
-// at once (512 x 4096 x 4096, 32 tiles: 18.3 us whole, 15.2 in two parts, 35.1 in four, where clusters of eight queue).
+// at once (512 x 4096 x 4096, 32 tiles: 13.2 us whole, 12.0 in two parts, 29.5 in four, where clusters of eight queue; 200 x
+// 4096 x 4096, 16 tiles: 13.1, 11.0, 19.1).
 template <typename T> uint32_t pair_split(const Product8& p) {
     const uint64_t tiles = (p.m + 255) / 256 * ((p.n + 255) / 256), kblocks = (p.k + 127) / 128;
     uint32_t split = 1;

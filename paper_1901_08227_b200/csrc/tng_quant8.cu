@@ -9,7 +9,7 @@ namespace {
 // ---- rows --------------------------------------------------------------------------------------------
 // blockDim.x threads share a row, blockDim.y rows a CTA (more than one only where a row is one warp).  A thread keeps
 // up to 128 bytes of its row in registers as they came: all its loads are in flight at once, and the row is read once;
-// longer rows (above 1024 threads' worth) are read twice.  16384 x 4096 bf16: 31 us, 6.4 TB/s; drawn 66 to 74 us, bound by
+// longer rows (above 1024 threads' worth) are read twice.  16384 x 4096 bf16: 31 us, 6.4 TB/s; drawn 66 to 77 us, bound by
 // issue slots (26 instructions an element and warp, 10 to nearest).
 template <typename T> constexpr int kHold = 16 / (int)sizeof(T);       // groups of eight elements
 template <typename T, bool VEC, bool DRAW>
@@ -159,8 +159,8 @@ __global__ void __launch_bounds__(256, 4) column_stats_kernel(const __grid_const
 // Codes, transposed.  A CTA owns 64 columns and kRowsPerCta rows, 128 rows at a time: a thread codes 4 rows x 8
 // columns, packs the four rows of a column into a word (rows are contiguous in the output), and the words
 // cross the CTA through shared memory so that a warp writes 128 contiguous bytes of one column.  The next 128
-// rows' loads are issued before that.  Both passes, 16384 x 4096 bf16: 64 us for 403 MB when the second read misses the L2
-// cache; drawn 104 us.
+// rows' loads are issued before that.  Both passes, 16384 x 4096 bf16: 60 to 64 us for 403 MB when the second read misses the
+// L2 cache; drawn 100 to 104 us.
 constexpr int kColTile = 64, kRowTile = 128, kRowsPerCta = 256;
 template <typename T, bool VEC, bool DRAW, bool ROWS>
 __global__ void __launch_bounds__(256, DRAW ? (ROWS ? 2 : 3) : (ROWS ? 3 : 4)) quant8_cols_kernel(const __grid_constant__ ColumnJobs<T> jobs, const __grid_constant__ DrawArgs draw) {
