@@ -406,6 +406,42 @@ tng_status tng_dropout(const void* x_dev, tng_dtype type, uint64_t rows, uint64_
                        const void* residual_dev, uint64_t ldr, float p, const tng_draw* draw, void* y_dev, uint64_t ldy,
                        void* stream);
 
+/* ---- token models: embedding rows and root-mean-square norm ---------------------------------- */
+/* The conventions and error reports of the training-layer operators hold.
+ *
+ * Rows of a table by token: y[t] = table[ids[t]] scale, an fp32 product rounded to `type`.  ids_dev: signed integers of
+ * id_bytes (4 or 8), one a token, aligned to their size.  An id of -1 is an empty place (padding): a row of zeros, and no part in
+ * the gradient.  Any other id outside [0, vocab) gives a row of NaN and takes no part in the gradient.  vocab, tokens and width
+ * are below 2^31. */
+tng_status tng_embed(const void* table_dev, tng_dtype table_type, uint64_t vocab, uint64_t width, uint64_t ldt, const void* ids_dev,
+                     uint32_t id_bytes, uint64_t tokens, float scale, void* y_dev, tng_dtype type, uint64_t ldy, void* stream);
+/* Its gradient: dtable[v] = scale * sum of dy[t] over the t with ids[t] = v, every row of the table written (zeros where no token
+ * names it), so that it can go straight into a worker's row of gradients.  The sums are fp32 in an order that the ids alone decide: the
+ * same inputs give the same bits.  scratch_dev: tng_embed_grad_scratch_bytes, 256-byte aligned.  width <= 2^26. */
+size_t tng_embed_grad_scratch_bytes(uint64_t tokens, uint64_t width);
+tng_status tng_embed_grad(const void* dy_dev, tng_dtype type, uint64_t tokens, uint64_t width, uint64_t lddy, const void* ids_dev,
+                          uint32_t id_bytes, uint64_t vocab, float scale, float* dtable_dev, uint64_t ldd, void* scratch_dev, void* stream);
+
+/* Root-mean-square norm by row, with the residual's addition: h = x + residual (one fp32 sum rounded to `type`; residual_dev may be
+ * NULL: h = x), r = 1/sqrt(mean(h^2) + eps) in fp32, y = (h r) w.  Outputs, each optional (NULL): h, y in `type`; r (a value a row,
+ * which the gradient takes); codes of y by row with a scale (q_dev and scale_dev together), ready for tng_product8.
+ * The codes are unique: with t = h w (one fp32 product) and A = max|t|, q and A/127 are tng_quant8_rows' codes and scale
+ * of t, and scale = (A/127) r: r cancels in q.  Padding is written as by tng_quant8_rows.  w: fp32, one a column.  eps > 0 (normal).
+ * A row whose sum of squares exceeds fp32 has r = 0.  h may be x or the residual itself, y may be x (same stride). */
+tng_status tng_rmsnorm(const void* x_dev, tng_dtype type, uint64_t rows, uint64_t cols, uint64_t ldx, const void* residual_dev, uint64_t ldres,
+                       const float* w_dev, float eps, void* h_dev, uint64_t ldh, void* y_dev, uint64_t ldy, int8_t* q_dev, uint64_t ldq,
+                       float* scale_dev, float* r_dev, void* stream);
+/* Its gradient from dy (with respect to y; the codes' rounding counts as the identity), h and r:
+ *   dx = r (g - h r^2 mean(g h)) + dres, g = dy w     the gradient of x and of the residual alike; dres_dev (may be NULL) is
+ *                                                     what reaches h on its other ways
+ *   dw = sum over the rows of dy h r                  fp32, in a fixed order
+ * each optional (NULL).  dx may be dy or dres itself (same stride).  scratch_dev: tng_rmsnorm_grad_scratch_bytes, 256-byte
+ * aligned, needed for dw alone. */
+size_t tng_rmsnorm_grad_scratch_bytes(uint64_t rows, uint64_t cols);
+tng_status tng_rmsnorm_grad(const void* dy_dev, uint64_t lddy, const void* h_dev, uint64_t ldh, tng_dtype type, uint64_t rows, uint64_t cols,
+                            const float* w_dev, const float* r_dev, const void* dres_dev, uint64_t lddres, void* dx_dev, uint64_t lddx,
+                            float* dw_dev, void* scratch_dev, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

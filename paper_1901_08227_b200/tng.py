@@ -31,6 +31,7 @@ EXPORTS = [
     "tng_selftest_bounded_wait", "tng_fuse_local", "tng_local_stats", "tng_local_stats_all", "tng_fuse_finish", "tng_encode_local", "tng_decode_commit",
     "tng_code_stride", "tng_quant8_rows", "tng_quant8_cols_scratch_bytes", "tng_quant8_cols", "tng_product8", "tng_linear8_scratch_bytes",
     "tng_linear8", "tng_linear8_grad_scratch_bytes", "tng_linear8_grad", "tng_dropout",
+    "tng_embed", "tng_embed_grad_scratch_bytes", "tng_embed_grad", "tng_rmsnorm", "tng_rmsnorm_grad_scratch_bytes", "tng_rmsnorm_grad",
 ]
 
 
@@ -125,6 +126,12 @@ def lib():
         L.tng_linear8_grad_scratch_bytes.argtypes, L.tng_linear8_grad_scratch_bytes.restype = [u64, u64, u64], st
         L.tng_linear8_grad.argtypes = [vp, u64, vp, u64, C.c_int, u64, u64, u64, vp, u64, vp, draw, vp, u64, vp, u64, vp, vp, vp]
         L.tng_dropout.argtypes = [vp, C.c_int, u64, u64, u64, vp, u64, f32, draw, vp, u64, vp]
+        L.tng_embed.argtypes = [vp, C.c_int, u64, u64, u64, vp, u32, u64, f32, vp, C.c_int, u64, vp]
+        L.tng_embed_grad_scratch_bytes.argtypes, L.tng_embed_grad_scratch_bytes.restype = [u64, u64], st
+        L.tng_embed_grad.argtypes = [vp, C.c_int, u64, u64, u64, vp, u32, u64, f32, vp, u64, vp, vp]
+        L.tng_rmsnorm.argtypes = [vp, C.c_int, u64, u64, u64, vp, u64, vp, f32, vp, u64, vp, u64, vp, u64, vp, vp, vp]
+        L.tng_rmsnorm_grad_scratch_bytes.argtypes, L.tng_rmsnorm_grad_scratch_bytes.restype = [u64, u64], st
+        L.tng_rmsnorm_grad.argtypes = [vp, u64, vp, u64, C.c_int, u64, u64, vp, vp, vp, u64, vp, u64, vp, vp, vp]
         L.tng_gram_static.argtypes = [C.POINTER(vp), u32, u64, vp, u32, u64, vp, vp]
         _lib = L
     return _lib
@@ -608,3 +615,123 @@ def dropout(x, p, draw, residual=None, out=None):
 def dropout_grad(dy, p, draw, out=None):
     """Gradient of `dropout` with respect to x (with respect to the residual it is dy itself)."""
     return dropout(dy, p, draw, None, out)
+
+
+# ---- token models -------------------------------------------------------------------------
+_ID_BYTES = {torch.int64: 8, torch.int32: 4}
+
+
+def _ids(t, dev):
+    """Token ids, any shape with contiguous memory -> (pointer, bytes an id, how many)."""
+    if t.get_device() != dev or t.dtype not in _ID_BYTES:
+        raise TypeError("ids must be an int64 or int32 tensor on the current CUDA device")
+    if t.dim() != 1 or (t.shape[0] > 1 and t.stride(0) != 1):
+        raise ValueError("ids must be one-dimensional and contiguous")
+    return t.data_ptr(), _ID_BYTES[t.dtype], t.shape[0]
+
+
+@functools.lru_cache(maxsize=4096)
+def _embed_grad_scratch(tokens, width):
+    return lib().tng_embed_grad_scratch_bytes(tokens, width)
+
+
+@functools.lru_cache(maxsize=4096)
+def _rmsnorm_grad_scratch(rows, cols):
+    return lib().tng_rmsnorm_grad_scratch_bytes(rows, cols)
+
+
+def embed(table, ids, scale=1.0, dtype=None, out=None):
+    """out[t] = table[ids[t]] * scale, in `dtype` (the table's unless given).  An id of -1 is an empty place (a row of zeros); any
+    other id outside the table gives a row of NaN."""
+    dev = _device(table)
+    pt, ldt = _matrix(table, "table", None, None, dev)
+    pi, id_bytes, tokens = _ids(ids, dev)
+    vocab, width = table.shape
+    if out is None:
+        out = table.new_empty((tokens, width), dtype=table.dtype if dtype is None else dtype)
+    elif dtype is not None and out.dtype != dtype:
+        raise TypeError(f"out is {out.dtype}, dtype says {dtype}")
+    po, ldo = _matrix(out, "out", None, (tokens, width), dev)
+    status = lib().tng_embed(pt, _DTYPE[table.dtype], vocab, width, ldt, pi, id_bytes, tokens, scale, po, _DTYPE[out.dtype], ldo, _stream(dev))
+    if status:
+        raise TngError(status, "tng_embed")
+    return out
+
+
+def embed_grad(dy, ids, vocab, scale=1.0, dtable=None, scratch=None):
+    """Gradient of `embed` with respect to the table, (vocab, width) float32, every row written.  `dtable` may be a strided view,
+    such as a part of a worker's row of gradients."""
+    dev = _device(dy)
+    py, ldy = _matrix(dy, "dy", None, None, dev)
+    tokens, width = dy.shape
+    pi, id_bytes, n = _ids(ids, dev)
+    if n != tokens:
+        raise ValueError(f"{n} ids for {tokens} rows of dy")
+    if dtable is None:
+        dtable = dy.new_empty((vocab, width), dtype=torch.float32)
+    pd, ldd = _matrix(dtable, "dtable", torch.float32, (vocab, width), dev)
+    ps, _keep = _scratch(scratch, _embed_grad_scratch(tokens, width), dy)
+    status = lib().tng_embed_grad(py, _DTYPE[dy.dtype], tokens, width, ldy, pi, id_bytes, vocab, scale, pd, ldd, ps, _stream(dev))
+    if status:
+        raise TngError(status, "tng_embed_grad")
+    return dtable
+
+
+def _norm(x, w, eps, residual, h, y, q, scale, r):
+    """Arguments of both norms; the outputs are tensors or None."""
+    dev = _device(x)
+    px, ldx = _matrix(x, "x", None, None, dev)
+    shape, dtype = x.shape, x.dtype
+    rows, cols = shape
+    pr, ldr = (None, 0) if residual is None else _matrix(residual, "residual", dtype, shape, dev)
+    ph, ldh = (None, 0) if h is None else _matrix(h, "h", dtype, shape, dev)
+    py, ldy = (None, 0) if y is None else _matrix(y, "y", dtype, shape, dev)
+    pq, ldq = (None, 0) if q is None else _codes_out(q, "q", shape)
+    status = lib().tng_rmsnorm(px, _DTYPE[dtype], rows, cols, ldx, pr, ldr, _vector(w, "w", cols, dev), eps, ph, ldh, py, ldy, pq, ldq,
+                               _vector(scale, "scale", rows, dev), _vector(r, "r", rows, dev), _stream(dev))
+    if status:
+        raise TngError(status, "tng_rmsnorm")
+
+
+def rmsnorm(x, w, eps=1e-6, residual=None, h=None, y=None, r=None):
+    """(y, h, r): h = x + residual (x itself without one), r = 1/sqrt(mean(h^2) + eps) by row, y = h r w in x's type.  w is float32.
+    `h` may be x's or the residual's own tensor, `y` x's."""
+    if residual is not None and h is None:
+        h = torch.empty_like(x, memory_format=torch.contiguous_format)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format) if y is None else y
+    r = x.new_empty(x.shape[0], dtype=torch.float32) if r is None else r
+    _norm(x, w, eps, residual, h, y, None, None, r)
+    return y, x if h is None else h, r
+
+
+def rmsnorm8(x, w, eps=1e-6, residual=None, h=None, q=None, scale=None, r=None, y=None):
+    """(q, scale, h, r): `rmsnorm` with its output as 8-bit codes by row and a scale per row, as `product8` takes them.  Given a `y`,
+    the rows are written there in x's type too (what `linear8_grad` takes).  A `q` is filled up as by `quant8_rows`."""
+    rows, cols = x.shape
+    if residual is not None and h is None:
+        h = torch.empty_like(x, memory_format=torch.contiguous_format)
+    q = empty_codes(rows, cols, x.device) if q is None else q
+    scale = x.new_empty(rows, dtype=torch.float32) if scale is None else scale
+    r = x.new_empty(rows, dtype=torch.float32) if r is None else r
+    _norm(x, w, eps, residual, h, y, q, scale, r)
+    return q, scale, x if h is None else h, r
+
+
+def rmsnorm_grad(dy, h, w, r, dres=None, dx=None, dw=None, scratch=None):
+    """(dx, dw) of `rmsnorm` and `rmsnorm8` from dy, the gradient of y, with the h and r that they returned.  dx is the gradient of
+    x and of the residual alike; `dres` (what reaches h on its other ways) is added to it.  dx may be dy's or dres's own tensor."""
+    dev = _device(dy)
+    py, ldy = _matrix(dy, "dy", None, None, dev)
+    shape, dtype = dy.shape, dy.dtype
+    rows, cols = shape
+    ph, ldh = _matrix(h, "h", dtype, shape, dev)
+    pr, ldr = (None, 0) if dres is None else _matrix(dres, "dres", dtype, shape, dev)
+    dx = torch.empty_like(dy, memory_format=torch.contiguous_format) if dx is None else dx
+    px, ldx = _matrix(dx, "dx", dtype, shape, dev)
+    dw = dy.new_empty(cols, dtype=torch.float32) if dw is None else dw
+    ps, _keep = _scratch(scratch, _rmsnorm_grad_scratch(rows, cols), dy)
+    status = lib().tng_rmsnorm_grad(py, ldy, ph, ldh, _DTYPE[dtype], rows, cols, _vector(w, "w", cols, dev), _vector(r, "r", rows, dev),
+                                    pr, ldr, px, ldx, _vector(dw, "dw", cols, dev), ps, _stream(dev))
+    if status:
+        raise TngError(status, "tng_rmsnorm_grad")
+    return dx, dw
