@@ -442,6 +442,22 @@ tng_status tng_rmsnorm_grad(const void* dy_dev, uint64_t lddy, const void* h_dev
                             const float* w_dev, const float* r_dev, const void* dres_dev, uint64_t lddres, void* dx_dev, uint64_t lddx,
                             float* dw_dev, void* scratch_dev, void* stream);
 
+/* ---- updates of weight matrices ------------------------------------------------------------ */
+/* Orthogonalised update: out = X after `steps` of X <- (a I + b G + c G^2) X, G = X X^T, from X = V / |V| (Frobenius norm), for
+ * each of `batch` matrices of rows x cols (row stride ldv, `stride` elements from one to the next; the same for out).  Every
+ * step maps each singular value x to a x + b x^3 + c x^5 and leaves the singular vectors as they are, so that suitable coefficients
+ * (3.4445, -4.7750, 2.0315; or 1.875, -1.25, 0.375) bring them all near one.  V may be a part of the aggregate of tng_step.
+ * The products run on the matrix unit with factors of 22 bits and fp32 sums; the result is rounded once to out_type.  A zero
+ * matrix gives zeros, one that is not finite gives NaN throughout; neither touches its neighbours in the batch.
+ * 1 <= steps <= 64; coefficients for which a singular value in (0, 1] could exceed 2, or its factor 15, in any of the steps are
+ * refused (TNG_ERR_INVALID_ARG).  rows, cols < 2^30, batch <= 65535, batch times the rounded-up longer side below 2^31.
+ * out must not overlap v.  scratch_dev: tng_orthogonalize_scratch_bytes, 256-byte aligned.  A bounded wait that gives up shows
+ * as NaN in the outputs. */
+size_t tng_orthogonalize_scratch_bytes(uint64_t batch, uint64_t rows, uint64_t cols);
+tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, uint64_t rows, uint64_t cols, uint64_t ldv, uint64_t stride,
+                             uint32_t steps, float a, float b, float c, void* out_dev, tng_dtype out_type, uint64_t ldo, uint64_t out_stride,
+                             void* scratch_dev, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,8 +1,8 @@
-// Tensor-memory matrix instructions on 8-bit integers, tiled copies and cluster barriers (sm_100a).
+// Tensor-memory matrix instructions on 8-bit integers and 16-bit floats, tiled copies and cluster barriers (sm_100a).
 //
-// Operand tiles are rows of 128 bytes (128 codes of the contraction), copied by TMA with the 128-byte
+// Operand tiles are rows of 128 bytes (128 codes or 64 floats of the contraction), copied by TMA with the 128-byte
 // swizzle: groups of eight rows make 1024-byte atoms, one after the other.  The matrix descriptor names the
-// atom pitch and the swizzle; a step of 32 codes along the contraction moves its start address by 32 bytes.
+// atom pitch and the swizzle; a step of 32 codes (16 floats) along the contraction moves its start address by 32 bytes.
 #pragma once
 
 #include <cuda.h>
@@ -23,6 +23,8 @@ __device__ __forceinline__ uint64_t umma_desc(uint32_t smem) {
 __host__ __device__ constexpr uint32_t umma_idesc_s8(uint32_t m, uint32_t n) {
     return (2u << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
+// kind::f16: fp32 accumulator (1 at bit 4), fp16 A and B (0 at bits 7 and 10), the rest alike.
+__host__ __device__ constexpr uint32_t umma_idesc_f16(uint32_t m, uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((m >> 4) << 24); }
 
 // One instruction: D (+)= A B^T over 32 codes, issued by one thread (of the even CTA with GROUP = 2).
 template <int GROUP>
@@ -36,12 +38,29 @@ __device__ __forceinline__ void umma_s8(uint32_t tmem, uint64_t a, uint64_t b, u
                      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc),
                      "r"((uint32_t)accumulate) : "memory");
 }
+// The same over 16 fp16 values.
+template <int GROUP>
+__device__ __forceinline__ void umma_f16(uint32_t tmem, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    if constexpr (GROUP == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc),
+                     "r"((uint32_t)accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc),
+                     "r"((uint32_t)accumulate) : "memory");
+}
 // Arrive on a barrier when every instruction issued so far is done: this CTA's, or the same one of the CTAs of a mask.
 __device__ __forceinline__ void umma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint16_t ctas) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(ctas) : "memory");
+}
+// umma_commit or umma_commit_pair
+template <int GROUP> __device__ __forceinline__ void umma_commit_all(uint32_t bar, uint16_t ctas) {
+    if constexpr (GROUP == 1) umma_commit(bar);
+    else umma_commit_pair(bar, ctas);
 }
 __device__ __forceinline__ void umma_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void umma_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }

@@ -32,6 +32,7 @@ EXPORTS = [
     "tng_code_stride", "tng_quant8_rows", "tng_quant8_cols_scratch_bytes", "tng_quant8_cols", "tng_product8", "tng_linear8_scratch_bytes",
     "tng_linear8", "tng_linear8_grad_scratch_bytes", "tng_linear8_grad", "tng_dropout",
     "tng_embed", "tng_embed_grad_scratch_bytes", "tng_embed_grad", "tng_rmsnorm", "tng_rmsnorm_grad_scratch_bytes", "tng_rmsnorm_grad",
+    "tng_orthogonalize_scratch_bytes", "tng_orthogonalize",
 ]
 
 
@@ -132,6 +133,8 @@ def lib():
         L.tng_rmsnorm.argtypes = [vp, C.c_int, u64, u64, u64, vp, u64, vp, f32, vp, u64, vp, u64, vp, u64, vp, vp, vp]
         L.tng_rmsnorm_grad_scratch_bytes.argtypes, L.tng_rmsnorm_grad_scratch_bytes.restype = [u64, u64], st
         L.tng_rmsnorm_grad.argtypes = [vp, u64, vp, u64, C.c_int, u64, u64, vp, vp, vp, u64, vp, u64, vp, vp, vp]
+        L.tng_orthogonalize_scratch_bytes.argtypes, L.tng_orthogonalize_scratch_bytes.restype = [u64, u64, u64], st
+        L.tng_orthogonalize.argtypes = [vp, C.c_int, u64, u64, u64, u64, u64, u32, f32, f32, f32, vp, C.c_int, u64, u64, vp, vp]
         L.tng_gram_static.argtypes = [C.POINTER(vp), u32, u64, vp, u32, u64, vp, vp]
         _lib = L
     return _lib
@@ -735,3 +738,43 @@ def rmsnorm_grad(dy, h, w, r, dres=None, dx=None, dw=None, scratch=None):
     if status:
         raise TngError(status, "tng_rmsnorm_grad")
     return dx, dw
+
+
+# ---- updates of weight matrices -------------------------------------------------------------
+@functools.lru_cache(maxsize=4096)
+def _orthogonalize_scratch(batch, rows, cols):
+    return lib().tng_orthogonalize_scratch_bytes(batch, rows, cols)
+
+
+def _matrices(t, name, shape, dev):
+    """One matrix (rows, cols) or a batch (batch, rows, cols), each row contiguous -> (pointer, row stride, stride of the batch)."""
+    if t.get_device() != dev or t.dtype not in _DTYPE:
+        raise TypeError(f"{name} must be a tensor on the current CUDA device of type float32, bfloat16 or float16")
+    if t.dim() not in (2, 3) or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {'two or three dimensions' if shape is None else tuple(shape)}")
+    rows, cols = t.shape[-2:]
+    ld, unit = t.stride()[-2:]
+    if unit != 1 and cols > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), ld if rows > 1 or ld > cols else cols, t.stride(0) if t.dim() == 3 else 0
+
+
+def orthogonalize(v, steps=5, coefficients=(3.4445, -4.7750, 2.0315), dtype=None, out=None, scratch=None):
+    """The orthogonalised update of a matrix (rows, cols), or of each of a batch: X = v / |v| and `steps` times
+    X <- (a I + b G + c G^2) X with G = X X^T, which brings all singular values near one.  `v` may be a view of the aggregate that
+    `Context.step` returns; the result has v's type unless `dtype` or `out` says otherwise."""
+    dev = _device(v)
+    pv, ldv, stride = _matrices(v, "v", None, dev)
+    batch, (rows, cols) = v.shape[0] if v.dim() == 3 else 1, v.shape[-2:]
+    a, b, c = coefficients
+    if out is None:
+        out = v.new_empty(v.shape, dtype=v.dtype if dtype is None else dtype)
+    elif dtype is not None and out.dtype != dtype:
+        raise TypeError(f"out is {out.dtype}, dtype says {dtype}")
+    po, ldo, out_stride = _matrices(out, "out", v.shape, dev)
+    ps, _keep = _scratch(scratch, _orthogonalize_scratch(batch, rows, cols), v)
+    status = lib().tng_orthogonalize(pv, _DTYPE[v.dtype], batch, rows, cols, ldv, stride, steps, a, b, c, po, _DTYPE[out.dtype], ldo, out_stride,
+                                     ps, _stream(dev))
+    if status:
+        raise TngError(status, "tng_orthogonalize")
+    return out
