@@ -652,9 +652,11 @@ def embed(table, ids, scale=1.0, dtype=None, out=None):
     vocab, width = table.shape
     if out is None:
         out = table.new_empty((tokens, width), dtype=table.dtype if dtype is None else dtype)
-    elif dtype is not None and out.dtype != dtype:
-        raise TypeError(f"out is {out.dtype}, dtype says {dtype}")
-    po, ldo = _matrix(out, "out", None, (tokens, width), dev)
+        po, ldo = out.data_ptr(), width
+    else:
+        if dtype is not None and out.dtype != dtype:
+            raise TypeError(f"out is {out.dtype}, dtype says {dtype}")
+        po, ldo = _matrix(out, "out", None, (tokens, width), dev)
     status = lib().tng_embed(pt, _DTYPE[table.dtype], vocab, width, ldt, pi, id_bytes, tokens, scale, po, _DTYPE[out.dtype], ldo, _stream(dev))
     if status:
         raise TngError(status, "tng_embed")
@@ -670,9 +672,7 @@ def embed_grad(dy, ids, vocab, scale=1.0, dtable=None, scratch=None):
     pi, id_bytes, n = _ids(ids, dev)
     if n != tokens:
         raise ValueError(f"{n} ids for {tokens} rows of dy")
-    if dtable is None:
-        dtable = dy.new_empty((vocab, width), dtype=torch.float32)
-    pd, ldd = _matrix(dtable, "dtable", torch.float32, (vocab, width), dev)
+    dtable, pd, ldd = _made(dtable, "dtable", torch.float32, (vocab, width), dev, dy)
     ps, _keep = _scratch(scratch, _embed_grad_scratch(tokens, width), dy)
     status = lib().tng_embed_grad(py, _DTYPE[dy.dtype], tokens, width, ldy, pi, id_bytes, vocab, scale, pd, ldd, ps, _stream(dev))
     if status:
@@ -680,43 +680,71 @@ def embed_grad(dy, ids, vocab, scale=1.0, dtable=None, scratch=None):
     return dtable
 
 
-def _norm(x, w, eps, residual, h, y, q, scale, r):
-    """Arguments of both norms; the outputs are tensors or None."""
+def _made(t, name, dtype, shape, dev, like):
+    """An output (rows, cols) -> (tensor, pointer, row stride): the one given, checked, or a new one, which needs no check."""
+    if t is None:
+        t = like.new_empty(shape, dtype=dtype)
+        return t, t.data_ptr(), shape[1]
+    p, ld = _matrix(t, name, dtype, shape, dev)
+    return t, p, ld
+
+
+def _made_vector(t, name, n, dev, like):
+    if t is None:
+        t = like.new_empty(n, dtype=torch.float32)
+        return t, t.data_ptr()
+    return t, _vector(t, name, n, dev)
+
+
+def _norm_inputs(x, w, residual, h):
+    """What both norms do first -> (dev, dtype, shape, h, pointers and strides of x, residual, w and h)."""
     dev = _device(x)
     px, ldx = _matrix(x, "x", None, None, dev)
-    shape, dtype = x.shape, x.dtype
-    rows, cols = shape
-    pr, ldr = (None, 0) if residual is None else _matrix(residual, "residual", dtype, shape, dev)
-    ph, ldh = (None, 0) if h is None else _matrix(h, "h", dtype, shape, dev)
-    py, ldy = (None, 0) if y is None else _matrix(y, "y", dtype, shape, dev)
-    pq, ldq = (None, 0) if q is None else _codes_out(q, "q", shape)
-    status = lib().tng_rmsnorm(px, _DTYPE[dtype], rows, cols, ldx, pr, ldr, _vector(w, "w", cols, dev), eps, ph, ldh, py, ldy, pq, ldq,
-                               _vector(scale, "scale", rows, dev), _vector(r, "r", rows, dev), _stream(dev))
-    if status:
-        raise TngError(status, "tng_rmsnorm")
+    dtype, shape = x.dtype, x.shape
+    pw = _vector(w, "w", shape[1], dev)
+    if pw is None:
+        raise TypeError("w must be a contiguous float32 vector on the current CUDA device")
+    if residual is None:
+        pr, ldr = None, 0
+        ph, ldh = (None, 0) if h is None else _matrix(h, "h", dtype, shape, dev)
+    else:
+        pr, ldr = _matrix(residual, "residual", dtype, shape, dev)
+        h, ph, ldh = _made(h, "h", dtype, shape, dev, x)
+    return dev, dtype, shape, h, (px, ldx, pr, ldr, pw, ph, ldh)
 
 
 def rmsnorm(x, w, eps=1e-6, residual=None, h=None, y=None, r=None):
     """(y, h, r): h = x + residual (x itself without one), r = 1/sqrt(mean(h^2) + eps) by row, y = h r w in x's type.  w is float32.
     `h` may be x's or the residual's own tensor, `y` x's."""
-    if residual is not None and h is None:
-        h = torch.empty_like(x, memory_format=torch.contiguous_format)
-    y = torch.empty_like(x, memory_format=torch.contiguous_format) if y is None else y
-    r = x.new_empty(x.shape[0], dtype=torch.float32) if r is None else r
-    _norm(x, w, eps, residual, h, y, None, None, r)
+    dev, dtype, shape, h, (px, ldx, pr, ldr, pw, ph, ldh) = _norm_inputs(x, w, residual, h)
+    rows, cols = shape
+    y, py, ldy = _made(y, "y", dtype, shape, dev, x)
+    r, p_r = _made_vector(r, "r", rows, dev, x)
+    status = lib().tng_rmsnorm(px, _DTYPE[dtype], rows, cols, ldx, pr, ldr, pw, eps, ph, ldh, py, ldy, None, 0, None, p_r, _stream(dev))
+    if status:
+        raise TngError(status, "tng_rmsnorm")
     return y, x if h is None else h, r
 
 
 def rmsnorm8(x, w, eps=1e-6, residual=None, h=None, q=None, scale=None, r=None, y=None):
     """(q, scale, h, r): `rmsnorm` with its output as 8-bit codes by row and a scale per row, as `product8` takes them.  Given a `y`,
     the rows are written there in x's type too (what `linear8_grad` takes).  A `q` is filled up as by `quant8_rows`."""
-    rows, cols = x.shape
-    if residual is not None and h is None:
-        h = torch.empty_like(x, memory_format=torch.contiguous_format)
-    q = empty_codes(rows, cols, x.device) if q is None else q
-    scale = x.new_empty(rows, dtype=torch.float32) if scale is None else scale
-    r = x.new_empty(rows, dtype=torch.float32) if r is None else r
-    _norm(x, w, eps, residual, h, y, q, scale, r)
+    dev, dtype, shape, h, (px, ldx, pr, ldr, pw, ph, ldh) = _norm_inputs(x, w, residual, h)
+    rows, cols = shape
+    if q is None:
+        ldq = -(-cols // 16) * 16
+        q = x.new_empty((rows, ldq), dtype=torch.int8)
+        pq = q.data_ptr()
+        if ldq != cols:
+            q = q[:, :cols]
+    else:
+        pq, ldq = _codes_out(q, "q", shape)
+    py, ldy = (None, 0) if y is None else _matrix(y, "y", dtype, shape, dev)
+    scale, ps = _made_vector(scale, "scale", rows, dev, x)
+    r, p_r = _made_vector(r, "r", rows, dev, x)
+    status = lib().tng_rmsnorm(px, _DTYPE[dtype], rows, cols, ldx, pr, ldr, pw, eps, ph, ldh, py, ldy, pq, ldq, ps, p_r, _stream(dev))
+    if status:
+        raise TngError(status, "tng_rmsnorm")
     return q, scale, x if h is None else h, r
 
 
@@ -729,12 +757,11 @@ def rmsnorm_grad(dy, h, w, r, dres=None, dx=None, dw=None, scratch=None):
     rows, cols = shape
     ph, ldh = _matrix(h, "h", dtype, shape, dev)
     pr, ldr = (None, 0) if dres is None else _matrix(dres, "dres", dtype, shape, dev)
-    dx = torch.empty_like(dy, memory_format=torch.contiguous_format) if dx is None else dx
-    px, ldx = _matrix(dx, "dx", dtype, shape, dev)
-    dw = dy.new_empty(cols, dtype=torch.float32) if dw is None else dw
+    dx, px, ldx = _made(dx, "dx", dtype, shape, dev, dy)
+    dw, pdw = _made_vector(dw, "dw", cols, dev, dy)
     ps, _keep = _scratch(scratch, _rmsnorm_grad_scratch(rows, cols), dy)
     status = lib().tng_rmsnorm_grad(py, ldy, ph, ldh, _DTYPE[dtype], rows, cols, _vector(w, "w", cols, dev), _vector(r, "r", rows, dev),
-                                    pr, ldr, px, ldx, _vector(dw, "dw", cols, dev), ps, _stream(dev))
+                                    pr, ldr, px, ldx, pdw, ps, _stream(dev))
     if status:
         raise TngError(status, "tng_rmsnorm_grad")
     return dx, dw

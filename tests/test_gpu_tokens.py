@@ -200,6 +200,17 @@ def test_norm(dtype, rows, cols):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(200000, 128), (40000, 1000), (8192, 4096), (4000, 8192), (2000, 16384)])
+def test_many_codes(dtype, rows, cols):
+    """A product and a sum rounded once instead of twice would change about one code in two million."""
+    x, res, w = normal((rows, cols), dtype, 1), normal((rows, cols), dtype, 2), 1 + normal((cols,), torch.float32, 5, 0.1)
+    q, s, h, r = tng.rmsnorm8(x, w, residual=res)
+    want, scale = tng.quant8_rows(h.float() * w)
+    assert torch.equal(q, want)
+    assert torch.equal(s, scale * r)                        # (an fp32 product)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("cols", [100, 1000, 5000, 20000])
 @pytest.mark.parametrize("lead,pad", [(0, 8), (8, 16), (1, 0), (3, 5), (0, 1)])
 def test_norm_rows_that_start_anywhere(dtype, cols, lead, pad):
