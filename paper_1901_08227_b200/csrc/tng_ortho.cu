@@ -105,14 +105,23 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const T* v, uint64_t l
 }
 
 // ---- products --------------------------------------------------------------------------------------------
-// D = P Q^T of two matrices in halves, contraction along the rows of both.  PAIR: 256 x 256 tiles of two SMs, else 128 x 128 of one:
-// either way a CTA copies 128 rows of each factor, both halves, 64 KB a stage of 64 of the contraction (12 instructions), and
-// three stages are under way.  Warps: 0-15 add up and write out (a quarter of the rows and of the columns each), 16 feeds, 17 issues.
+// D = P Q^T of two matrices in halves, contraction along the rows of both, by pairs of CTAs on two SMs: tiles of 256 x 256 or 256 x 128
+// outputs.  A CTA copies 128 rows of P and half the tile's rows of Q, both halves of them, for a stage of 64 of the contraction (12
+// instructions).  What the instructions read from shared memory and the copies write there is the bound: 106 bytes a cycle of 128 for
+// 256 x 256, and the matrix unit then sets the time (1536 cycles a stage); 158 for 256 x 128 (950 cycles for half the work), so those are
+// for matrices of few tiles.  (128 x 128 tiles of one SM would want 213: measured 1580 cycles.)
+// SPLIT (256 x 128): a cluster of 2 or 4 pairs takes consecutive parts of one tile's contraction; each then adds the others' sums, read
+// from their shared memories, to its own for its share of the columns and writes those out.
+// Warps: 0-15 add up and write out (a quarter of the rows and of the columns each), 16 feeds, 17 issues.
 enum Kind { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
 constexpr int kThreads = 576;
-constexpr uint32_t kBox = 128 * 128, kStage = 4 * kBox, kStages = 3, kStaging = 2048, kBlock = 64, kChunk = 1;
-constexpr uint32_t kSmem = 1024 + kStages * kStage + 16 * kStaging + 256;
-static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
+constexpr uint32_t kBox = 128 * 128, kStages = 3, kBlock = 64, kChunk = 1;
+template <uint32_t COLS> struct Geom {
+    static constexpr uint32_t kQ = COLS / 2 * 128, kStage = 2 * kBox + 2 * kQ, kBuffers = COLS == 256 ? 1 : 2, kStaging = 2048 * kBuffers;
+    static constexpr uint32_t kSmem = 1024 + kStages * kStage + 16 * kStaging + 256;
+    static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
+};
+static_assert(128 * 128 * 4 <= kStages * Geom<128>::kStage, "the stages also hold the sums");
 
 struct OrthoMaps {
     CUtensorMap p[2], q[2], d[2], t[2];   // hi and lo of the factors, of D and of its transpose
@@ -120,31 +129,34 @@ struct OrthoMaps {
 struct OrthoArgs {
     uint64_t rows, cols, k;         // of D, and the contraction
     uint64_t pad_p, pad_q, pad_d, pad_t;   // rows from one matrix of the batch to the next
-    uint32_t batch, symmetric;
+    uint32_t batch, symmetric, split;
     float scale, linear, diagonal;  // D = scale * sum (+ linear * g + diagonal on the diagonal: kPoly)
     Halves g;                       // kPoly: the factor itself
     void* out;                      // kLast
     uint64_t ldo, stride;
 };
 
-// A launch's tiles: by matrix, then by rows of tiles.  Symmetric products: those on and below the diagonal.
+// A launch's tiles, 256 rows by `width` columns: by matrix, then by rows of tiles.  Symmetric products: those that reach below the
+// diagonal; a block of 256 on it is computed whole, what lies left of it is written twice.
 struct Tiles {
-    uint32_t down, across, per, count, symmetric;
-    __device__ __forceinline__ Tiles(const OrthoArgs& a, uint32_t edge) {
-        down = (uint32_t)((a.rows + edge - 1) / edge);
-        across = (uint32_t)((a.cols + edge - 1) / edge);
+    uint32_t down, across, ratio, per, count, symmetric;
+    __device__ __forceinline__ Tiles(const OrthoArgs& a, uint32_t width) {
+        down = (uint32_t)((a.rows + 255) / 256);
+        across = (uint32_t)((a.cols + width - 1) / width);
+        ratio = 256 / width;
         symmetric = a.symmetric;
-        per = symmetric ? down * (down + 1) / 2 : down * across;
+        per = symmetric ? ratio * (down * (down + 1) / 2) - (down * ratio - across) : down * across;
         count = per * a.batch;
     }
     __device__ __forceinline__ void at(uint32_t t, uint32_t& b, uint32_t& tm, uint32_t& tn) const {
         b = t / per;
         t -= b * per;
         if (symmetric) {
-            tm = (uint32_t)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
-            while (tm * (tm + 1) / 2 > t) --tm;
-            while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
-            tn = t - tm * (tm + 1) / 2;
+            const uint32_t u = t / ratio;
+            tm = (uint32_t)((sqrtf(8.f * (float)u + 1.f) - 1.f) * 0.5f);
+            while (tm * (tm + 1) / 2 > u) --tm;
+            while ((tm + 1) * (tm + 2) / 2 <= u) ++tm;
+            tn = t - ratio * (tm * (tm + 1) / 2);
         } else {
             // groups of eight rows of tiles, columns outside: neighbours in time share factors
             const uint32_t band = 8 * across, g = t / band, top = g * 8, high = down - top < 8 ? down - top : 8, r = t - g * band;
@@ -161,9 +173,9 @@ __device__ __forceinline__ float both_halves(float v) {
     split(v, hi, lo);
     return __uint_as_float((uint32_t)__half_as_ushort(hi) << 16 | __half_as_ushort(lo));
 }
-template <bool LO, uint32_t C, uint32_t N>
+template <bool LO, uint32_t C, int BUFFERS, uint32_t N>
 __device__ __forceinline__ void put_rows(const CUtensorMap* map, const float (&v)[N], int32_t x, int32_t y, unsigned char* stage, uint32_t lane) {
-    if (lane == 0) tile_store_wait_read<0>();
+    if (lane == 0) tile_store_wait_read<BUFFERS - 1>();
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -177,9 +189,9 @@ __device__ __forceinline__ void put_rows(const CUtensorMap* map, const float (&v
     if (lane == 0) tile_store(map, x, y, smem_u32(stage));
 }
 // The same transposed: row j of the box is column j, its 32 values the lanes'.
-template <bool LO, uint32_t C, uint32_t N>
+template <bool LO, uint32_t C, int BUFFERS, uint32_t N>
 __device__ __forceinline__ void put_turned(const CUtensorMap* map, const float (&v)[N], int32_t x, int32_t y, unsigned char* stage, uint32_t lane) {
-    if (lane == 0) tile_store_wait_read<0>();
+    if (lane == 0) tile_store_wait_read<BUFFERS - 1>();
     __syncwarp();
 #pragma unroll
     for (uint32_t j = 0; j < 32; ++j) {
@@ -192,7 +204,7 @@ __device__ __forceinline__ void put_turned(const CUtensorMap* map, const float (
 }
 
 // A warp's 32 columns from C of its sums, finished and written: see ortho_product_kernel.
-template <int KIND, typename T, uint32_t C, uint32_t N>
+template <int KIND, typename T, uint32_t C, int BUFFERS, uint32_t N>
 __device__ __forceinline__ void finish(const OrthoMaps& maps, const OrthoArgs& a, float (&sum)[N], uint32_t b, uint64_t row0, uint64_t col, bool mirrored,
                                        unsigned char* stage, uint32_t lane) {
     if (col >= a.cols) return;
@@ -230,31 +242,36 @@ __device__ __forceinline__ void finish(const OrthoMaps& maps, const OrthoArgs& a
             for (uint32_t j = 0; j < 32; ++j) sum[C + j] = both_halves(__fmul_rn(sum[C + j], a.scale));
         }
         const int32_t x = (int32_t)col, y = (int32_t)(b * a.pad_d + row0), xt = (int32_t)row0, yt = (int32_t)(b * a.pad_t + col);
-        put_rows<false, C>(&maps.d[0], sum, x, y, stage, lane);
-        put_rows<true, C>(&maps.d[1], sum, x, y, stage, lane);
+        unsigned char* other = stage + (BUFFERS - 1) * 2048;
+        put_rows<false, C, BUFFERS>(&maps.d[0], sum, x, y, stage, lane);
+        put_rows<true, C, BUFFERS>(&maps.d[1], sum, x, y, other, lane);
         if (mirrored) {
-            put_turned<false, C>(&maps.t[0], sum, xt, yt, stage, lane);
-            put_turned<true, C>(&maps.t[1], sum, xt, yt, stage, lane);
+            put_turned<false, C, BUFFERS>(&maps.t[0], sum, xt, yt, stage, lane);
+            put_turned<true, C, BUFFERS>(&maps.t[1], sum, xt, yt, other, lane);
         }
     }
 }
 
 // T: type of kLast's output.
-template <bool PAIR, int KIND, typename T>
+template <uint32_t COLS, bool SPLIT, int KIND, typename T>
 __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant__ OrthoArgs a) {
-    constexpr int GROUP = PAIR ? 2 : 1;
-    constexpr uint32_t kEdge = PAIR ? 256 : 128, kWide = kEdge / 4;         // columns a warp
+    static_assert(!SPLIT || COLS == 128, "the exchange is laid out for 128 columns");
+    using G = Geom<COLS>;
+    constexpr uint32_t kWide = COLS / 4;                   // columns a warp
     extern __shared__ unsigned char dyn[];
     __shared__ volatile uint32_t sh_tmem, sh_failed;
     const uint32_t data = (smem_u32(dyn) + 1023u) & ~1023u;
-    const uint32_t bars = data + kStages * kStage + 16 * kStaging;
+    unsigned char* stages = dyn + (data - smem_u32(dyn));
+    const uint32_t bars = data + kStages * G::kStage + 16 * G::kStaging;
     const auto full = [&](uint32_t s) { return bars + 16u * s; };
     const auto empty = [&](uint32_t s) { return bars + 16u * s + 8u; };
     const uint32_t acc_full = bars + 16u * kStages, acc_empty = acc_full + 16u, drain = acc_full + 32u, ready = acc_full + 40u;
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = PAIR ? cluster_rank() : 0u;
-    const uint32_t unit = PAIR ? blockIdx.x >> 1 : blockIdx.x, units = PAIR ? gridDim.x >> 1 : gridDim.x;
-    const Tiles tiles(a, kEdge);
-    const uint32_t blocks = (uint32_t)((a.k + kBlock - 1) / kBlock);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, in_cluster = cluster_rank();
+    const uint32_t rank = in_cluster & 1u, even = in_cluster & ~1u;            // the pair's CTA that issues
+    const uint32_t part = SPLIT ? in_cluster >> 1 : 0, parts = SPLIT ? a.split : 1;
+    const uint32_t unit = (blockIdx.x >> 1) / parts, units = (gridDim.x >> 1) / parts;
+    const Tiles tiles(a, COLS);
+    const uint32_t all_blocks = (uint32_t)((a.k + kBlock - 1) / kBlock), first = all_blocks * part / parts, blocks = all_blocks * (part + 1) / parts - first;
 
     if (threadIdx.x == 0) {
         sh_failed = 0;
@@ -264,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
         }
         for (uint32_t i = 0; i < 2; ++i) {
             mbar_init(acc_full + 8 * i, 1);
-            mbar_init(acc_empty + 8 * i, 16 * GROUP);      // sixteen warps of each CTA
+            mbar_init(acc_empty + 8 * i, 32);              // sixteen warps of either CTA
         }
         mbar_init(drain, 1);
         mbar_init(ready, 1);
@@ -275,12 +292,11 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
             map_prefetch(&maps.q[i]);
         }
     }
-    if (PAIR) cluster_sync_all();
-    else __syncthreads();
+    cluster_sync_all();
     grid_wait();
     if (warp == 17) {                                      // tensor memory is taken only now: see the 8-bit products
-        tmem_alloc<GROUP>(smem_u32((const void*)&sh_tmem), 2 * kEdge);
-        if (PAIR && rank == 1 && lane == 0) cluster_arrive(cluster_map(ready, 0));
+        tmem_alloc<2>(smem_u32((const void*)&sh_tmem), 2 * COLS);
+        if (rank == 1 && lane == 0) cluster_arrive(cluster_map(ready, even));
     }
     if (warp != 16) {
         umma_fence_before();
@@ -296,16 +312,16 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
         for (uint32_t t = unit; ok && t < tiles.count; t += units) {
             uint32_t b, tm, tn;
             tiles.at(t, b, tm, tn);
-            const int32_t yp = (int32_t)(b * a.pad_p + tm * kEdge + rank * 128), yq = (int32_t)(b * a.pad_q + tn * kEdge + rank * 128);
-            for (uint32_t kb = 0; kb < blocks; ++kb, ++it) {
+            const int32_t yp = (int32_t)(b * a.pad_p + tm * 256 + rank * 128), yq = (int32_t)(b * a.pad_q + tn * COLS + rank * (COLS / 2));
+            for (uint32_t kb = first; kb < first + blocks; ++kb, ++it) {
                 if (it >= kStages && !mbar_wait(empty(s), parity)) { ok = false; break; }
-                if (rank == 0) mbar_expect_tx(full(s), GROUP * kStage);
-                const uint32_t dst = data + s * kStage, bar = PAIR ? cluster_map(full(s), 0) : full(s);
+                if (rank == 0) mbar_expect_tx(full(s), 2 * G::kStage);
+                const uint32_t dst = data + s * G::kStage, bar = cluster_map(full(s), even);
                 const int32_t x = (int32_t)(kb * kBlock);
-                tile_load<GROUP>(dst, &maps.p[0], x, yp, bar);
-                tile_load<GROUP>(dst + kBox, &maps.p[1], x, yp, bar);
-                tile_load<GROUP>(dst + 2 * kBox, &maps.q[0], x, yq, bar);
-                tile_load<GROUP>(dst + 3 * kBox, &maps.q[1], x, yq, bar);
+                tile_load<2>(dst, &maps.p[0], x, yp, bar);
+                tile_load<2>(dst + kBox, &maps.p[1], x, yp, bar);
+                tile_load<2>(dst + 2 * kBox, &maps.q[0], x, yq, bar);
+                tile_load<2>(dst + 2 * kBox + G::kQ, &maps.q[1], x, yq, bar);
                 if (++s == kStages) { s = 0; parity ^= 1u; }
             }
         }
@@ -320,90 +336,139 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
         }
     } else if (warp == 17 && lane == 0 && rank == 0) {
         // ---- issue
-        constexpr uint32_t idesc = umma_idesc_f16(kEdge, kEdge);
+        constexpr uint32_t idesc = umma_idesc_f16(256, COLS);
+        const uint16_t both = (uint16_t)(3u << even);
         uint32_t s = 0, parity = 0, n_acc = 0;
-        bool ok = !PAIR || mbar_wait(ready, 0);            // the odd CTA has its tensor memory
+        bool ok = mbar_wait(ready, 0);                     // the odd CTA has its tensor memory
         for (uint32_t t = unit; ok && t < tiles.count; t += units) {
             for (uint32_t k0 = 0; ok && k0 < blocks; k0 += kChunk, ++n_acc) {
-                const uint32_t acc = n_acc & 1u, use = n_acc >> 1, into = sh_tmem + acc * kEdge, n = blocks - k0 < kChunk ? blocks - k0 : kChunk;
+                const uint32_t acc = n_acc & 1u, use = n_acc >> 1, into = sh_tmem + acc * COLS, n = blocks - k0 < kChunk ? blocks - k0 : kChunk;
                 if (use > 0 && !mbar_wait(acc_empty + 8 * acc, (use - 1) & 1u)) { ok = false; break; }
                 umma_fence_after();
                 for (uint32_t kb = 0; kb < n; ++kb) {
                     if (!mbar_wait(full(s), parity)) { ok = false; break; }
                     umma_fence_after();
-                    const uint32_t at = data + s * kStage;
-                    const uint64_t ph = umma_desc(at), pl = umma_desc(at + kBox), qh = umma_desc(at + 2 * kBox), ql = umma_desc(at + 3 * kBox);
+                    const uint32_t at = data + s * G::kStage;
+                    const uint64_t ph = umma_desc(at), pl = umma_desc(at + kBox), qh = umma_desc(at + 2 * kBox), ql = umma_desc(at + 2 * kBox + G::kQ);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) umma_f16<GROUP>(into, ph + 2 * j, ql + 2 * j, idesc, kb > 0 || j > 0);
+                    for (int j = 0; j < 4; ++j) umma_f16<2>(into, ph + 2 * j, ql + 2 * j, idesc, kb > 0 || j > 0);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) umma_f16<GROUP>(into, pl + 2 * j, qh + 2 * j, idesc, true);
+                    for (int j = 0; j < 4; ++j) umma_f16<2>(into, pl + 2 * j, qh + 2 * j, idesc, true);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) umma_f16<GROUP>(into, ph + 2 * j, qh + 2 * j, idesc, true);
-                    umma_commit_all<GROUP>(empty(s), 3);
+                    for (int j = 0; j < 4; ++j) umma_f16<2>(into, ph + 2 * j, qh + 2 * j, idesc, true);
+                    umma_commit_pair(empty(s), both);
                     if (++s == kStages) { s = 0; parity ^= 1u; }
                 }
-                if (ok) umma_commit_all<GROUP>(acc_full + 8 * acc, 3);
+                if (ok) umma_commit_pair(acc_full + 8 * acc, both);
             }
         }
         if (!ok) {
             sh_failed = 1;
-            umma_commit_all<GROUP>(drain, 1);
+            umma_commit_pair(drain, (uint16_t)(1u << even));
             (void)mbar_wait(drain, 0);
         }
         // the hand-backs that nothing else waits for come from the other CTA too: they arrive before this one may leave
         for (uint32_t j = n_acc > 2 ? n_acc - 2 : 0; j < n_acc; ++j) (void)mbar_wait(acc_empty + 8 * (j & 1u), (j >> 1) & 1u);
     }
     __syncwarp();
-    if (warp < 16) {
-        // ---- add up and write out: rows 32 quad + lane of this CTA's 128, kWide columns
-        unsigned char* stage = dyn + (data - smem_u32(dyn)) + kStages * kStage + warp * kStaging;
-        const uint32_t quad = warp & 3, group = warp >> 2;
-        uint32_t n_acc = 0;
-        bool ok = true;
-        for (uint32_t t = unit; t < tiles.count; t += units) {
-            uint32_t b, tm, tn;
-            tiles.at(t, b, tm, tn);
-            const uint64_t row0 = (uint64_t)tm * kEdge + rank * 128 + quad * 32, col0 = (uint64_t)tn * kEdge + group * kWide;
-            float sum[kWide];
-            for (uint32_t k0 = 0; k0 < blocks; k0 += kChunk, ++n_acc) {
-                const uint32_t acc = n_acc & 1u, use = n_acc >> 1;
-                if (ok && !mbar_wait(acc_full + 8 * acc, use & 1u)) ok = false;
-                ok = __all_sync(kFullMask, ok && !sh_failed);
-                umma_fence_after();
-                if (ok) {
+    unsigned char* stage = stages + kStages * G::kStage + warp * G::kStaging;
+    const uint32_t quad = warp & 3, group = warp >> 2, row_in = rank * 128 + quad * 32;
+    uint32_t n_acc = 0;
+    bool ok = true;
+    // A tile's sums, chunk by chunk as they come; a failure hands nothing back and shows as NaN.
+    float sum[kWide];
+    const auto add_up = [&] {
+        for (uint32_t k0 = 0; k0 < blocks; k0 += kChunk, ++n_acc) {
+            const uint32_t acc = n_acc & 1u, use = n_acc >> 1;
+            if (ok && !mbar_wait(acc_full + 8 * acc, use & 1u)) ok = false;
+            ok = __all_sync(kFullMask, ok && !sh_failed);
+            umma_fence_after();
+            if (!ok) continue;
 #pragma unroll
-                    for (uint32_t c = 0; c < kWide; c += 16) {
-                        uint32_t r[16];
-                        tmem_ld16(sh_tmem + ((quad * 32) << 16) + acc * kEdge + group * kWide + c, r);
-                        tmem_wait_ld();
-                        if (k0 == 0) {
+            for (uint32_t c = 0; c < kWide; c += 16) {
+                uint32_t r[16];
+                tmem_ld16(sh_tmem + ((quad * 32) << 16) + acc * COLS + group * kWide + c, r);
+                tmem_wait_ld();
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) sum[c + j] = __uint_as_float(r[j]);
-                        } else {
+                for (int j = 0; j < 16; ++j) sum[c + j] = k0 == 0 ? __uint_as_float(r[j]) : __fadd_rn(sum[c + j], __uint_as_float(r[j]));
+            }
+            umma_fence_before();
+            __syncwarp();
+            if (lane == 0) cluster_arrive(cluster_map(acc_empty + 8 * acc, even));
+        }
+    };
+    if constexpr (!SPLIT) {
+        if (warp < 16) {
+            for (uint32_t t = unit; t < tiles.count; t += units) {
+                uint32_t b, tm, tn;
+                tiles.at(t, b, tm, tn);
+                const uint64_t row0 = (uint64_t)tm * 256 + row_in, col0 = (uint64_t)tn * COLS + group * kWide;
+                add_up();
+                if (!ok) {
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) sum[c + j] = __fadd_rn(sum[c + j], __uint_as_float(r[j]));
-                        }
-                    }
-                    umma_fence_before();
-                    __syncwarp();
-                    if (lane == 0) cluster_arrive(cluster_map(acc_empty + 8 * acc, 0));    // (a failure hands nothing back)
+                    for (uint32_t j = 0; j < kWide; ++j) sum[j] = CUDART_NAN_F;
+                }
+                if (row0 >= a.rows) continue;
+                const bool mirrored = KIND == kApply || tn < tiles.ratio * tm;
+                finish<KIND, T, 0, G::kBuffers>(maps, a, sum, b, row0, col0, mirrored, stage, lane);
+                if constexpr (COLS == 256) finish<KIND, T, 32, G::kBuffers>(maps, a, sum, b, row0, col0 + 32, mirrored, stage, lane);
+            }
+            if (KIND != kLast && lane == 0) tile_store_wait_all();
+        }
+        __syncwarp();
+        __syncthreads();
+        cluster_meet_all();                                // the odd CTA's memory is read until the last instruction of the even one
+    } else {
+        // ---- one tile: leave the other pairs their columns in shared memory, then add up and write out one's own
+        const uint32_t cols = 128 / parts, mine = part * cols;
+        float4* sums = reinterpret_cast<float4*>(stages);  // [four columns][row]: a warp's access is contiguous; every copy has
+        uint32_t b, tm, tn;                                // landed and every instruction has read its operands
+        tiles.at(unit, b, tm, tn);
+        const uint64_t row0 = (uint64_t)tm * 256 + row_in, col0 = (uint64_t)tn * COLS + group * 32;
+        const bool own = warp < 16 && group * 32 >= mine && group * 32 < mine + cols && row0 < a.rows && col0 < a.cols;
+        if (warp < 16) {
+            add_up();
+            if (!ok) sh_failed = 1;
+            if (group * 32 < mine || group * 32 >= mine + cols) {
+                float4* to = sums + group * 8 * 128 + quad * 32 + lane;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) to[j * 128] = make_float4(sum[4 * j], sum[4 * j + 1], sum[4 * j + 2], sum[4 * j + 3]);
+            }
+        }
+        __syncwarp();
+        cluster_sync_all();
+        if (own) {
+            const uint32_t from = data + (group * 8 * 128 + quad * 32 + lane) * 16;
+            ok = cluster_all_zero(smem_u32((const void*)&sh_failed), 2 * parts);
+#pragma unroll 1
+            for (uint32_t q = 1; q < parts; ++q) {         // (in the same order each time, not in that of the parts)
+                const uint32_t at = cluster_map(from, ((part + q) & (parts - 1)) * 2 + rank);
+                int4 v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = cluster_ld4(at + j * 2048);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    sum[4 * j] = __fadd_rn(sum[4 * j], __int_as_float(v[j].x));
+                    sum[4 * j + 1] = __fadd_rn(sum[4 * j + 1], __int_as_float(v[j].y));
+                    sum[4 * j + 2] = __fadd_rn(sum[4 * j + 2], __int_as_float(v[j].z));
+                    sum[4 * j + 3] = __fadd_rn(sum[4 * j + 3], __int_as_float(v[j].w));
                 }
             }
+        }
+        __syncwarp();
+        cluster_arrive_all();                              // done with the others' sums
+        if (own) {
             if (!ok) {
 #pragma unroll
                 for (uint32_t j = 0; j < kWide; ++j) sum[j] = CUDART_NAN_F;
             }
-            if (row0 >= a.rows) continue;
-            const bool mirrored = KIND == kApply || tm != tn;
-            finish<KIND, T, 0>(maps, a, sum, b, row0, col0, mirrored, stage, lane);
-            if constexpr (PAIR) finish<KIND, T, 32>(maps, a, sum, b, row0, col0 + 32, mirrored, stage, lane);
+            finish<KIND, T, 0, G::kBuffers>(maps, a, sum, b, row0, col0, KIND == kApply || tn < tiles.ratio * tm, stage, lane);
+            if (KIND != kLast && lane == 0) tile_store_wait_all();
         }
-        if (KIND != kLast && lane == 0) tile_store_wait_all();
+        __syncwarp();
+        cluster_wait_all();                                // nobody leaves while its sums are being read
     }
-    __syncwarp();
-    __syncthreads();
-    if (PAIR) cluster_meet_all();                          // the odd CTA's memory is read until the last instruction of the even one
-    if (warp == 17) tmem_free<GROUP>(sh_tmem, 2 * kEdge);
+    if (warp == 17) tmem_free<2>(sh_tmem, 2 * COLS);
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -422,40 +487,54 @@ EncodeTiled encode_tiled() {
     }();
     return fn;
 }
-// The batch's matrices one below the other; boxes to load are 64 columns x 128 rows, boxes to store 32 x 32.
-bool make_map(CUtensorMap* map, const __half* m, const Halves& h, uint64_t batch, bool load) {
+// The batch's matrices one below the other; boxes to load are 64 columns x `load` rows, boxes to store (load = 0) 32 x 32.
+bool make_map(CUtensorMap* map, const __half* m, const Halves& h, uint64_t batch, uint32_t load) {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
     const cuuint64_t dims[2] = {h.cols, h.pad_rows * batch}, strides[1] = {h.ld * 2};
-    const cuuint32_t boxes[2] = {load ? 64u : 32u, load ? 128u : 32u}, steps[2] = {1, 1};
+    const cuuint32_t boxes[2] = {load ? 64u : 32u, load ? load : 32u}, steps[2] = {1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half*>(m), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   load ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, load ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_NONE,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-bool make_maps(CUtensorMap (&maps)[2], const Halves& h, uint64_t batch, bool load) {
+bool make_maps(CUtensorMap (&maps)[2], const Halves& h, uint64_t batch, uint32_t load) {
     return make_map(&maps[0], h.hi, h, batch, load) && make_map(&maps[1], h.lo, h, batch, load);
 }
 
-template <bool PAIR, int KIND, typename T> cudaError_t launch_product_as(const OrthoMaps& maps, const OrthoArgs& a, cudaStream_t st) {
+template <uint32_t COLS, bool SPLIT, int KIND, typename T> cudaError_t launch_product_as(const OrthoMaps& maps, const OrthoArgs& a, uint64_t tiles, cudaStream_t st) {
     static PerDevice<bool> done;
-    const auto kernel = ortho_product_kernel<PAIR, KIND, T>;
+    const auto kernel = ortho_product_kernel<COLS, SPLIT, KIND, T>;
     const int slot = device_slot();
     if (slot < 0 || !done.v[slot]) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Geom<COLS>::kSmem);
         if (e != cudaSuccess) return e;
         if (slot >= 0) done.v[slot] = true;
     }
-    const uint64_t edge = PAIR ? 256 : 128, down = (a.rows + edge - 1) / edge, across = (a.cols + edge - 1) / edge;
-    const uint64_t tiles = a.batch * (a.symmetric ? down * (down + 1) / 2 : down * across), most = (uint64_t)sm_count_now() / (PAIR ? 2 : 1);
-    return launch_layer(kernel, (unsigned)((tiles < most ? tiles : most) * (PAIR ? 2 : 1)), kThreads, kSmem, PAIR ? 2 : 1, st, maps, a);
+    const uint64_t pairs = (uint64_t)sm_count_now() / 2, units = SPLIT ? tiles * a.split : tiles < pairs ? tiles : pairs;
+    return launch_layer(kernel, (unsigned)(2 * units), kThreads, Geom<COLS>::kSmem, 2 * a.split, st, maps, a);
 }
-// Which tiles: large ones where they keep the pairs busy.
-bool takes_pairs(const OrthoArgs& a) {
-    const uint64_t down = (a.rows + 255) / 256, across = (a.cols + 255) / 256;
-    return a.batch * (a.symmetric ? down * (down + 1) / 2 : down * across) >= (uint64_t)sm_count_now() / 2;
+uint64_t count_tiles(uint64_t batch, uint64_t rows, uint64_t cols, bool symmetric, uint64_t width) {
+    const uint64_t down = (rows + 255) / 256, across = (cols + width - 1) / width, ratio = 256 / width;
+    return batch * (symmetric ? ratio * (down * (down + 1) / 2) - (down * ratio - across) : down * across);
 }
-template <int KIND, typename T> cudaError_t launch_product(const OrthoMaps& maps, const OrthoArgs& a, cudaStream_t st) {
-    return takes_pairs(a) ? launch_product_as<true, KIND, T>(maps, a, st) : launch_product_as<false, KIND, T>(maps, a, st);
+// How a product is cut.
+struct Cut {
+    uint32_t width, split;
+    uint64_t tiles;
+};
+// The tiles whose waves over the pairs take less time (1536 and 950 cycles a block of the contraction); narrow ones that leave pairs idle
+// have their contraction split, two blocks at least to a part, as long as all clusters run at once (counted on a B200: 74 pairs, 33
+// clusters of two, 16 of four).
+Cut cut_product(uint64_t batch, uint64_t rows, uint64_t cols, uint64_t k, bool symmetric) {
+    const uint64_t pairs = (uint64_t)sm_count_now() / 2, blocks = (k + kBlock - 1) / kBlock;
+    const uint64_t wide = count_tiles(batch, rows, cols, symmetric, 256), narrow = count_tiles(batch, rows, cols, symmetric, 128);
+    if ((wide + pairs - 1) / pairs * 1536 <= (narrow + pairs - 1) / pairs * 950) return {256, 1, wide};
+    const uint32_t split = narrow <= 16 && blocks >= 8 ? 4 : narrow <= 33 && blocks >= 4 ? 2 : 1;
+    return {128, split, narrow};
+}
+template <int KIND, typename T> cudaError_t launch_product(const OrthoMaps& maps, const OrthoArgs& a, const Cut& cut, cudaStream_t st) {
+    if (cut.width == 256) return launch_product_as<256, false, KIND, T>(maps, a, cut.tiles, st);
+    return cut.split > 1 ? launch_product_as<128, true, KIND, T>(maps, a, cut.tiles, st) : launch_product_as<128, false, KIND, T>(maps, a, cut.tiles, st);
 }
 
 uint64_t up(uint64_t n, uint64_t to) { return (n + to - 1) / to * to; }
@@ -529,7 +608,7 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
     double* part = reinterpret_cast<double*>(at);
     Carver carve{at + batch * kNormBlocks * 8};
     const Halves x = carve.take(batch, s, l), g = carve.take(batch, s, s), poly = carve.take(batch, s, s);
-    Halves xt = carve.take(batch, l, s), xt2 = carve.take(batch, l, s);
+    const Halves xt = carve.take(batch, l, s), xt2 = carve.take(batch, l, s);
     const bool tall = rows > cols;
     cudaError_t e = with_type(type, [&](auto t) {
         using T = decltype(t);
@@ -540,64 +619,55 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
         return launch_layer(ortho_split_kernel<T>, grid, 256, 0, 1, st, v, ldv, stride, static_cast<const double*>(part), tall ? xt : x, tall ? x : xt);
     });
     if (e != cudaSuccess) return layer_status(e);
-    OrthoMaps gram = {}, square = {}, apply = {};
-    bool made = make_maps(gram.p, x, batch, true) && make_maps(gram.d, g, batch, false) && make_maps(square.p, g, batch, true) &&
-                make_maps(square.d, poly, batch, false) && make_maps(apply.d, x, batch, false);
-    for (int i = 0; i < 2; ++i) {
-        gram.q[i] = gram.p[i];
-        gram.t[i] = gram.d[i];
-        square.q[i] = square.p[i];
-        square.t[i] = square.d[i];
-    }
-    OrthoMaps next = apply;
-    made = made && make_maps(apply.p, poly, batch, true) && make_maps(apply.q, xt, batch, true) && make_maps(apply.t, xt2, batch, false) &&
-           make_maps(next.q, xt2, batch, true) && make_maps(next.t, xt, batch, false);
-    if (!made) return TNG_ERR_CUDA;
-    next.p[0] = apply.p[0];
-    next.p[1] = apply.p[1];
-    OrthoArgs args = {};
-    args.batch = (uint32_t)batch;
+    // The products of a step: G = X X^T, B from G, X <- B X (the last one as the output lies: B X, or X^T B).
+    const Cut cut_gram = cut_product(batch, s, s, l, true), cut_poly = cut_product(batch, s, s, s, true);
+    const Cut cut_apply = cut_product(batch, s, l, s, false), cut_last = cut_product(batch, rows, cols, s, false);
+    const auto maps_of = [&](OrthoMaps& m, const Cut& cut, const Halves& p, const Halves& q, const Halves* d, const Halves* t) {
+        return make_maps(m.p, p, batch, 128) && make_maps(m.q, q, batch, cut.width / 2) && (!d || (make_maps(m.d, *d, batch, 0) && make_maps(m.t, *t, batch, 0)));
+    };
+    OrthoMaps gram = {}, square = {}, apply[2] = {}, last = {};
+    const Halves& xt_last = (steps - 1) & 1 ? xt2 : xt;
+    if (!maps_of(gram, cut_gram, x, x, &g, &g) || !maps_of(square, cut_poly, g, g, &poly, &poly) ||
+        (steps > 1 && !maps_of(apply[0], cut_apply, poly, xt, &x, &xt2)) || (steps > 2 && !maps_of(apply[1], cut_apply, poly, xt2, &x, &xt)) ||
+        !(tall ? maps_of(last, cut_last, xt_last, poly, nullptr, nullptr) : maps_of(last, cut_last, poly, xt_last, nullptr, nullptr)))
+        return TNG_ERR_CUDA;
+    OrthoArgs square_args = {};                            // of both symmetric products
+    square_args.batch = (uint32_t)batch;
+    square_args.rows = square_args.cols = s;
+    square_args.pad_p = square_args.pad_q = square_args.pad_d = square_args.pad_t = x.pad_rows;
+    square_args.symmetric = 1;
+    square_args.g = g;
     for (uint32_t i = 0; i < steps; ++i) {
-        const OrthoMaps& here = i & 1 ? next : apply;
-        args.rows = args.cols = s;
+        OrthoArgs args = square_args;
+        args.split = cut_gram.split;
         args.k = l;
-        args.pad_p = args.pad_q = args.pad_d = args.pad_t = x.pad_rows;
-        args.symmetric = 1;
         args.scale = kScaleG / (kScaleX * kScaleX);
-        e = launch_product<kGram, float>(gram, args, st);
+        e = launch_product<kGram, float>(gram, args, cut_gram, st);
         if (e != cudaSuccess) return layer_status(e);
+        args.split = cut_poly.split;
         args.k = s;
-        args.g = g;
         args.scale = c * (kScaleB / (kScaleG * kScaleG));
         args.linear = b * (kScaleB / kScaleG);
         args.diagonal = a * kScaleB;
-        e = launch_product<kPoly, float>(square, args, st);
+        e = launch_product<kPoly, float>(square, args, cut_poly, st);
         if (e != cudaSuccess) return layer_status(e);
         args.symmetric = 0;
         if (i + 1 < steps) {
+            args.split = cut_apply.split;
             args.cols = l;
             args.pad_q = args.pad_t = xt.pad_rows;
-            args.scale = kScaleX / (kScaleB * kScaleX);
-            e = launch_product<kApply, float>(here, args, st);
+            args.scale = 1.f / kScaleB;
+            e = launch_product<kApply, float>(apply[i & 1], args, cut_apply, st);
         } else {
-            // the last one as the output lies: B X, or X^T B
-            OrthoMaps last = here;
-            if (tall) {
-                for (int j = 0; j < 2; ++j) {
-                    last.p[j] = here.q[j];
-                    last.q[j] = here.p[j];
-                }
-                args.pad_p = xt.pad_rows;
-            } else {
-                args.pad_q = xt.pad_rows;
-            }
+            args.split = cut_last.split;
             args.rows = rows;
             args.cols = cols;
+            (tall ? args.pad_p : args.pad_q) = xt.pad_rows;
             args.scale = 1.f / (kScaleB * kScaleX);
             args.out = out_dev;
             args.ldo = ldo;
             args.stride = out_stride;
-            e = with_type(out_type, [&](auto t) { return launch_product<kLast, decltype(t)>(last, args, st); });
+            e = with_type(out_type, [&](auto t) { return launch_product<kLast, decltype(t)>(last, args, cut_last, st); });
         }
         if (e != cudaSuccess) return layer_status(e);
     }
