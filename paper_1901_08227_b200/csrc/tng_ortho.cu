@@ -35,18 +35,24 @@ struct Halves {
 // ---- |V| and its two halves --------------------------------------------------------------------------------
 // The sum of squares in 64 bits (no overflow, no underflow, and its rounding does not show), each block's share on its own.
 constexpr uint32_t kNormBlocks = 128;
+constexpr int kNormThreads = 512;
 template <typename T>
-__global__ void __launch_bounds__(256) ortho_norm_kernel(const T* v, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t stride, double* part) {
-    __shared__ double sh[8];
+__global__ void __launch_bounds__(kNormThreads) ortho_norm_kernel(const T* v, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t stride, double* part) {
+    __shared__ double sh[kNormThreads / 32];
     grid_wait();
     grid_go();
     v += blockIdx.y * stride;
     double s = 0.0;
-    for (uint64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    constexpr int kAhead = 8;
+    // a warp has a row at a time, eight loads a lane under way
+    for (uint64_t r = (uint64_t)(threadIdx.x >> 5) * gridDim.x + blockIdx.x; r < rows; r += (uint64_t)(kNormThreads / 32) * gridDim.x) {
         const T* row = v + r * ld;
-        for (uint64_t c = threadIdx.x; c < cols; c += 256) {
-            const double e = (double)to_f32(row[c]);
-            s += e * e;
+        for (uint64_t c = threadIdx.x & 31; c < cols; c += 32 * kAhead) {
+            float e[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) e[i] = c + 32 * i < cols ? to_f32(row[c + 32 * i]) : 0.f;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) s += (double)e[i] * (double)e[i];
         }
     }
 #pragma unroll
@@ -54,7 +60,7 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const T* v, uint64_t ro
     if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) s += sh[i];
+        for (int i = 1; i < kNormThreads / 32; ++i) s += sh[i];
         part[blockIdx.y * kNormBlocks + blockIdx.x] = s;
     }
 }
@@ -64,42 +70,47 @@ __device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
     lo = __float2half_rn(__fsub_rn(v, __half2float(hi)));
 }
 
-// V / |V| in two halves, as it lies and transposed.  A block has 64 x 64 elements.
+// V / |V| in two halves, as it lies and transposed.  A block has 64 x 64 elements; they leave in pairs (rows are padded to 64).
 template <typename T>
 __global__ void __launch_bounds__(256) ortho_split_kernel(const T* v, uint64_t ld, uint64_t stride, const double* part, const __grid_constant__ Halves as,
                                                           const __grid_constant__ Halves turned) {
     __shared__ __half hi[64][66], lo[64][66];
-    __shared__ double total[8];
+    __shared__ double total[4];
     grid_wait();
     grid_go();
     const uint32_t b = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint64_t r0 = (uint64_t)blockIdx.y * 64, c0 = (uint64_t)blockIdx.x * 64;
+    v += b * stride;
+    float e[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const uint64_t r = r0 + (threadIdx.x >> 6) + 4 * k, c = c0 + (threadIdx.x & 63);
+        e[k] = r < as.rows && c < as.cols ? to_f32(v[r * ld + c]) : 0.f;
+    }
+    static_assert(kNormBlocks == 128, "four warps add up the shares");
     double s = threadIdx.x < kNormBlocks ? part[b * kNormBlocks + threadIdx.x] : 0.0;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(kFullMask, s, d);
-    if (lane == 0) total[warp] = s;
+    if (lane == 0 && warp < 4) total[warp] = s;
     __syncthreads();
     const double norm = sqrt((total[0] + total[1]) + (total[2] + total[3]));
     // (a norm that is not finite makes all of the matrix NaN, a zero one leaves it zero)
     const double f = norm == 0.0 ? 0.0 : norm < (double)CUDART_INF ? (double)kScaleX / norm : (double)CUDART_NAN_F;
-    const uint64_t r0 = (uint64_t)blockIdx.y * 64, c0 = (uint64_t)blockIdx.x * 64;
-    v += b * stride;
-    for (uint32_t i = threadIdx.x; i < 4096; i += 256) {
-        const uint64_t r = r0 + (i >> 6), c = c0 + (i & 63);
-        const float e = r < as.rows && c < as.cols ? (float)((double)to_f32(v[r * ld + c]) * f) : 0.f;
-        split(e, hi[i >> 6][i & 63], lo[i >> 6][i & 63]);
-    }
+#pragma unroll
+    for (int k = 0; k < 16; ++k) split((float)((double)e[k] * f), hi[(threadIdx.x >> 6) + 4 * k][threadIdx.x & 63], lo[(threadIdx.x >> 6) + 4 * k][threadIdx.x & 63]);
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < 4096; i += 256) {
-        const uint32_t p = i >> 6, q = i & 63;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t p = (threadIdx.x >> 5) + 8 * k, q = 2 * lane;
         if (r0 + p < as.rows && c0 + q < as.cols) {
             const uint64_t at = (b * as.pad_rows + r0 + p) * as.ld + c0 + q;
-            as.hi[at] = hi[p][q];
-            as.lo[at] = lo[p][q];
+            *reinterpret_cast<__half2*>(as.hi + at) = __halves2half2(hi[p][q], hi[p][q + 1]);
+            *reinterpret_cast<__half2*>(as.lo + at) = __halves2half2(lo[p][q], lo[p][q + 1]);
         }
         if (c0 + p < turned.rows && r0 + q < turned.cols) {
             const uint64_t at = (b * turned.pad_rows + c0 + p) * turned.ld + r0 + q;
-            turned.hi[at] = hi[q][p];
-            turned.lo[at] = lo[q][p];
+            *reinterpret_cast<__half2*>(turned.hi + at) = __halves2half2(hi[q][p], hi[q + 1][p]);
+            *reinterpret_cast<__half2*>(turned.lo + at) = __halves2half2(lo[q][p], lo[q + 1][p]);
         }
     }
 }
@@ -116,12 +127,13 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const T* v, uint64_t l
 enum Kind { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
 constexpr int kThreads = 576;
 constexpr uint32_t kBox = 128 * 128, kStages = 3, kBlock = 64, kChunk = 1;
-template <uint32_t COLS> struct Geom {
-    static constexpr uint32_t kQ = COLS / 2 * 128, kStage = 2 * kBox + 2 * kQ, kBuffers = COLS == 256 ? 1 : 2, kStaging = 2048 * kBuffers;
-    static constexpr uint32_t kSmem = 1024 + kStages * kStage + 16 * kStaging + 256;
+// Staging of the output: buffers of 2 KB, 4 a warp where at most eight warps write (SPLIT).
+template <uint32_t COLS, bool SPLIT> struct Geom {
+    static constexpr uint32_t kQ = COLS / 2 * 128, kStage = 2 * kBox + 2 * kQ, kBuffers = COLS == 256 ? 1 : SPLIT ? 4 : 2, kStaging = 2048 * kBuffers;
+    static constexpr uint32_t kSmem = 1024 + kStages * kStage + (SPLIT ? 8 : 16) * kStaging + 256;
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
-static_assert(128 * 128 * 4 <= kStages * Geom<128>::kStage, "the stages also hold the sums");
+static_assert(128 * 128 * 4 <= kStages * Geom<128, true>::kStage, "the stages also hold the sums");
 
 struct OrthoMaps {
     CUtensorMap p[2], q[2], d[2], t[2];   // hi and lo of the factors, of D and of its transpose
@@ -226,7 +238,7 @@ __device__ __forceinline__ void finish(const OrthoMaps& maps, const OrthoArgs& a
         if constexpr (KIND == kPoly) {
             const uint64_t at = (b * a.g.pad_rows + row0 + lane) * a.g.ld + col;
 #pragma unroll
-            for (uint32_t i = 0; i < 32; i += 8) {
+            for (uint32_t i = 0; i < 32; i += 8) {         // (loads ahead of the sums: no faster, and more spills)
                 const bool in = row0 + lane < a.rows && col + i < a.cols;
                 const uint4 zero = make_uint4(0u, 0u, 0u, 0u), h = in ? load16(a.g.hi + at + i) : zero, l = in ? load16(a.g.lo + at + i) : zero;
                 const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
@@ -242,12 +254,12 @@ __device__ __forceinline__ void finish(const OrthoMaps& maps, const OrthoArgs& a
             for (uint32_t j = 0; j < 32; ++j) sum[C + j] = both_halves(__fmul_rn(sum[C + j], a.scale));
         }
         const int32_t x = (int32_t)col, y = (int32_t)(b * a.pad_d + row0), xt = (int32_t)row0, yt = (int32_t)(b * a.pad_t + col);
-        unsigned char* other = stage + (BUFFERS - 1) * 2048;
-        put_rows<false, C, BUFFERS>(&maps.d[0], sum, x, y, stage, lane);
-        put_rows<true, C, BUFFERS>(&maps.d[1], sum, x, y, other, lane);
+        const auto buffer = [&](int i) { return stage + (i & (BUFFERS - 1)) * 2048; };
+        put_rows<false, C, BUFFERS>(&maps.d[0], sum, x, y, buffer(0), lane);
+        put_rows<true, C, BUFFERS>(&maps.d[1], sum, x, y, buffer(1), lane);
         if (mirrored) {
-            put_turned<false, C, BUFFERS>(&maps.t[0], sum, xt, yt, stage, lane);
-            put_turned<true, C, BUFFERS>(&maps.t[1], sum, xt, yt, other, lane);
+            put_turned<false, C, BUFFERS>(&maps.t[0], sum, xt, yt, buffer(2), lane);
+            put_turned<true, C, BUFFERS>(&maps.t[1], sum, xt, yt, buffer(3), lane);
         }
     }
 }
@@ -256,13 +268,13 @@ __device__ __forceinline__ void finish(const OrthoMaps& maps, const OrthoArgs& a
 template <uint32_t COLS, bool SPLIT, int KIND, typename T>
 __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant__ OrthoArgs a) {
     static_assert(!SPLIT || COLS == 128, "the exchange is laid out for 128 columns");
-    using G = Geom<COLS>;
+    using G = Geom<COLS, SPLIT>;
     constexpr uint32_t kWide = COLS / 4;                   // columns a warp
     extern __shared__ unsigned char dyn[];
     __shared__ volatile uint32_t sh_tmem, sh_failed;
     const uint32_t data = (smem_u32(dyn) + 1023u) & ~1023u;
     unsigned char* stages = dyn + (data - smem_u32(dyn));
-    const uint32_t bars = data + kStages * G::kStage + 16 * G::kStaging;
+    const uint32_t bars = data + G::kSmem - 1024 - 256;
     const auto full = [&](uint32_t s) { return bars + 16u * s; };
     const auto empty = [&](uint32_t s) { return bars + 16u * s + 8u; };
     const uint32_t acc_full = bars + 16u * kStages, acc_empty = acc_full + 16u, drain = acc_full + 32u, ready = acc_full + 40u;
@@ -290,6 +302,10 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
         for (int i = 0; i < 2; ++i) {
             map_prefetch(&maps.p[i]);
             map_prefetch(&maps.q[i]);
+            if (KIND != kLast) {
+                map_prefetch(&maps.d[i]);
+                map_prefetch(&maps.t[i]);
+            }
         }
     }
     cluster_sync_all();
@@ -371,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
         for (uint32_t j = n_acc > 2 ? n_acc - 2 : 0; j < n_acc; ++j) (void)mbar_wait(acc_empty + 8 * (j & 1u), (j >> 1) & 1u);
     }
     __syncwarp();
-    unsigned char* stage = stages + kStages * G::kStage + warp * G::kStaging;
+    unsigned char* stage = stages + kStages * G::kStage + (SPLIT ? warp & 7 : warp) * G::kStaging;     // (of eight warps in a row eight write)
     const uint32_t quad = warp & 3, group = warp >> 2, row_in = rank * 128 + quad * 32;
     uint32_t n_acc = 0;
     bool ok = true;
@@ -506,12 +522,12 @@ template <uint32_t COLS, bool SPLIT, int KIND, typename T> cudaError_t launch_pr
     const auto kernel = ortho_product_kernel<COLS, SPLIT, KIND, T>;
     const int slot = device_slot();
     if (slot < 0 || !done.v[slot]) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Geom<COLS>::kSmem);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Geom<COLS, SPLIT>::kSmem);
         if (e != cudaSuccess) return e;
         if (slot >= 0) done.v[slot] = true;
     }
     const uint64_t pairs = (uint64_t)sm_count_now() / 2, units = SPLIT ? tiles * a.split : tiles < pairs ? tiles : pairs;
-    return launch_layer(kernel, (unsigned)(2 * units), kThreads, Geom<COLS>::kSmem, 2 * a.split, st, maps, a);
+    return launch_layer(kernel, (unsigned)(2 * units), kThreads, Geom<COLS, SPLIT>::kSmem, 2 * a.split, st, maps, a);
 }
 uint64_t count_tiles(uint64_t batch, uint64_t rows, uint64_t cols, bool symmetric, uint64_t width) {
     const uint64_t down = (rows + 255) / 256, across = (cols + width - 1) / width, ratio = 256 / width;
@@ -613,7 +629,7 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
     cudaError_t e = with_type(type, [&](auto t) {
         using T = decltype(t);
         const T* v = static_cast<const T*>(v_dev);
-        cudaError_t err = launch_layer(ortho_norm_kernel<T>, dim3(kNormBlocks, (unsigned)batch), 256, 0, 1, st, v, rows, cols, ldv, stride, part);
+        cudaError_t err = launch_layer(ortho_norm_kernel<T>, dim3(kNormBlocks, (unsigned)batch), kNormThreads, 0, 1, st, v, rows, cols, ldv, stride, part);
         if (err != cudaSuccess) return err;
         const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)((rows + 63) / 64), (unsigned)batch);
         return launch_layer(ortho_split_kernel<T>, grid, 256, 0, 1, st, v, ldv, stride, static_cast<const double*>(part), tall ? xt : x, tall ? x : xt);
