@@ -11,11 +11,18 @@
 // memory's sums lose about half a step of fp32 with every instruction, all in one direction; so they run over kChunk blocks
 // of the contraction only, and the chunks are added to nearest in registers.
 //
+// Long matrices with 16-bit results take several steps (up to kMostGroup) with one look at X: G after a step is B G B, so that only
+// products of the shorter side's size lie between G = X X^T and the product of the Bs, which X then takes at once: for m steps
+// 3 s^2 l + (4 m - 3) s^3 operations instead of 3 m s^2 l + m s^3 (4096 x 16384, five steps: 11.4 ms, so 6.4).  The rounding of B G B is
+// several times that of X X^T and takes the result's error from 1.1e-6 to 8.5e-6 of its norm: nothing beside bf16's 1.7e-3 or
+// fp16's 2e-4, but more than fp32 products throughout leave (2.9e-6), so results in fp32 go step by step.
+//
 // Bounds (checked on the host for the given coefficients): singular values of X at most 2, so entries of X at most 2, of G 4, and of B
 // 15; stored as X 2^14, G 2^13, B 2^12.
 #include <math_constants.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "tng_layers.cuh"
 #include "tng_umma.cuh"
@@ -25,6 +32,7 @@ namespace {
 
 constexpr float kScaleX = 0x1p14f, kScaleG = 0x1p13f, kScaleB = 0x1p12f;
 constexpr double kMostX = 2.0, kMostB = 15.0;
+constexpr uint32_t kMostGroup = 3;
 
 // A matrix held in two halves: `batch` of them, rows rounded up to 128, row stride ld.
 struct Halves {
@@ -548,6 +556,12 @@ Cut cut_product(uint64_t batch, uint64_t rows, uint64_t cols, uint64_t k, bool s
     const uint32_t split = narrow <= 16 && blocks >= 8 ? 4 : narrow <= 33 && blocks >= 4 ? 2 : 1;
     return {128, split, narrow};
 }
+// Cycles that a product takes about: its waves, and 7 us for a launch, its first copies and its output.
+uint64_t product_cycles(uint64_t batch, uint64_t rows, uint64_t cols, uint64_t k, bool symmetric) {
+    const Cut cut = cut_product(batch, rows, cols, k, symmetric);
+    const uint64_t pairs = (uint64_t)sm_count_now() / 2;
+    return (cut.tiles + pairs - 1) / pairs * ((k + kBlock - 1) / kBlock) * (cut.width == 256 ? 1536 : 950) / cut.split + 13000;
+}
 template <int KIND, typename T> cudaError_t launch_product(const OrthoMaps& maps, const OrthoArgs& a, const Cut& cut, cudaStream_t st) {
     if (cut.width == 256) return launch_product_as<256, false, KIND, T>(maps, a, cut.tiles, st);
     return cut.split > 1 ? launch_product_as<128, true, KIND, T>(maps, a, cut.tiles, st) : launch_product_as<128, false, KIND, T>(maps, a, cut.tiles, st);
@@ -595,10 +609,13 @@ using namespace tng;
 
 extern "C" {
 
+// Three more matrices of the shorter side for sizes that may take several steps at once.
+static bool may_group(uint64_t s, uint64_t l) { return s >= 1024 && l >= 2 * s; }
+
 size_t tng_orthogonalize_scratch_bytes(uint64_t batch, uint64_t rows, uint64_t cols) {
     if (batch == 0 || rows == 0 || cols == 0) return 256;
     const uint64_t s = rows < cols ? rows : cols, l = rows < cols ? cols : rows;
-    return (size_t)(batch * kNormBlocks * 8 + halves_bytes(batch, s, l) + 2 * halves_bytes(batch, l, s) + 2 * halves_bytes(batch, s, s));
+    return (size_t)(batch * kNormBlocks * 8 + halves_bytes(batch, s, l) + 2 * halves_bytes(batch, l, s) + (may_group(s, l) ? 5 : 2) * halves_bytes(batch, s, s));
 }
 
 tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, uint64_t rows, uint64_t cols, uint64_t ldv, uint64_t stride,
@@ -608,12 +625,13 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
         !std::isfinite(b) || !std::isfinite(c))
         return TNG_ERR_INVALID_ARG;
     // what the factors may grow to, step by step (2^-10 for rounding)
-    double most = 1.0;
+    double most = 1.0, factors[64];
     for (uint32_t i = 0; i < steps; ++i) {
         double value, factor;
         polynomial_bounds(a, b, c, most, value, factor);
         if (!(value <= kMostX && factor <= kMostB)) return TNG_ERR_INVALID_ARG;
         most = std::fmax(value, 0.0) * (1.0 + 0x1p-10);
+        factors[i] = factor * (1.0 + 0x1p-10);
     }
     if (batch == 0) return TNG_OK;
     const uint64_t s = rows < cols ? rows : cols, l = rows < cols ? cols : rows;
@@ -635,6 +653,82 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
         return launch_layer(ortho_split_kernel<T>, grid, 256, 0, 1, st, v, ldv, stride, static_cast<const double*>(part), tall ? xt : x, tall ? x : xt);
     });
     if (e != cudaSuccess) return layer_status(e);
+    if (may_group(s, l) && out_type != TNG_F32) {
+        const uint32_t groups = (steps + kMostGroup - 1) / kMostGroup;
+        const uint64_t square = product_cycles(batch, s, s, s, true), once = product_cycles(batch, s, s, l, true) + product_cycles(batch, s, l, s, false);
+        // (the products of the shorter side's size: steps + 3 (steps - groups))
+        if (groups * once + (4 * steps - 3 * groups) * square < steps * (once + square)) {
+            Halves t = carve.take(batch, s, s), q[2] = {carve.take(batch, s, s), carve.take(batch, s, s)};
+            OrthoArgs args = {};
+            args.batch = (uint32_t)batch;
+            // a symmetric product of the shorter side's size, or G itself
+            const auto symmetric = [&](auto kind, const Halves& p, const Halves& o, const Halves& d, uint64_t k, float scale) {
+                const Cut cut = cut_product(batch, s, s, k, true);
+                OrthoMaps m = {};
+                if (!make_maps(m.p, p, batch, 128) || !make_maps(m.q, o, batch, cut.width / 2) || !make_maps(m.d, d, batch, 0) || !make_maps(m.t, d, batch, 0)) return cudaErrorNotSupported;
+                args.rows = args.cols = s;
+                args.k = k;
+                args.pad_p = args.pad_q = args.pad_d = args.pad_t = x.pad_rows;
+                args.symmetric = 1;
+                args.split = cut.split;
+                args.scale = scale;
+                return launch_product<decltype(kind)::value, float>(m, args, cut, st);
+            };
+            using Gram = std::integral_constant<int, kGram>;
+            using Poly = std::integral_constant<int, kPoly>;
+            args.linear = b * (kScaleB / kScaleG);
+            args.diagonal = a * kScaleB;
+            args.g = g;
+            for (uint32_t group = 0, i = 0; group < groups && e == cudaSuccess; ++group) {
+                const uint32_t end = steps * (group + 1) / groups;
+                e = symmetric(Gram(), x, x, g, l, kScaleG / (kScaleX * kScaleX));
+                // Q, the product of the group's Bs: the first B itself; as large a power of two as its bound leaves room for
+                uint32_t now = 0;
+                float scale_q = kScaleB;
+                double bound = 1.0;
+                for (uint32_t first = i; i < end && e == cudaSuccess; ++i) {
+                    const Halves& by = i == first ? q[0] : poly;
+                    bound *= factors[i];
+                    e = symmetric(Poly(), g, g, by, s, c * (kScaleB / (kScaleG * kScaleG)));
+                    if (i > first && e == cudaSuccess) {
+                        const float scale = std::fmin(kScaleB, (float)std::exp2(std::floor(std::log2(60000.0 / std::fmax(bound, 1.0)))));
+                        e = symmetric(Gram(), poly, q[now], q[now ^ 1], s, scale / (kScaleB * scale_q));
+                        scale_q = scale;
+                        now ^= 1;
+                    }
+                    if (i + 1 < end && e == cudaSuccess) {         // G <- B (B G)
+                        e = symmetric(Gram(), by, g, t, s, kScaleG / (kScaleB * kScaleG));
+                        if (e == cudaSuccess) e = symmetric(Gram(), by, t, g, s, kScaleG / (kScaleB * kScaleG));
+                    }
+                }
+                if (e != cudaSuccess) break;
+                const bool final = group + 1 == groups, flip = final && tall;
+                const Halves &from = group & 1 ? xt2 : xt, &to = group & 1 ? xt : xt2;
+                const Cut cut = final ? cut_product(batch, rows, cols, s, false) : cut_product(batch, s, l, s, false);
+                OrthoMaps m = {};
+                if (!make_maps(m.p, flip ? from : q[now], batch, 128) || !make_maps(m.q, flip ? q[now] : from, batch, cut.width / 2) ||
+                    (!final && (!make_maps(m.d, x, batch, 0) || !make_maps(m.t, to, batch, 0))))
+                    return TNG_ERR_CUDA;
+                OrthoArgs last = args;
+                last.symmetric = 0;
+                last.k = s;
+                last.split = cut.split;
+                last.rows = final ? rows : s;
+                last.cols = final ? cols : l;
+                last.pad_p = flip ? xt.pad_rows : x.pad_rows;
+                last.pad_q = flip ? x.pad_rows : xt.pad_rows;
+                last.pad_t = xt.pad_rows;
+                last.scale = 1.f / (final ? scale_q * kScaleX : scale_q);
+                last.out = out_dev;
+                last.ldo = ldo;
+                last.stride = out_stride;
+                e = final ? with_type(out_type, [&](auto type_of) { return launch_product<kLast, decltype(type_of)>(m, last, cut, st); })
+                          : launch_product<kApply, float>(m, last, cut, st);
+            }
+            return layer_status(e);
+        }
+    }
+
     // The products of a step: G = X X^T, B from G, X <- B X (the last one as the output lies: B X, or X^T B).
     const Cut cut_gram = cut_product(batch, s, s, l, true), cut_poly = cut_product(batch, s, s, s, true);
     const Cut cut_apply = cut_product(batch, s, l, s, false), cut_last = cut_product(batch, rows, cols, s, false);

@@ -107,6 +107,26 @@ def test_steps(steps, m, n):
     assert rel(tng.orthogonalize(v, steps=steps), wanted(v, steps)) < growth(steps)
 
 
+# Sides that differ twofold and 16-bit results: several steps with one Gram matrix.
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 5, 6, 7])
+@pytest.mark.parametrize("m,n", [(1100, 4200), (4100, 1030)])
+@pytest.mark.parametrize("coefficients", [MUON, CLASSIC])
+def test_several_steps_at_once(dtype, steps, m, n, coefficients):
+    v = normal((m, n), seed=steps)
+    assert rel(tng.orthogonalize(v, steps=steps, coefficients=coefficients, dtype=dtype), wanted(v, steps, coefficients)) < growth(steps) + torch.finfo(dtype).eps / 2
+
+
+@pytest.mark.parametrize("m,n", [(1100, 4200), (4100, 1030)])
+def test_several_steps_at_once_of_a_batch(m, n):
+    v = normal((3, m, n), torch.bfloat16, 4)
+    got = tng.orthogonalize(v)
+    assert all(rel(got[i], wanted(v[i], 5)) < growth(5) + torch.finfo(torch.bfloat16).eps / 2 for i in range(3))
+    v[1, 3, 4] = float("nan")
+    again = tng.orthogonalize(v)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[2], got[2]) and bool(again[1].isnan().all())
+
+
 def test_singular_values_come_near_one():
     """The classic coefficients converge; singular values from 0.02 of the norm up are at one within 2^-10 after twelve steps."""
     g = torch.linalg.qr(normal((300, 200)).double())[0] * torch.linspace(1.0, 0.1, 200, dtype=torch.float64, device="cuda")
