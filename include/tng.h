@@ -417,7 +417,7 @@ tng_status tng_embed(const void* table_dev, tng_dtype table_type, uint64_t vocab
                      uint32_t id_bytes, uint64_t tokens, float scale, void* y_dev, tng_dtype type, uint64_t ldy, void* stream);
 /* Its gradient: dtable[v] = scale * sum of dy[t] over the t with ids[t] = v, every row of the table written (zeros where no token
  * names it), so that it can go straight into a worker's row of gradients.  The sums are fp32 in an order that the ids alone decide: the
- * same inputs give the same bits.  scratch_dev: tng_embed_grad_scratch_bytes, 256-byte aligned.  width <= 2^26. */
+ * same inputs give the same bits.  scratch_dev: tng_embed_grad_scratch_bytes, 256-byte aligned.  width < 2^25. */
 size_t tng_embed_grad_scratch_bytes(uint64_t tokens, uint64_t width);
 tng_status tng_embed_grad(const void* dy_dev, tng_dtype type, uint64_t tokens, uint64_t width, uint64_t lddy, const void* ids_dev,
                           uint32_t id_bytes, uint64_t vocab, float scale, float* dtable_dev, uint64_t ldd, void* scratch_dev, void* stream);

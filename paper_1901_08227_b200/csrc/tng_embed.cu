@@ -517,7 +517,7 @@ size_t tng_embed_grad_scratch_bytes(uint64_t tokens, uint64_t width) {
 
 tng_status tng_embed_grad(const void* dy_dev, tng_dtype type, uint64_t tokens, uint64_t width, uint64_t lddy, const void* ids_dev,
                           uint32_t id_bytes, uint64_t vocab, float scale, float* dtable_dev, uint64_t ldd, void* scratch_dev, void* stream) {
-    if (!type_ok(type) || width < 1 || vocab < 1 || !dims_ok(tokens, width) || !dims_ok(vocab, width) || (id_bytes != 4 && id_bytes != 8) ||
+    if (!type_ok(type) || width < 1 || width >= (1u << 25) || vocab < 1 || !dims_ok(tokens, width) || !dims_ok(vocab, width) || (id_bytes != 4 && id_bytes != 8) ||
         !matrix_ok(dtable_dev, TNG_F32, width, ldd))
         return TNG_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -529,7 +529,6 @@ tng_status tng_embed_grad(const void* dy_dev, tng_dtype type, uint64_t tokens, u
     const uint64_t list = up256(tokens * 8);
     for (int i = 0; i < 2; ++i) s.pair[i] = reinterpret_cast<uint2*>(at + i * list);
     const uint64_t chunk = chunk_of(tokens), chunks = (tokens + chunk - 1) / chunk, spans = (width + kGradSpan - 1) / kGradSpan;
-    if (spans > 65535) return TNG_ERR_INVALID_ARG;
     uint32_t* crossing = reinterpret_cast<uint32_t*>(at + 2 * list);
     float* parts = reinterpret_cast<float*>(at + 2 * list + up256((1 + chunks) * 4));
     s.crossing = crossing;

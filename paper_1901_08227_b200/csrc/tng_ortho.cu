@@ -8,8 +8,8 @@
 // fp16's range and its steps far below the entries; a product is three (hi lo, lo hi, hi hi), lo lo being below 2^-22 of it.
 // (bf16 factors alone, 8 bits, would do for the singular values that are near one, but a step multiplies what lies in the
 // directions of the small ones by up to a: after five steps rounding noise of 2^-9 has grown by a factor of hundreds there.)  The tensor
-// memory's sums lose about half a step of fp32 with every instruction, all in one direction; so they run over kChunk blocks
-// of the contraction only, and the chunks are added to nearest in registers.
+// memory's sums lose about half a step of fp32 with every instruction, all in one direction; so they run over one or two
+// blocks of the contraction only, and the chunks are added to nearest in registers.
 //
 // Long matrices with 16-bit results take several steps (up to kMostGroup) with one look at X: G after a step is B G B, so that only
 // products of the shorter side's size lie between G = X X^T and the product of the Bs, which X then takes at once: for m steps
@@ -134,11 +134,14 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const T* v, uint64_t l
 // Warps: 0-15 add up and write out (a quarter of the rows and of the columns each), 16 feeds, 17 issues.
 enum Kind { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
 constexpr int kThreads = 576;
-constexpr uint32_t kBox = 128 * 128, kStages = 3, kBlock = 64, kChunk = 1;
+constexpr uint32_t kBox = 128 * 128, kStages = 3, kBlock = 64;
 // Staging of the output: buffers of 2 KB, 4 a warp where at most eight warps write (SPLIT).
 template <uint32_t COLS, bool SPLIT> struct Geom {
     static constexpr uint32_t kQ = COLS / 2 * 128, kStage = 2 * kBox + 2 * kQ, kBuffers = COLS == 256 ? 1 : SPLIT ? 4 : 2, kStaging = 2048 * kBuffers;
     static constexpr uint32_t kSmem = 1024 + kStages * kStage + (SPLIT ? 8 : 16) * kStaging + 256;
+    // Blocks whose sum the tensor memory forms, and such sums under way: all of it.  (A sum's way from its last instruction into registers and
+    // the free place's way back take longer than one block: with two places 128 columns wide, 1750 cycles a block instead of 950.)
+    static constexpr uint32_t kChunk = COLS == 256 ? 2 : 1, kSums = 512 / COLS;
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
 static_assert(128 * 128 * 4 <= kStages * Geom<128, true>::kStage, "the stages also hold the sums");
@@ -285,7 +288,8 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
     const uint32_t bars = data + G::kSmem - 1024 - 256;
     const auto full = [&](uint32_t s) { return bars + 16u * s; };
     const auto empty = [&](uint32_t s) { return bars + 16u * s + 8u; };
-    const uint32_t acc_full = bars + 16u * kStages, acc_empty = acc_full + 16u, drain = acc_full + 32u, ready = acc_full + 40u;
+    constexpr uint32_t kChunk = G::kChunk, kSums = G::kSums;
+    const uint32_t acc_full = bars + 16u * kStages, acc_empty = acc_full + 8u * kSums, drain = acc_empty + 8u * kSums, ready = drain + 8u;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, in_cluster = cluster_rank();
     const uint32_t rank = in_cluster & 1u, even = in_cluster & ~1u;            // the pair's CTA that issues
     const uint32_t part = SPLIT ? in_cluster >> 1 : 0, parts = SPLIT ? a.split : 1;
@@ -299,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
         }
-        for (uint32_t i = 0; i < 2; ++i) {
+        for (uint32_t i = 0; i < kSums; ++i) {
             mbar_init(acc_full + 8 * i, 1);
             mbar_init(acc_empty + 8 * i, 32);              // sixteen warps of either CTA
         }
@@ -319,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
     cluster_sync_all();
     grid_wait();
     if (warp == 17) {                                      // tensor memory is taken only now: see the 8-bit products
-        tmem_alloc<2>(smem_u32((const void*)&sh_tmem), 2 * COLS);
+        tmem_alloc<2>(smem_u32((const void*)&sh_tmem), 512);
         if (rank == 1 && lane == 0) cluster_arrive(cluster_map(ready, even));
     }
     if (warp != 16) {
@@ -366,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
         bool ok = mbar_wait(ready, 0);                     // the odd CTA has its tensor memory
         for (uint32_t t = unit; ok && t < tiles.count; t += units) {
             for (uint32_t k0 = 0; ok && k0 < blocks; k0 += kChunk, ++n_acc) {
-                const uint32_t acc = n_acc & 1u, use = n_acc >> 1, into = sh_tmem + acc * COLS, n = blocks - k0 < kChunk ? blocks - k0 : kChunk;
+                const uint32_t acc = n_acc % kSums, use = n_acc / kSums, into = sh_tmem + acc * COLS, n = blocks - k0 < kChunk ? blocks - k0 : kChunk;
                 if (use > 0 && !mbar_wait(acc_empty + 8 * acc, (use - 1) & 1u)) { ok = false; break; }
                 umma_fence_after();
                 for (uint32_t kb = 0; kb < n; ++kb) {
@@ -392,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
             (void)mbar_wait(drain, 0);
         }
         // the hand-backs that nothing else waits for come from the other CTA too: they arrive before this one may leave
-        for (uint32_t j = n_acc > 2 ? n_acc - 2 : 0; j < n_acc; ++j) (void)mbar_wait(acc_empty + 8 * (j & 1u), (j >> 1) & 1u);
+        for (uint32_t j = n_acc > kSums ? n_acc - kSums : 0; j < n_acc; ++j) (void)mbar_wait(acc_empty + 8 * (j % kSums), (j / kSums) & 1u);
     }
     __syncwarp();
     unsigned char* stage = stages + kStages * G::kStage + (SPLIT ? warp & 7 : warp) * G::kStaging;     // (of eight warps in a row eight write)
@@ -403,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
     float sum[kWide];
     const auto add_up = [&] {
         for (uint32_t k0 = 0; k0 < blocks; k0 += kChunk, ++n_acc) {
-            const uint32_t acc = n_acc & 1u, use = n_acc >> 1;
+            const uint32_t acc = n_acc % kSums, use = n_acc / kSums;
             if (ok && !mbar_wait(acc_full + 8 * acc, use & 1u)) ok = false;
             ok = __all_sync(kFullMask, ok && !sh_failed);
             umma_fence_after();
@@ -414,7 +418,12 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
                 tmem_ld16(sh_tmem + ((quad * 32) << 16) + acc * COLS + group * kWide + c, r);
                 tmem_wait_ld();
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sum[c + j] = k0 == 0 ? __uint_as_float(r[j]) : __fadd_rn(sum[c + j], __uint_as_float(r[j]));
+                for (int j = 0; j < 16; j += 2) {
+                    const float2 two = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
+                    const float2 all = k0 == 0 ? two : __fadd2_rn(make_float2(sum[c + j], sum[c + j + 1]), two);
+                    sum[c + j] = all.x;
+                    sum[c + j + 1] = all.y;
+                }
             }
             umma_fence_before();
             __syncwarp();
@@ -492,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
         __syncwarp();
         cluster_wait_all();                                // nobody leaves while its sums are being read
     }
-    if (warp == 17) tmem_free<2>(sh_tmem, 2 * COLS);
+    if (warp == 17) tmem_free<2>(sh_tmem, 512);
 }
 
 // ---- host ------------------------------------------------------------------------------------------
