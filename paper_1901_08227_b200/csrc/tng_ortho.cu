@@ -134,27 +134,29 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const T* v, uint64_t l
 // Warps: 0-15 add up and write out (a quarter of the rows and of the columns each), 16 feeds, 17 issues.
 enum Kind { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
 constexpr int kThreads = 576;
-constexpr uint32_t kBox = 128 * 128, kStages = 3, kBlock = 64;
-// Staging of the output: buffers of 2 KB, 4 a warp where at most eight warps write (SPLIT).
+constexpr uint32_t kBox = 128 * 128, kBlock = 64;
+// (Stages of 32, twice as many, whose rows are 64 bytes: 2048 x 2048 x 8192 134 us instead of 113.)
+// Staging of the output: buffers of 2 KB, two a warp where at most eight warps write (SPLIT).
 template <uint32_t COLS, bool SPLIT> struct Geom {
-    static constexpr uint32_t kQ = COLS / 2 * 128, kStage = 2 * kBox + 2 * kQ, kBuffers = COLS == 256 ? 1 : SPLIT ? 4 : 2, kStaging = 2048 * kBuffers;
+    static constexpr uint32_t kQ = COLS / 2 * 128, kStage = 2 * kBox + 2 * kQ, kStages = COLS == 256 ? 3 : 4;
+    static constexpr uint32_t kBuffers = SPLIT ? 2 : 1, kStaging = 2048 * kBuffers;
     static constexpr uint32_t kSmem = 1024 + kStages * kStage + (SPLIT ? 8 : 16) * kStaging + 256;
-    // Blocks whose sum the tensor memory forms, and such sums under way: all of it.  (A sum's way from its last instruction into registers and
-    // the free place's way back take longer than one block: with two places 128 columns wide, 1750 cycles a block instead of 950.)
+    // Blocks whose sum the tensor memory forms, and such sums under way: all of it.
     static constexpr uint32_t kChunk = COLS == 256 ? 2 : 1, kSums = 512 / COLS;
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
+    static_assert(16 * kStages + 16 * kSums + 16 <= 256, "barriers");
 };
-static_assert(128 * 128 * 4 <= kStages * Geom<128, true>::kStage, "the stages also hold the sums");
+static_assert(128 * 128 * 4 <= Geom<128, true>::kStages * Geom<128, true>::kStage, "the stages also hold the sums");
 
 struct OrthoMaps {
-    CUtensorMap p[2], q[2], d[2], t[2];   // hi and lo of the factors, of D and of its transpose
+    CUtensorMap p[2], q[2], d[2];   // hi and lo of the factors and of D
 };
 struct OrthoArgs {
     uint64_t rows, cols, k;         // of D, and the contraction
-    uint64_t pad_p, pad_q, pad_d, pad_t;   // rows from one matrix of the batch to the next
+    uint64_t pad_p, pad_q, pad_d;   // rows from one matrix of the batch to the next
     uint32_t batch, symmetric, split;
     float scale, linear, diagonal;  // D = scale * sum (+ linear * g + diagonal on the diagonal: kPoly)
-    Halves g;                       // kPoly: the factor itself
+    Halves g, t;                    // kPoly: the factor itself; D's transpose (D, if it is symmetric)
     void* out;                      // kLast
     uint64_t ldo, stride;
 };
@@ -211,19 +213,23 @@ __device__ __forceinline__ void put_rows(const CUtensorMap* map, const float (&v
     __syncwarp();
     if (lane == 0) tile_store(map, x, y, smem_u32(stage));
 }
-// The same transposed: row j of the box is column j, its 32 values the lanes'.
-template <bool LO, uint32_t C, int BUFFERS, uint32_t N>
-__device__ __forceinline__ void put_turned(const CUtensorMap* map, const float (&v)[N], int32_t x, int32_t y, unsigned char* stage, uint32_t lane) {
-    if (lane == 0) tile_store_wait_read<BUFFERS - 1>();
-    __syncwarp();
+// The same transposed, both halves, straight into memory: neighbouring lanes exchange a value, so that each stores two of one column, and 16
+// lanes 64 bytes.  (By copies through staging too: 20 k cycles a tile of 256 x 256 in all, which the next tile's first sums do not hide.)
+template <uint32_t C, uint32_t N>
+__device__ __forceinline__ void put_turned(const Halves& t, const float (&v)[N], uint32_t b, uint64_t row0, uint64_t col, uint64_t rows, uint64_t cols, uint32_t lane) {
+    const uint32_t odd = lane & 1;
+    const uint64_t row = row0 + (lane & 30u);              // (a pair may end one past the last row: rows of t are padded to 64)
+    uint64_t at = (b * t.pad_rows + col + odd) * t.ld + row;
 #pragma unroll
-    for (uint32_t j = 0; j < 32; ++j) {
-        const uint32_t w = __float_as_uint(v[C + j]);
-        *reinterpret_cast<uint16_t*>(stage + j * 64 + (((lane >> 3) ^ ((j >> 1) & 3)) * 16) + (lane & 7) * 2) = (uint16_t)(LO ? w : w >> 16);
+    for (uint32_t j = 0; j < 32; j += 2, at += 2 * t.ld) {
+        const uint32_t v0 = __float_as_uint(v[C + j]), v1 = __float_as_uint(v[C + j + 1]);
+        const uint32_t got = __shfl_xor_sync(kFullMask, odd ? v0 : v1, 1);
+        const uint32_t low = odd ? got : v0, high = odd ? v1 : got;        // rows `row` and `row` + 1 of column j + odd
+        if (row < rows && col + j + odd < cols) {
+            *reinterpret_cast<uint32_t*>(t.hi + at) = __byte_perm(low, high, 0x7632);
+            *reinterpret_cast<uint32_t*>(t.lo + at) = __byte_perm(low, high, 0x5410);
+        }
     }
-    smem_to_copies();
-    __syncwarp();
-    if (lane == 0) tile_store(map, x, y, smem_u32(stage));
 }
 
 // A warp's 32 columns from C of its sums, finished and written: see ortho_product_kernel.
@@ -264,14 +270,10 @@ __device__ __forceinline__ void finish(const OrthoMaps& maps, const OrthoArgs& a
 #pragma unroll
             for (uint32_t j = 0; j < 32; ++j) sum[C + j] = both_halves(__fmul_rn(sum[C + j], a.scale));
         }
-        const int32_t x = (int32_t)col, y = (int32_t)(b * a.pad_d + row0), xt = (int32_t)row0, yt = (int32_t)(b * a.pad_t + col);
-        const auto buffer = [&](int i) { return stage + (i & (BUFFERS - 1)) * 2048; };
-        put_rows<false, C, BUFFERS>(&maps.d[0], sum, x, y, buffer(0), lane);
-        put_rows<true, C, BUFFERS>(&maps.d[1], sum, x, y, buffer(1), lane);
-        if (mirrored) {
-            put_turned<false, C, BUFFERS>(&maps.t[0], sum, xt, yt, buffer(2), lane);
-            put_turned<true, C, BUFFERS>(&maps.t[1], sum, xt, yt, buffer(3), lane);
-        }
+        const int32_t x = (int32_t)col, y = (int32_t)(b * a.pad_d + row0);
+        put_rows<false, C, BUFFERS>(&maps.d[0], sum, x, y, stage, lane);
+        put_rows<true, C, BUFFERS>(&maps.d[1], sum, x, y, stage + (BUFFERS - 1) * 2048, lane);
+        if (mirrored) put_turned<C>(a.t, sum, b, row0, col, a.rows, a.cols, lane);
     }
 }
 
@@ -288,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
     const uint32_t bars = data + G::kSmem - 1024 - 256;
     const auto full = [&](uint32_t s) { return bars + 16u * s; };
     const auto empty = [&](uint32_t s) { return bars + 16u * s + 8u; };
-    constexpr uint32_t kChunk = G::kChunk, kSums = G::kSums;
+    constexpr uint32_t kChunk = G::kChunk, kSums = G::kSums, kStages = G::kStages;
     const uint32_t acc_full = bars + 16u * kStages, acc_empty = acc_full + 8u * kSums, drain = acc_empty + 8u * kSums, ready = drain + 8u;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, in_cluster = cluster_rank();
     const uint32_t rank = in_cluster & 1u, even = in_cluster & ~1u;            // the pair's CTA that issues
@@ -314,10 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
         for (int i = 0; i < 2; ++i) {
             map_prefetch(&maps.p[i]);
             map_prefetch(&maps.q[i]);
-            if (KIND != kLast) {
-                map_prefetch(&maps.d[i]);
-                map_prefetch(&maps.t[i]);
-            }
+            if (KIND != kLast) map_prefetch(&maps.d[i]);
         }
     }
     cluster_sync_all();
@@ -674,10 +673,11 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
             const auto symmetric = [&](auto kind, const Halves& p, const Halves& o, const Halves& d, uint64_t k, float scale) {
                 const Cut cut = cut_product(batch, s, s, k, true);
                 OrthoMaps m = {};
-                if (!make_maps(m.p, p, batch, 128) || !make_maps(m.q, o, batch, cut.width / 2) || !make_maps(m.d, d, batch, 0) || !make_maps(m.t, d, batch, 0)) return cudaErrorNotSupported;
+                if (!make_maps(m.p, p, batch, 128) || !make_maps(m.q, o, batch, cut.width / 2) || !make_maps(m.d, d, batch, 0)) return cudaErrorNotSupported;
                 args.rows = args.cols = s;
                 args.k = k;
-                args.pad_p = args.pad_q = args.pad_d = args.pad_t = x.pad_rows;
+                args.pad_p = args.pad_q = args.pad_d = x.pad_rows;
+                args.t = d;
                 args.symmetric = 1;
                 args.split = cut.split;
                 args.scale = scale;
@@ -716,7 +716,7 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
                 const Cut cut = final ? cut_product(batch, rows, cols, s, false) : cut_product(batch, s, l, s, false);
                 OrthoMaps m = {};
                 if (!make_maps(m.p, flip ? from : q[now], batch, 128) || !make_maps(m.q, flip ? q[now] : from, batch, cut.width / 2) ||
-                    (!final && (!make_maps(m.d, x, batch, 0) || !make_maps(m.t, to, batch, 0))))
+                    (!final && !make_maps(m.d, x, batch, 0)))
                     return TNG_ERR_CUDA;
                 OrthoArgs last = args;
                 last.symmetric = 0;
@@ -726,7 +726,7 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
                 last.cols = final ? cols : l;
                 last.pad_p = flip ? xt.pad_rows : x.pad_rows;
                 last.pad_q = flip ? x.pad_rows : xt.pad_rows;
-                last.pad_t = xt.pad_rows;
+                last.t = to;
                 last.scale = 1.f / (final ? scale_q * kScaleX : scale_q);
                 last.out = out_dev;
                 last.ldo = ldo;
@@ -741,30 +741,31 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
     // The products of a step: G = X X^T, B from G, X <- B X (the last one as the output lies: B X, or X^T B).
     const Cut cut_gram = cut_product(batch, s, s, l, true), cut_poly = cut_product(batch, s, s, s, true);
     const Cut cut_apply = cut_product(batch, s, l, s, false), cut_last = cut_product(batch, rows, cols, s, false);
-    const auto maps_of = [&](OrthoMaps& m, const Cut& cut, const Halves& p, const Halves& q, const Halves* d, const Halves* t) {
-        return make_maps(m.p, p, batch, 128) && make_maps(m.q, q, batch, cut.width / 2) && (!d || (make_maps(m.d, *d, batch, 0) && make_maps(m.t, *t, batch, 0)));
+    const auto maps_of = [&](OrthoMaps& m, const Cut& cut, const Halves& p, const Halves& q, const Halves* d) {
+        return make_maps(m.p, p, batch, 128) && make_maps(m.q, q, batch, cut.width / 2) && (!d || make_maps(m.d, *d, batch, 0));
     };
     OrthoMaps gram = {}, square = {}, apply[2] = {}, last = {};
     const Halves& xt_last = (steps - 1) & 1 ? xt2 : xt;
-    if (!maps_of(gram, cut_gram, x, x, &g, &g) || !maps_of(square, cut_poly, g, g, &poly, &poly) ||
-        (steps > 1 && !maps_of(apply[0], cut_apply, poly, xt, &x, &xt2)) || (steps > 2 && !maps_of(apply[1], cut_apply, poly, xt2, &x, &xt)) ||
-        !(tall ? maps_of(last, cut_last, xt_last, poly, nullptr, nullptr) : maps_of(last, cut_last, poly, xt_last, nullptr, nullptr)))
+    if (!maps_of(gram, cut_gram, x, x, &g) || !maps_of(square, cut_poly, g, g, &poly) || (steps > 1 && !maps_of(apply[0], cut_apply, poly, xt, &x)) ||
+        (steps > 2 && !maps_of(apply[1], cut_apply, poly, xt2, &x)) || !(tall ? maps_of(last, cut_last, xt_last, poly, nullptr) : maps_of(last, cut_last, poly, xt_last, nullptr)))
         return TNG_ERR_CUDA;
     OrthoArgs square_args = {};                            // of both symmetric products
     square_args.batch = (uint32_t)batch;
     square_args.rows = square_args.cols = s;
-    square_args.pad_p = square_args.pad_q = square_args.pad_d = square_args.pad_t = x.pad_rows;
+    square_args.pad_p = square_args.pad_q = square_args.pad_d = x.pad_rows;
     square_args.symmetric = 1;
     square_args.g = g;
     for (uint32_t i = 0; i < steps; ++i) {
         OrthoArgs args = square_args;
         args.split = cut_gram.split;
         args.k = l;
+        args.t = g;
         args.scale = kScaleG / (kScaleX * kScaleX);
         e = launch_product<kGram, float>(gram, args, cut_gram, st);
         if (e != cudaSuccess) return layer_status(e);
         args.split = cut_poly.split;
         args.k = s;
+        args.t = poly;
         args.scale = c * (kScaleB / (kScaleG * kScaleG));
         args.linear = b * (kScaleB / kScaleG);
         args.diagonal = a * kScaleB;
@@ -774,7 +775,8 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
         if (i + 1 < steps) {
             args.split = cut_apply.split;
             args.cols = l;
-            args.pad_q = args.pad_t = xt.pad_rows;
+            args.pad_q = xt.pad_rows;
+            args.t = i & 1 ? xt : xt2;
             args.scale = 1.f / kScaleB;
             e = launch_product<kApply, float>(apply[i & 1], args, cut_apply, st);
         } else {
