@@ -126,30 +126,32 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const T* v, uint64_t l
 // ---- products --------------------------------------------------------------------------------------------
 // D = P Q^T of two matrices in halves, contraction along the rows of both, by pairs of CTAs on two SMs: tiles of 256 x 256 or 256 x 128
 // outputs.  A CTA copies 128 rows of P and half the tile's rows of Q, both halves of them, for a stage of 64 of the contraction (12
-// instructions).  What the instructions read from shared memory and the copies write there is the bound: 106 bytes a cycle of 128 for
-// 256 x 256, and the matrix unit then sets the time (1536 cycles a stage); 158 for 256 x 128 (950 cycles for half the work), so those are
-// for matrices of few tiles.  (128 x 128 tiles of one SM would want 213: measured 1580 cycles.)
+// instructions).  The matrix unit would take 1536 cycles a stage for 256 x 256 and 768 for 256 x 128; measured 2000 (the sums' way into
+// registers: two of them have all of the tensor memory) and 1150 (issue), so the narrow tiles are for matrices of few tiles.  (128 x 128
+// tiles of one SM: 1580 cycles; they want 213 bytes a cycle of shared memory.)
 // SPLIT (256 x 128): a cluster of 2 or 4 pairs takes consecutive parts of one tile's contraction; each then adds the others' sums, read
 // from their shared memories, to its own for its share of the columns and writes those out.
-// Warps: 0-15 add up and write out (a quarter of the rows and of the columns each), 16 feeds, 17 issues.
+// Warps: 0-15 add up and write out (a quarter of the rows and of the columns each), 16 feeds, 17 and 18 issue, every other sum each: an
+// instruction takes its thread 54 cycles, a block with its waits and commits 1285, where the matrix unit takes 768 for 256 x 128.
 enum Kind { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
-constexpr int kThreads = 576;
+constexpr int kThreads = 608;
 constexpr uint32_t kBox = 128 * 128, kBlock = 64;
 // (Stages of 32, twice as many, whose rows are 64 bytes: 2048 x 2048 x 8192 134 us instead of 113.)
-// Staging of the output: buffers of 2 KB, two a warp where at most eight warps write (SPLIT).
+// Staging of the output: buffers of 2 KB, four a warp where at most eight warps write (SPLIT).
 template <uint32_t COLS, bool SPLIT> struct Geom {
-    static constexpr uint32_t kQ = COLS / 2 * 128, kStage = 2 * kBox + 2 * kQ, kStages = COLS == 256 ? 3 : 4;
-    static constexpr uint32_t kBuffers = SPLIT ? 2 : 1, kStaging = 2048 * kBuffers;
+    static constexpr uint32_t kQ = COLS / 2 * 128, kStage = 2 * kBox + 2 * kQ, kStages = COLS == 256 || SPLIT ? 3 : 4;
+    static constexpr uint32_t kBuffers = SPLIT ? 4 : 1, kStaging = 2048 * kBuffers;
     static constexpr uint32_t kSmem = 1024 + kStages * kStage + (SPLIT ? 8 : 16) * kStaging + 256;
     // Blocks whose sum the tensor memory forms, and such sums under way: all of it.
     static constexpr uint32_t kChunk = COLS == 256 ? 2 : 1, kSums = 512 / COLS;
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
-    static_assert(16 * kStages + 16 * kSums + 16 <= 256, "barriers");
+    static_assert(16 * kStages + 16 * kSums + 24 <= 256, "barriers");
+    static_assert(kSums % 2 == 0, "a sum's place belongs to one of the two issuing warps");
 };
 static_assert(128 * 128 * 4 <= Geom<128, true>::kStages * Geom<128, true>::kStage, "the stages also hold the sums");
 
 struct OrthoMaps {
-    CUtensorMap p[2], q[2], d[2];   // hi and lo of the factors and of D
+    CUtensorMap p[2], q[2], d[2], t[2];   // hi and lo of the factors, of D and (split products) of its transpose
 };
 struct OrthoArgs {
     uint64_t rows, cols, k;         // of D, and the contraction
@@ -213,8 +215,23 @@ __device__ __forceinline__ void put_rows(const CUtensorMap* map, const float (&v
     __syncwarp();
     if (lane == 0) tile_store(map, x, y, smem_u32(stage));
 }
-// The same transposed, both halves, straight into memory: neighbouring lanes exchange a value, so that each stores two of one column, and 16
-// lanes 64 bytes.  (By copies through staging too: 20 k cycles a tile of 256 x 256 in all, which the next tile's first sums do not hide.)
+// The same transposed: row j of the box is column j, its 32 values the lanes'.
+template <bool LO, uint32_t C, int BUFFERS, uint32_t N>
+__device__ __forceinline__ void put_turned_staged(const CUtensorMap* map, const float (&v)[N], int32_t x, int32_t y, unsigned char* stage, uint32_t lane) {
+    if (lane == 0) tile_store_wait_read<BUFFERS - 1>();
+    __syncwarp();
+#pragma unroll
+    for (uint32_t j = 0; j < 32; ++j) {
+        const uint32_t w = __float_as_uint(v[C + j]);
+        *reinterpret_cast<uint16_t*>(stage + j * 64 + (((lane >> 3) ^ ((j >> 1) & 3)) * 16) + (lane & 7) * 2) = (uint16_t)(LO ? w : w >> 16);
+    }
+    smem_to_copies();
+    __syncwarp();
+    if (lane == 0) tile_store(map, x, y, smem_u32(stage));
+}
+// The same, both halves, straight into memory: neighbouring lanes exchange a value, so that each stores two of one column, and 16
+// lanes 64 bytes.  Where staging is short (one buffer a warp) this is faster than copies (2048 x 8192 x 2048 186 -> 180 us), with four buffers
+// a warp it is slower (512 x 512, five steps: 146 -> 157 us).
 template <uint32_t C, uint32_t N>
 __device__ __forceinline__ void put_turned(const Halves& t, const float (&v)[N], uint32_t b, uint64_t row0, uint64_t col, uint64_t rows, uint64_t cols, uint32_t lane) {
     const uint32_t odd = lane & 1;
@@ -272,8 +289,16 @@ __device__ __forceinline__ void finish(const OrthoMaps& maps, const OrthoArgs& a
         }
         const int32_t x = (int32_t)col, y = (int32_t)(b * a.pad_d + row0);
         put_rows<false, C, BUFFERS>(&maps.d[0], sum, x, y, stage, lane);
-        put_rows<true, C, BUFFERS>(&maps.d[1], sum, x, y, stage + (BUFFERS - 1) * 2048, lane);
-        if (mirrored) put_turned<C>(a.t, sum, b, row0, col, a.rows, a.cols, lane);
+        put_rows<true, C, BUFFERS>(&maps.d[1], sum, x, y, stage + (BUFFERS > 1 ? 2048 : 0), lane);
+        if (mirrored) {
+            if constexpr (BUFFERS == 4) {
+                const int32_t xt = (int32_t)row0, yt = (int32_t)(b * a.t.pad_rows + col);
+                put_turned_staged<false, C, BUFFERS>(&maps.t[0], sum, xt, yt, stage + 4096, lane);
+                put_turned_staged<true, C, BUFFERS>(&maps.t[1], sum, xt, yt, stage + 6144, lane);
+            } else {
+                put_turned<C>(a.t, sum, b, row0, col, a.rows, a.cols, lane);
+            }
+        }
     }
 }
 
@@ -291,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
     const auto full = [&](uint32_t s) { return bars + 16u * s; };
     const auto empty = [&](uint32_t s) { return bars + 16u * s + 8u; };
     constexpr uint32_t kChunk = G::kChunk, kSums = G::kSums, kStages = G::kStages;
-    const uint32_t acc_full = bars + 16u * kStages, acc_empty = acc_full + 8u * kSums, drain = acc_empty + 8u * kSums, ready = drain + 8u;
+    const uint32_t acc_full = bars + 16u * kStages, acc_empty = acc_full + 8u * kSums, drain = acc_empty + 8u * kSums, ready = drain + 16u;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, in_cluster = cluster_rank();
     const uint32_t rank = in_cluster & 1u, even = in_cluster & ~1u;            // the pair's CTA that issues
     const uint32_t part = SPLIT ? in_cluster >> 1 : 0, parts = SPLIT ? a.split : 1;
@@ -310,6 +335,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
             mbar_init(acc_empty + 8 * i, 32);              // sixteen warps of either CTA
         }
         mbar_init(drain, 1);
+        mbar_init(drain + 8, 1);
         mbar_init(ready, 1);
         mbar_init_fence();
 #pragma unroll
@@ -317,6 +343,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
             map_prefetch(&maps.p[i]);
             map_prefetch(&maps.q[i]);
             if (KIND != kLast) map_prefetch(&maps.d[i]);
+            if (KIND != kLast && SPLIT) map_prefetch(&maps.t[i]);
         }
     }
     cluster_sync_all();
@@ -327,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
     }
     if (warp != 16) {
         umma_fence_before();
-        asm volatile("bar.sync 1, 544;" ::: "memory");     // the seventeen warps that use it
+        asm volatile("bar.sync 1, 576;" ::: "memory");     // the eighteen warps that use it
         umma_fence_after();
         grid_go();
     }
@@ -361,19 +388,25 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
             if (rank == 0) (void)mbar_wait(full(j % kStages), (j / kStages) & 1u);
             if (ok && !mbar_wait(empty(j % kStages), (j / kStages) & 1u)) ok = false;
         }
-    } else if (warp == 17 && lane == 0 && rank == 0) {
+    } else if (warp >= 17 && lane == 0 && rank == 0) {
         // ---- issue
         constexpr uint32_t idesc = umma_idesc_f16(256, COLS);
         const uint16_t both = (uint16_t)(3u << even);
-        uint32_t s = 0, parity = 0, n_acc = 0;
+        const uint32_t mine = warp - 17;
+        uint32_t it = 0, n_acc = 0;                        // blocks and sums so far, the other warp's too
         bool ok = mbar_wait(ready, 0);                     // the odd CTA has its tensor memory
         for (uint32_t t = unit; ok && t < tiles.count; t += units) {
             for (uint32_t k0 = 0; ok && k0 < blocks; k0 += kChunk, ++n_acc) {
                 const uint32_t acc = n_acc % kSums, use = n_acc / kSums, into = sh_tmem + acc * COLS, n = blocks - k0 < kChunk ? blocks - k0 : kChunk;
+                if ((n_acc & 1u) != mine) {
+                    it += n;
+                    continue;
+                }
                 if (use > 0 && !mbar_wait(acc_empty + 8 * acc, (use - 1) & 1u)) { ok = false; break; }
                 umma_fence_after();
-                for (uint32_t kb = 0; kb < n; ++kb) {
-                    if (!mbar_wait(full(s), parity)) { ok = false; break; }
+                for (uint32_t kb = 0; kb < n; ++kb, ++it) {
+                    const uint32_t s = it % kStages;
+                    if (!mbar_wait(full(s), (it / kStages) & 1u)) { ok = false; break; }
                     umma_fence_after();
                     const uint32_t at = data + s * G::kStage;
                     const uint64_t ph = umma_desc(at), pl = umma_desc(at + kBox), qh = umma_desc(at + 2 * kBox), ql = umma_desc(at + 2 * kBox + G::kQ);
@@ -384,18 +417,18 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
 #pragma unroll
                     for (int j = 0; j < 4; ++j) umma_f16<2>(into, ph + 2 * j, qh + 2 * j, idesc, true);
                     umma_commit_pair(empty(s), both);
-                    if (++s == kStages) { s = 0; parity ^= 1u; }
                 }
                 if (ok) umma_commit_pair(acc_full + 8 * acc, both);
             }
         }
         if (!ok) {
             sh_failed = 1;
-            umma_commit_pair(drain, (uint16_t)(1u << even));
-            (void)mbar_wait(drain, 0);
+            umma_commit_pair(drain + 8 * mine, (uint16_t)(1u << even));
+            (void)mbar_wait(drain + 8 * mine, 0);
         }
         // the hand-backs that nothing else waits for come from the other CTA too: they arrive before this one may leave
-        for (uint32_t j = n_acc > kSums ? n_acc - kSums : 0; j < n_acc; ++j) (void)mbar_wait(acc_empty + 8 * (j % kSums), (j / kSums) & 1u);
+        for (uint32_t j = n_acc > kSums ? n_acc - kSums : 0; ok && j < n_acc; ++j)
+            if ((j & 1u) == mine) (void)mbar_wait(acc_empty + 8 * (j % kSums), (j / kSums) & 1u);
     }
     __syncwarp();
     unsigned char* stage = stages + kStages * G::kStage + (SPLIT ? warp & 7 : warp) * G::kStaging;     // (of eight warps in a row eight write)
@@ -554,13 +587,13 @@ struct Cut {
     uint32_t width, split;
     uint64_t tiles;
 };
-// The tiles whose waves over the pairs take less time (1536 and 950 cycles a block of the contraction); narrow ones that leave pairs idle
+// The tiles whose waves over the pairs take less time (about 2000 and 1150 cycles a block of the contraction); narrow ones that leave pairs idle
 // have their contraction split, two blocks at least to a part, as long as all clusters run at once (counted on a B200: 74 pairs, 33
 // clusters of two, 16 of four).
 Cut cut_product(uint64_t batch, uint64_t rows, uint64_t cols, uint64_t k, bool symmetric) {
     const uint64_t pairs = (uint64_t)sm_count_now() / 2, blocks = (k + kBlock - 1) / kBlock;
     const uint64_t wide = count_tiles(batch, rows, cols, symmetric, 256), narrow = count_tiles(batch, rows, cols, symmetric, 128);
-    if ((wide + pairs - 1) / pairs * 1536 <= (narrow + pairs - 1) / pairs * 950) return {256, 1, wide};
+    if ((wide + pairs - 1) / pairs * 2000 <= (narrow + pairs - 1) / pairs * 1150) return {256, 1, wide};
     const uint32_t split = narrow <= 16 && blocks >= 8 ? 4 : narrow <= 33 && blocks >= 4 ? 2 : 1;
     return {128, split, narrow};
 }
@@ -568,7 +601,7 @@ Cut cut_product(uint64_t batch, uint64_t rows, uint64_t cols, uint64_t k, bool s
 uint64_t product_cycles(uint64_t batch, uint64_t rows, uint64_t cols, uint64_t k, bool symmetric) {
     const Cut cut = cut_product(batch, rows, cols, k, symmetric);
     const uint64_t pairs = (uint64_t)sm_count_now() / 2;
-    return (cut.tiles + pairs - 1) / pairs * ((k + kBlock - 1) / kBlock) * (cut.width == 256 ? 1536 : 950) / cut.split + 13000;
+    return (cut.tiles + pairs - 1) / pairs * ((k + kBlock - 1) / kBlock) * (cut.width == 256 ? 2000 : 1150) / cut.split + 13000;
 }
 template <int KIND, typename T> cudaError_t launch_product(const OrthoMaps& maps, const OrthoArgs& a, const Cut& cut, cudaStream_t st) {
     if (cut.width == 256) return launch_product_as<256, false, KIND, T>(maps, a, cut.tiles, st);
@@ -673,7 +706,7 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
             const auto symmetric = [&](auto kind, const Halves& p, const Halves& o, const Halves& d, uint64_t k, float scale) {
                 const Cut cut = cut_product(batch, s, s, k, true);
                 OrthoMaps m = {};
-                if (!make_maps(m.p, p, batch, 128) || !make_maps(m.q, o, batch, cut.width / 2) || !make_maps(m.d, d, batch, 0)) return cudaErrorNotSupported;
+                if (!make_maps(m.p, p, batch, 128) || !make_maps(m.q, o, batch, cut.width / 2) || !make_maps(m.d, d, batch, 0) || (cut.split > 1 && !make_maps(m.t, d, batch, 0))) return cudaErrorNotSupported;
                 args.rows = args.cols = s;
                 args.k = k;
                 args.pad_p = args.pad_q = args.pad_d = x.pad_rows;
@@ -716,7 +749,7 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
                 const Cut cut = final ? cut_product(batch, rows, cols, s, false) : cut_product(batch, s, l, s, false);
                 OrthoMaps m = {};
                 if (!make_maps(m.p, flip ? from : q[now], batch, 128) || !make_maps(m.q, flip ? q[now] : from, batch, cut.width / 2) ||
-                    (!final && !make_maps(m.d, x, batch, 0)))
+                    (!final && (!make_maps(m.d, x, batch, 0) || (cut.split > 1 && !make_maps(m.t, to, batch, 0)))))
                     return TNG_ERR_CUDA;
                 OrthoArgs last = args;
                 last.symmetric = 0;
@@ -741,13 +774,15 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
     // The products of a step: G = X X^T, B from G, X <- B X (the last one as the output lies: B X, or X^T B).
     const Cut cut_gram = cut_product(batch, s, s, l, true), cut_poly = cut_product(batch, s, s, s, true);
     const Cut cut_apply = cut_product(batch, s, l, s, false), cut_last = cut_product(batch, rows, cols, s, false);
-    const auto maps_of = [&](OrthoMaps& m, const Cut& cut, const Halves& p, const Halves& q, const Halves* d) {
-        return make_maps(m.p, p, batch, 128) && make_maps(m.q, q, batch, cut.width / 2) && (!d || make_maps(m.d, *d, batch, 0));
+    const auto maps_of = [&](OrthoMaps& m, const Cut& cut, const Halves& p, const Halves& q, const Halves* d, const Halves* t) {
+        return make_maps(m.p, p, batch, 128) && make_maps(m.q, q, batch, cut.width / 2) && (!d || make_maps(m.d, *d, batch, 0)) &&
+               (!t || cut.split == 1 || make_maps(m.t, *t, batch, 0));
     };
     OrthoMaps gram = {}, square = {}, apply[2] = {}, last = {};
     const Halves& xt_last = (steps - 1) & 1 ? xt2 : xt;
-    if (!maps_of(gram, cut_gram, x, x, &g) || !maps_of(square, cut_poly, g, g, &poly) || (steps > 1 && !maps_of(apply[0], cut_apply, poly, xt, &x)) ||
-        (steps > 2 && !maps_of(apply[1], cut_apply, poly, xt2, &x)) || !(tall ? maps_of(last, cut_last, xt_last, poly, nullptr) : maps_of(last, cut_last, poly, xt_last, nullptr)))
+    if (!maps_of(gram, cut_gram, x, x, &g, &g) || !maps_of(square, cut_poly, g, g, &poly, &poly) ||
+        (steps > 1 && !maps_of(apply[0], cut_apply, poly, xt, &x, &xt2)) || (steps > 2 && !maps_of(apply[1], cut_apply, poly, xt2, &x, &xt)) ||
+        !(tall ? maps_of(last, cut_last, xt_last, poly, nullptr, nullptr) : maps_of(last, cut_last, poly, xt_last, nullptr, nullptr)))
         return TNG_ERR_CUDA;
     OrthoArgs square_args = {};                            // of both symmetric products
     square_args.batch = (uint32_t)batch;
