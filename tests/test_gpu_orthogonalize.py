@@ -230,6 +230,18 @@ def test_part_of_an_aggregate():
     ctx.close()
 
 
+def test_offsets_beyond_32_bits():
+    ld = (1 << 30) + 64                                     # rows 4 GB apart
+    buf = torch.zeros(ld + 64, device="cuda")
+    far = buf.as_strided((2, 40), (ld, 1))
+    near = normal((2, 40))
+    far.copy_(near)
+    want = tng.orthogonalize(near)
+    assert torch.equal(tng.orthogonalize(far), want)
+    tng.orthogonalize(near, out=far)
+    assert torch.equal(far, want) and not buf[40:64].any()
+
+
 def test_refusals():
     v = normal((4, 8))
     with pytest.raises(ValueError):

@@ -403,6 +403,47 @@ def test_calls_on_two_streams_at_once():
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_embed_grad_of_a_long_batch():
+    """Chunks longer than what a block looks up at a time."""
+    tokens, vocab = 1300000, 50
+    dy, ids = normal((tokens, 5), torch.float32, 1), ids_of(tokens, vocab, 2, torch.int32)
+    embed_grad_check(dy, ids, vocab, 1.0, tng.embed_grad(dy, ids, vocab))
+
+
+def test_gradients_of_empty_places_may_be_anything():
+    dy, ids = normal((500, 96), torch.bfloat16, 1), ids_of(500, 40, 2)
+    ids[::7] = -1
+    want = tng.embed_grad(dy, ids, 40)
+    dy[ids < 0] = float("nan")
+    assert torch.equal(tng.embed_grad(dy, ids, 40), want)
+    want = tng.embed(dy, torch.full((3,), -1, device="cuda"))
+    assert not want.any()                                   # zeros, whatever the table holds
+
+
+def test_offsets_beyond_32_bits():
+    ld = (1 << 31) + 64                                     # elements of bf16: rows 4 GB apart
+    buf = torch.zeros(ld + 4096, dtype=torch.bfloat16, device="cuda")
+    far = buf.as_strided((2, 4096), (ld, 1))
+    far.copy_(normal((2, 4096), torch.bfloat16, 1))
+    near, w = far.contiguous(), 1 + normal((4096,), torch.float32, 2, 0.1)
+    ids = torch.tensor([1, 0, 1], device="cuda")
+    assert torch.equal(tng.embed(far, ids), near[ids])
+    assert all(torch.equal(a, b) for a, b in zip(tng.rmsnorm8(far, w), tng.rmsnorm8(near, w)))
+    r = tng.rmsnorm(near, w)[2]
+    assert all(torch.equal(a, b) for a, b in zip(tng.rmsnorm_grad(far, near, w, r), tng.rmsnorm_grad(near, near, w, r)))
+    assert torch.equal(tng.embed_grad(far, ids[:2], 3), tng.embed_grad(near, ids[:2], 3))
+    out = torch.empty_like(near)
+    tng.rmsnorm(near, w, y=far)
+    tng.rmsnorm(near, w, y=out)
+    assert torch.equal(far, out)
+    del buf, far
+    ld = (1 << 30) + 64                                     # of fp32
+    buf = torch.full((ld + 64,), 5.0, device="cuda")
+    d = buf.as_strided((2, 33), (ld, 1))
+    tng.embed_grad(near[:, :33], ids[:2], 2, dtable=d)
+    assert torch.equal(d, near[:, :33].float().flip(0)) and bool((buf[33:64] == 5).all()) and bool((buf[ld + 33:] == 5).all())
+
+
 def test_refusals():
     x, w = normal((4, 32), torch.bfloat16, 1), torch.ones(32, device="cuda")
     ids = torch.zeros(4, dtype=torch.int64, device="cuda")
