@@ -537,21 +537,6 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiled encode_tiled() {
-    static const EncodeTiled fn = [] {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            f = nullptr;
-        }
-        return reinterpret_cast<EncodeTiled>(f);
-    }();
-    return fn;
-}
 // The batch's matrices one below the other; boxes to load are 64 columns x `load` rows, boxes to store (load = 0) 32 x 32.
 bool make_map(CUtensorMap* map, const __half* m, const Halves& h, uint64_t batch, uint32_t load) {
     const EncodeTiled encode = encode_tiled();

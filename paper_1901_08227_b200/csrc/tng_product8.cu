@@ -783,21 +783,6 @@ __global__ void __launch_bounds__(kSlimThreads, 2)
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiled encode_tiled() {
-    static const EncodeTiled fn = [] {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            f = nullptr;
-        }
-        return reinterpret_cast<EncodeTiled>(f);
-    }();
-    return fn;
-}
 // `lines` lines of k codes, boxes of 128 codes x `box` lines; codes beyond a line's end read as zero.
 bool make_map(CUtensorMap* map, const int8_t* codes, uint64_t lines, uint64_t k, uint64_t ld, uint32_t box) {
     const EncodeTiled encode = encode_tiled();

@@ -177,4 +177,22 @@ __device__ __forceinline__ bool cluster_all_zero(uint32_t flag, uint32_t n) {
     return __all_sync(0xFFFFFFFFu, lane >= n || cluster_ld(cluster_map(flag, lane)) == 0);
 }
 
+// ---- tensor maps (host) ---------------------------------------------------------------------------
+// The driver's encoder, or nullptr where it cannot be had.
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+inline EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(f);
+    }();
+    return fn;
+}
+
 }  // namespace tng

@@ -315,6 +315,30 @@ def test_norm_grad_rows_that_start_anywhere(dtype, cols, lead, pad):
     assert untouched(views[3][1], dx) and bool((big[:3] == 7).all()) and bool((big[3 + cols:] == 7).all())
 
 
+@pytest.mark.parametrize("rows,cols", [(3, 100), (500, 64), (500, 1001), (500, 3000), (500, 16384), (40, 20000)])
+def test_outputs_that_are_left_out(rows, cols):
+    """The C calls' optional outputs, one by one."""
+    x, res, w = normal((rows, cols), torch.bfloat16, 1), normal((rows, cols), torch.bfloat16, 2), 1 + normal((cols,), torch.float32, 5, 0.1)
+    y = torch.empty_like(x)
+    q, s, h, r = tng.rmsnorm8(x, w, residual=res, y=y)
+    dx, dw = tng.rmsnorm_grad(x, h, w, r)
+    st = torch.cuda.current_stream().cuda_stream
+    L, P = tng.lib(), lambda t: t.data_ptr()
+    ldq = -(-cols // 16) * 16
+    for want in ("h", "y", "r", "q"):
+        out = {"h": torch.zeros_like(h), "y": torch.zeros_like(y), "r": torch.zeros_like(r), "q": tng.empty_codes(rows, cols)}[want]
+        scale = torch.zeros_like(s)
+        give = lambda n: P(out) if n == want else None
+        assert L.tng_rmsnorm(P(x), tng.BF16, rows, cols, cols, P(res), cols, P(w), 1e-6, give("h"), cols, give("y"), cols, give("q"), ldq,
+                             P(scale) if want == "q" else None, give("r"), st) == tng.OK
+        assert torch.equal(out, {"h": h, "y": y, "r": r, "q": q}[want]) and (want != "q" or torch.equal(scale, s))
+    scratch = torch.empty(L.tng_rmsnorm_grad_scratch_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    gx, gw = torch.zeros_like(dx), torch.zeros_like(dw)
+    assert L.tng_rmsnorm_grad(P(x), cols, P(h), cols, tng.BF16, rows, cols, P(w), P(r), None, 0, P(gx), cols, None, None, st) == tng.OK
+    assert L.tng_rmsnorm_grad(P(x), cols, P(h), cols, tng.BF16, rows, cols, P(w), P(r), None, 0, None, 0, P(gw), P(scratch), st) == tng.OK
+    assert torch.equal(gx, dx) and torch.equal(gw, dw)
+
+
 def test_norm_grad_by_differences():
     """The directional derivative of sum(y dy) in 64 bits, central differences with a step of 2^-12: off by step^2 times a third
     derivative (of the order of the gradient over h^2) and the rounding of the fp32 gradient."""
