@@ -131,8 +131,8 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const T* v, uint64_t l
 // tiles of one SM: 1580 cycles; they want 213 bytes a cycle of shared memory.)
 // SPLIT (256 x 128): a cluster of 2 or 4 pairs takes consecutive parts of one tile's contraction; each then adds the others' sums, read
 // from their shared memories, to its own for its share of the columns and writes those out.
-// Warps: 0-15 add up and write out (a quarter of the rows and of the columns each), 16 feeds, 17 and 18 issue, every other sum each: an
-// instruction takes its thread 54 cycles, a block with its waits and commits 1285, where the matrix unit takes 768 for 256 x 128.
+// Warps: 0-15 add up and write out (a quarter of the rows and of the columns each), 16 feeds, 17 issues.  256 x 128 unsplit: 17 and 18 issue
+// every other sum each: an instruction takes its thread 54 cycles, a block with its waits and commits 1285, the matrix unit 768.
 enum Kind { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
 constexpr int kThreads = 608;
 constexpr uint32_t kBox = 128 * 128, kBlock = 64;
@@ -146,7 +146,10 @@ template <uint32_t COLS, bool SPLIT> struct Geom {
     static constexpr uint32_t kChunk = COLS == 256 ? 2 : 1, kSums = 512 / COLS;
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
     static_assert(16 * kStages + 16 * kSums + 24 <= 256, "barriers");
-    static_assert(kSums % 2 == 0, "a sum's place belongs to one of the two issuing warps");
+    // A barrier's parity tells a phase only from its neighbours: a warp that waits for one phase has to have seen the one before.  So with two
+    // issuing warps every stage and every place of a sum belongs to one of them.
+    static constexpr uint32_t kIssuers = COLS == 128 && !SPLIT ? 2 : 1;
+    static_assert(kIssuers == 1 || (kChunk == 1 && kStages % kIssuers == 0 && kSums % kIssuers == 0), "a stage is waited for by one warp alone");
 };
 static_assert(128 * 128 * 4 <= Geom<128, true>::kStages * Geom<128, true>::kStage, "the stages also hold the sums");
 
@@ -388,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
             if (rank == 0) (void)mbar_wait(full(j % kStages), (j / kStages) & 1u);
             if (ok && !mbar_wait(empty(j % kStages), (j / kStages) & 1u)) ok = false;
         }
-    } else if (warp >= 17 && lane == 0 && rank == 0) {
+    } else if (warp >= 17 && warp < 17 + G::kIssuers && lane == 0 && rank == 0) {
         // ---- issue
         constexpr uint32_t idesc = umma_idesc_f16(256, COLS);
         const uint16_t both = (uint16_t)(3u << even);
@@ -398,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
         for (uint32_t t = unit; ok && t < tiles.count; t += units) {
             for (uint32_t k0 = 0; ok && k0 < blocks; k0 += kChunk, ++n_acc) {
                 const uint32_t acc = n_acc % kSums, use = n_acc / kSums, into = sh_tmem + acc * COLS, n = blocks - k0 < kChunk ? blocks - k0 : kChunk;
-                if ((n_acc & 1u) != mine) {
+                if (n_acc % G::kIssuers != mine) {
                     it += n;
                     continue;
                 }
@@ -428,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
         }
         // the hand-backs that nothing else waits for come from the other CTA too: they arrive before this one may leave
         for (uint32_t j = n_acc > kSums ? n_acc - kSums : 0; ok && j < n_acc; ++j)
-            if ((j & 1u) == mine) (void)mbar_wait(acc_empty + 8 * (j % kSums), (j / kSums) & 1u);
+            if (j % G::kIssuers == mine) (void)mbar_wait(acc_empty + 8 * (j % kSums), (j / kSums) & 1u);
     }
     __syncwarp();
     unsigned char* stage = stages + kStages * G::kStage + (SPLIT ? warp & 7 : warp) * G::kStaging;     // (of eight warps in a row eight write)
