@@ -131,16 +131,16 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const T* v, uint64_t l
 // tiles of one SM: 1580 cycles; they want 213 bytes a cycle of shared memory.)
 // SPLIT (256 x 128): a cluster of 2 or 4 pairs takes consecutive parts of one tile's contraction; each then adds the others' sums, read
 // from their shared memories, to its own for its share of the columns and writes those out.
-// Warps: 0-15 add up and write out (a quarter of the rows and of the columns each), 16 feeds, 17 issues.  256 x 128 unsplit: 17 and 18 issue
+// Warps: 0-15 add up and write out (a quarter of the rows and of the columns each), 16 feeds, 17 issues.  256 x 128: 17 and 18 issue
 // every other sum each: an instruction takes its thread 54 cycles, a block with its waits and commits 1285, the matrix unit 768.
 enum Kind { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
 constexpr int kThreads = 608;
 constexpr uint32_t kBox = 128 * 128, kBlock = 64;
 // (Stages of 32, twice as many, whose rows are 64 bytes: 2048 x 2048 x 8192 134 us instead of 113.)
-// Staging of the output: buffers of 2 KB, four a warp where at most eight warps write (SPLIT).
+// Staging of the output: buffers of 2 KB, two a warp where at most eight warps write (SPLIT).
 template <uint32_t COLS, bool SPLIT> struct Geom {
-    static constexpr uint32_t kQ = COLS / 2 * 128, kStage = 2 * kBox + 2 * kQ, kStages = COLS == 256 || SPLIT ? 3 : 4;
-    static constexpr uint32_t kBuffers = SPLIT ? 4 : 1, kStaging = 2048 * kBuffers;
+    static constexpr uint32_t kQ = COLS / 2 * 128, kStage = 2 * kBox + 2 * kQ, kStages = COLS == 256 ? 3 : 4;
+    static constexpr uint32_t kBuffers = SPLIT ? 2 : 1, kStaging = 2048 * kBuffers;
     static constexpr uint32_t kSmem = 1024 + kStages * kStage + (SPLIT ? 8 : 16) * kStaging + 256;
     // Blocks whose sum the tensor memory forms, and such sums under way: all of it.
     static constexpr uint32_t kChunk = COLS == 256 ? 2 : 1, kSums = 512 / COLS;
@@ -148,7 +148,7 @@ template <uint32_t COLS, bool SPLIT> struct Geom {
     static_assert(16 * kStages + 16 * kSums + 24 <= 256, "barriers");
     // A barrier's parity tells a phase only from its neighbours: a warp that waits for one phase has to have seen the one before.  So with two
     // issuing warps every stage and every place of a sum belongs to one of them.
-    static constexpr uint32_t kIssuers = COLS == 128 && !SPLIT ? 2 : 1;
+    static constexpr uint32_t kIssuers = COLS == 128 ? 2 : 1;
     static_assert(kIssuers == 1 || (kChunk == 1 && kStages % kIssuers == 0 && kSums % kIssuers == 0), "a stage is waited for by one warp alone");
 };
 static_assert(128 * 128 * 4 <= Geom<128, true>::kStages * Geom<128, true>::kStage, "the stages also hold the sums");
@@ -233,8 +233,8 @@ __device__ __forceinline__ void put_turned_staged(const CUtensorMap* map, const 
     if (lane == 0) tile_store(map, x, y, smem_u32(stage));
 }
 // The same, both halves, straight into memory: neighbouring lanes exchange a value, so that each stores two of one column, and 16
-// lanes 64 bytes.  Where staging is short (one buffer a warp) this is faster than copies (2048 x 8192 x 2048 186 -> 180 us), with four buffers
-// a warp it is slower (512 x 512, five steps: 146 -> 157 us).
+// lanes 64 bytes.  Where staging is short (one buffer a warp) this is faster than copies (2048 x 8192 x 2048 186 -> 180 us), with more it
+// is slower (512 x 512, five steps: 146 -> 157 us).
 template <uint32_t C, uint32_t N>
 __device__ __forceinline__ void put_turned(const Halves& t, const float (&v)[N], uint32_t b, uint64_t row0, uint64_t col, uint64_t rows, uint64_t cols, uint32_t lane) {
     const uint32_t odd = lane & 1;
@@ -294,10 +294,10 @@ __device__ __forceinline__ void finish(const OrthoMaps& maps, const OrthoArgs& a
         put_rows<false, C, BUFFERS>(&maps.d[0], sum, x, y, stage, lane);
         put_rows<true, C, BUFFERS>(&maps.d[1], sum, x, y, stage + (BUFFERS > 1 ? 2048 : 0), lane);
         if (mirrored) {
-            if constexpr (BUFFERS == 4) {
+            if constexpr (BUFFERS == 2) {
                 const int32_t xt = (int32_t)row0, yt = (int32_t)(b * a.t.pad_rows + col);
-                put_turned_staged<false, C, BUFFERS>(&maps.t[0], sum, xt, yt, stage + 4096, lane);
-                put_turned_staged<true, C, BUFFERS>(&maps.t[1], sum, xt, yt, stage + 6144, lane);
+                put_turned_staged<false, C, BUFFERS>(&maps.t[0], sum, xt, yt, stage, lane);
+                put_turned_staged<true, C, BUFFERS>(&maps.t[1], sum, xt, yt, stage + 2048, lane);
             } else {
                 put_turned<C>(a.t, sum, b, row0, col, a.rows, a.cols, lane);
             }
