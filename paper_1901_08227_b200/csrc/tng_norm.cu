@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const __grid_constant__
 // team's rows, a block its teams', and leaves that in `part`; a second kernel adds the blocks' shares, always in the same order.
 // 16384 x 4096 bf16 with dres: 90 us, 0.91 of the copy rate; 16384 x 1024: 39 us.
 // kStaged: a row is read from shared memory twice, before the meeting and after it, and its place is free once the team has met
-// again.  (G = 4 of the other modes has no room to keep it either.)
+// again.  (kApart with G = 4 has no room to keep it either.)
 template <typename T, Mode MODE, int G>
 __global__ void __launch_bounds__(512, MODE == kStaged ? 1 : 2) norm_grad_kernel(const __grid_constant__ NormGradArgs a) {
     constexpr bool STAGED = MODE == kStaged, VEC = MODE != kApart;
@@ -680,13 +680,17 @@ template <typename K> cudaError_t allow_rows(K kernel, PerDevice<bool>& done) {
     if (e == cudaSuccess && slot >= 0) done.v[slot] = true;
     return e;
 }
-// Calls f with a shape's mode and groups as types.
-template <class F> cudaError_t with_shape(const NormShape& s, F&& f) {
-    const auto groups = [&](auto mode) {
-        return s.groups == 1 ? f(mode, std::integral_constant<int, 1>()) : s.groups == 2 ? f(mode, std::integral_constant<int, 2>()) : f(mode, std::integral_constant<int, 4>());
-    };
-    return s.mode == kStaged ? groups(std::integral_constant<Mode, kStaged>()) : s.mode == kDirect ? groups(std::integral_constant<Mode, kDirect>())
-                                                                                                  : groups(std::integral_constant<Mode, kApart>());
+// Calls f with a shape's mode and groups as types; the most groups that each mode is used with.
+template <Mode MODE, int MOST, class F> cudaError_t with_groups(int groups, F&& f) {
+    const std::integral_constant<Mode, MODE> mode;
+    if (groups > MOST) return cudaErrorInvalidValue;       // (no shape asks for that)
+    if constexpr (MOST == 4) {
+        if (groups == 4) return f(mode, std::integral_constant<int, 4>());
+    }
+    return groups == 2 ? f(mode, std::integral_constant<int, 2>()) : f(mode, std::integral_constant<int, 1>());
+}
+template <int STAGED, int DIRECT, int APART, class F> cudaError_t with_shape(const NormShape& s, F&& f) {
+    return s.mode == kStaged ? with_groups<kStaged, STAGED>(s.groups, f) : s.mode == kDirect ? with_groups<kDirect, DIRECT>(s.groups, f) : with_groups<kApart, APART>(s.groups, f);
 }
 
 template <typename T> cudaError_t launch_norm(NormArgs a, cudaStream_t st) {
@@ -700,7 +704,7 @@ template <typename T> cudaError_t launch_norm(NormArgs a, cudaStream_t st) {
     else if (fits && a.cols > 1024 && !staged_shape(a.cols, e, arrays, 2, 512, 2, 1, shape)) (void)staged_shape(a.cols, e, arrays, 2, 1024, 1, 1, shape);
     a.stages = shape.stages;
     const uint64_t want = (a.rows + shape.block.y - 1) / shape.block.y, most = shape.per_sm * sms;
-    return with_shape(shape, [&](auto mode, auto g) {
+    return with_shape<2, 4, 2>(shape, [&](auto mode, auto g) {
         static PerDevice<bool> done;
         const auto kernel = norm_kernel<T, decltype(mode)::value, decltype(g)::value>;
         const cudaError_t err = allow_rows(kernel, done);
@@ -735,7 +739,7 @@ template <typename T> cudaError_t launch_norm_grad(NormGradArgs a, float* dw, cu
         a.arrays = shape.arrays;
         const uint64_t want = (a.rows + shape.block.y - 1) / shape.block.y, most = shape.per_sm * 148 < shares ? shape.per_sm * 148 : shares;
         shares = want < most ? want : most;
-        err = with_shape(shape, [&](auto mode, auto g) {
+        err = with_shape<4, 2, 4>(shape, [&](auto mode, auto g) {
             static PerDevice<bool> done;
             const auto kernel = norm_grad_kernel<T, decltype(mode)::value, decltype(g)::value>;
             const cudaError_t allowed = allow_rows(kernel, done);
