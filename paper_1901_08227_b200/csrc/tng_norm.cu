@@ -520,7 +520,9 @@ __global__ void __launch_bounds__(512, MODE == kStaged ? 1 : 2) norm_grad_kernel
     if (!a.part) return;
     float* out = a.part + (uint64_t)blockIdx.x * a.cols;
     if constexpr (STAGED) {
-        // each team's sums where its rows were (whose places hold four bytes a column at least), in the weights' order; then added up
+        // each team's sums where its rows were (whose places hold four bytes a column at least), in the weights' order; then added up.
+        // The last row is read up to here by all of the team: it meets before its place is written.
+        team_meet();
         const uint32_t held = n * G * 8, pitch = stages * a.arrays * held * (uint32_t)sizeof(T);
         unsigned char* rows = dyn + n * G * 32;
         float4* mine = reinterpret_cast<float4*>(rows + threadIdx.y * pitch);
