@@ -720,8 +720,9 @@ template <typename T> cudaError_t launch_norm_grad(NormGradArgs a, float* dw, cu
     uint64_t shares = grad_shares(a.rows, a.cols);
     cudaError_t err = cudaSuccess;
     if (a.cols > kHeld) {
-        if (a.dx) err = launch_layer(norm_grad_long_kernel<T>, (unsigned)(a.rows < 2 * sms ? a.rows : 2 * sms), 1024, 0, 1, st, a);
-        if (err == cudaSuccess && dw) err = launch_layer(norm_grad_long_dw_kernel<T>, dim3((a.cols + 255) / 256, (unsigned)shares), 256, 0, 1, st, a);
+        // dw first: dx may take the place of dy
+        if (dw) err = launch_layer(norm_grad_long_dw_kernel<T>, dim3((a.cols + 255) / 256, (unsigned)shares), 256, 0, 1, st, a);
+        if (err == cudaSuccess && a.dx) err = launch_layer(norm_grad_long_kernel<T>, (unsigned)(a.rows < 2 * sms ? a.rows : 2 * sms), 1024, 0, 1, st, a);
     } else {
         const bool fits = row_fits(a.dy, bytes, a.rows, a.lddy * e) && row_fits(a.h, bytes, a.rows, a.ldh * e) && row_fits(a.dres, bytes, a.rows, a.lddres * e) &&
                           row_fits(a.dx, bytes, a.rows, a.lddx * e);

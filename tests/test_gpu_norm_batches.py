@@ -76,3 +76,16 @@ def test_norm_grad(dtype, rows, cols):
                 a, b = dy.clone(), None if dres is None else dres.clone()
                 again = tng.rmsnorm_grad(a, h, w, r, dres=b, dx=a if into == "dy" else b)
                 assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 16400), (70, 16385), (200, 20000), (3, 100003)])
+def test_norm_grad_in_place_of_rows_longer_than_a_block_holds(dtype, rows, cols):
+    """dx and dw are two kernels there, and either reads dy."""
+    h, w = normal((rows, cols), dtype, 1, 2.0), 1 + normal((cols,), torch.float32, 5, 0.1)
+    dy, res = normal((rows, cols), dtype, 2, 0.1), normal((rows, cols), dtype, 3, 0.1)
+    r = torch.rsqrt(h.float().square().mean(1) + 1e-6)
+    for dres, into in ((None, "dy"), (res, "dy"), (res, "dres")):
+        a, b = dy.clone(), None if dres is None else dres.clone()
+        dx, dw = tng.rmsnorm_grad(a, h, w, r, dres=b, dx=a if into == "dy" else b)
+        grad_check(dy, h, w, r, dres, dx, dw)
