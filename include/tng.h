@@ -450,7 +450,8 @@ tng_status tng_rmsnorm_grad(const void* dy_dev, uint64_t lddy, const void* h_dev
  * The products run on the matrix unit with factors of 22 bits and fp32 sums; the result is rounded once to out_type.  A zero
  * matrix gives zeros, one that is not finite gives NaN throughout; neither touches its neighbours in the batch.
  * 1 <= steps <= 64; coefficients for which a singular value in (0, 1] could exceed 2, or its factor 15, in any of the steps are
- * refused (TNG_ERR_INVALID_ARG).  rows, cols < 2^30, batch <= 65535, batch times the rounded-up longer side below 2^31.
+ * refused (TNG_ERR_INVALID_ARG).  rows, cols < 2^30, the shorter side at most 4194240, batch <= 65535, batch times the rounded-up
+ * longer side below 2^31.
  * out must not overlap v.  scratch_dev: tng_orthogonalize_scratch_bytes, 256-byte aligned.  A bounded wait that gives up shows
  * as NaN in the outputs. */
 size_t tng_orthogonalize_scratch_bytes(uint64_t batch, uint64_t rows, uint64_t cols);

@@ -78,7 +78,8 @@ __device__ __forceinline__ void split(float v, __half& hi, __half& lo) {
     lo = __float2half_rn(__fsub_rn(v, __half2float(hi)));
 }
 
-// V / |V| in two halves, as it lies and transposed.  A block has 64 x 64 elements; they leave in pairs (rows are padded to 64).
+// V / |V| in two halves, as it lies and transposed.  A block has 64 x 64 elements; they leave in pairs (rows are padded to 64).  The blocks of the
+// longer side are counted by the grid's x: its y ends at 65535.
 template <typename T>
 __global__ void __launch_bounds__(256) ortho_split_kernel(const T* v, uint64_t ld, uint64_t stride, const double* part, const __grid_constant__ Halves as,
                                                           const __grid_constant__ Halves turned) {
@@ -87,7 +88,8 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const T* v, uint64_t l
     grid_wait();
     grid_go();
     const uint32_t b = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint64_t r0 = (uint64_t)blockIdx.y * 64, c0 = (uint64_t)blockIdx.x * 64;
+    const bool tall = as.rows > as.cols;
+    const uint64_t r0 = (uint64_t)(tall ? blockIdx.x : blockIdx.y) * 64, c0 = (uint64_t)(tall ? blockIdx.y : blockIdx.x) * 64;
     v += b * stride;
     float e[16];
 #pragma unroll
@@ -664,7 +666,7 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
     }
     if (batch == 0) return TNG_OK;
     const uint64_t s = rows < cols ? rows : cols, l = rows < cols ? cols : rows;
-    if (batch * up(l, 128) >= (1ull << 31) || (batch * up(s, 128) / 128) * (up(l, 128) / 128) >= (1ull << 31)) return TNG_ERR_INVALID_ARG;
+    if (s > 64 * 65535 || batch * up(l, 128) >= (1ull << 31) || (batch * up(s, 128) / 128) * (up(l, 128) / 128) >= (1ull << 31)) return TNG_ERR_INVALID_ARG;
     if (!matrix_ok(v_dev, type, cols, ldv) || !matrix_ok(out_dev, out_type, cols, ldo) || (batch > 1 && out_stride == 0) || !scratch_dev || !aligned(scratch_dev, 256)) return TNG_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     unsigned char* at = static_cast<unsigned char*>(scratch_dev);
@@ -678,7 +680,7 @@ tng_status tng_orthogonalize(const void* v_dev, tng_dtype type, uint64_t batch, 
         const T* v = static_cast<const T*>(v_dev);
         cudaError_t err = launch_layer(ortho_norm_kernel<T>, dim3(kNormBlocks, (unsigned)batch), kNormThreads, 0, 1, st, v, rows, cols, ldv, stride, part);
         if (err != cudaSuccess) return err;
-        const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)((rows + 63) / 64), (unsigned)batch);
+        const dim3 grid((unsigned)((l + 63) / 64), (unsigned)((s + 63) / 64), (unsigned)batch);
         return launch_layer(ortho_split_kernel<T>, grid, 256, 0, 1, st, v, ldv, stride, static_cast<const double*>(part), tall ? xt : x, tall ? x : xt);
     });
     if (e != cudaSuccess) return layer_status(e);
