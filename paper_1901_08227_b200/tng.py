@@ -651,6 +651,8 @@ def embed(table, ids, scale=1.0, dtype=None, out=None):
     pi, id_bytes, tokens = _ids(ids, dev)
     vocab, width = table.shape
     if out is None:
+        if dtype is not None and dtype not in _DTYPE:
+            raise TypeError(f"dtype must be float32, bfloat16 or float16, not {dtype}")
         out = table.new_empty((tokens, width), dtype=table.dtype if dtype is None else dtype)
         po, ldo = out.data_ptr(), width
     else:
