@@ -58,7 +58,42 @@ def dx_alone(dy, h, w, r, dres):
     return dx
 
 
+def norm_check(x, w, eps, residual, y, q, scale, h, r):
+    """h as stored, r and y in 64 bits; codes and their scale before r by fp32 steps."""
+    k = x.shape[1]
+    want_h = x if residual is None else (x.float() + residual.float()).to(x.dtype)
+    h64 = want_h.double()
+    want_r = 1.0 / (h64.square().mean(1) + eps).sqrt()
+    want_y = h64 * want_r[:, None] * w.double()
+    want_q, want_s = tng.quant8_rows(want_h.float() * w)    # (tested on its own)
+    assert torch.equal(h, want_h) and torch.equal(q, want_q)
+    rel = 1.01 * (k / 2 + 4) * U                            # the mean's sum, division, sum with eps: halved by the root; its rounding
+    close(r, want_r, rel * want_r)
+    # two products and the type's rounding (a step of its smallest number below that)
+    close(y, want_y, ((rel + 2.02 * U) * (1 + half(y.dtype)) + half(y.dtype)) * want_y.abs() + torch.finfo(y.dtype).smallest_normal * half(y.dtype))
+    close(scale, want_s.double() * want_r, (rel + 1.01 * U) * want_s.double() * want_r)
+
+
 BATCHES = [(300, 1028), (500, 1032), (1500, 1536), (300, 2048), (701, 2048), (500, 4096), (1500, 4096), (4096, 4096), (449, 8192), (1301, 8192), (600, 11264), (600, 16384)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", BATCHES + [(3000, 1032), (2500, 3000), (3001, 6016)])
+def test_norm(dtype, rows, cols):
+    x, residual, w = normal((rows, cols), dtype, cols), normal((rows, cols), dtype, cols + 1, 3.0), 1 + normal((cols,), torch.float32, 5, 0.1)
+    for res in (None, residual):
+        y8 = torch.empty_like(x)
+        q, s, h, r = tng.rmsnorm8(x, w, residual=res, y=y8)
+        norm_check(x, w, 1e-6, res, y8, q, s, h, r)
+        y, h2, r2 = tng.rmsnorm(x, w, residual=res)
+        assert torch.equal(y, y8) and torch.equal(h2, h) and torch.equal(r2, r)
+        for into in ("x", "residual"):
+            if into == "x" or res is not None:
+                a, b = x.clone(), None if res is None else res.clone()
+                q3, s3, h3, r3 = tng.rmsnorm8(a, w, residual=b, h=None if res is None else a if into == "x" else b)
+                assert torch.equal(h3, h) and torch.equal(r3, r) and torch.equal(q3, q) and torch.equal(s3, s)
+        a = x.clone()
+        assert torch.equal(tng.rmsnorm(a, w, residual=res, y=a)[0], y)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
