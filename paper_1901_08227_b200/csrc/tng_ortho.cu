@@ -416,11 +416,11 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_kernel(const __grid
                     const uint32_t at = data + s * G::kStage;
                     const uint64_t ph = umma_desc(at), pl = umma_desc(at + kBox), qh = umma_desc(at + 2 * kBox), ql = umma_desc(at + 2 * kBox + G::kQ);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) umma_f16<2>(into, ph + 2 * j, ql + 2 * j, idesc, kb > 0 || j > 0);
+                    for (int j = 0; j < 4; ++j) umma_f16_pair(into, ph + 2 * j, ql + 2 * j, idesc, kb > 0 || j > 0);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) umma_f16<2>(into, pl + 2 * j, qh + 2 * j, idesc, true);
+                    for (int j = 0; j < 4; ++j) umma_f16_pair(into, pl + 2 * j, qh + 2 * j, idesc, true);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) umma_f16<2>(into, ph + 2 * j, qh + 2 * j, idesc, true);
+                    for (int j = 0; j < 4; ++j) umma_f16_pair(into, ph + 2 * j, qh + 2 * j, idesc, true);
                     umma_commit_pair(empty(s), both);
                 }
                 if (ok) umma_commit_pair(acc_full + 8 * acc, both);

@@ -38,17 +38,11 @@ __device__ __forceinline__ void umma_s8(uint32_t tmem, uint64_t a, uint64_t b, u
                      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc),
                      "r"((uint32_t)accumulate) : "memory");
 }
-// The same over 16 fp16 values.
-template <int GROUP>
-__device__ __forceinline__ void umma_f16(uint32_t tmem, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    if constexpr (GROUP == 1)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc),
-                     "r"((uint32_t)accumulate) : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc),
-                     "r"((uint32_t)accumulate) : "memory");
+// The same over 16 fp16 values, of a pair of CTAs.
+__device__ __forceinline__ void umma_f16_pair(uint32_t tmem, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc),
+                 "r"((uint32_t)accumulate) : "memory");
 }
 // Arrive on a barrier when every instruction issued so far is done: this CTA's, or the same one of the CTAs of a mask.
 __device__ __forceinline__ void umma_commit(uint32_t bar) {
@@ -56,11 +50,6 @@ __device__ __forceinline__ void umma_commit(uint32_t bar) {
 }
 __device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint16_t ctas) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(ctas) : "memory");
-}
-// umma_commit or umma_commit_pair
-template <int GROUP> __device__ __forceinline__ void umma_commit_all(uint32_t bar, uint16_t ctas) {
-    if constexpr (GROUP == 1) umma_commit(bar);
-    else umma_commit_pair(bar, ctas);
 }
 __device__ __forceinline__ void umma_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void umma_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }

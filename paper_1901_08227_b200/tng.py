@@ -625,7 +625,7 @@ _ID_BYTES = {torch.int64: 8, torch.int32: 4}
 
 
 def _ids(t, dev):
-    """Token ids, any shape with contiguous memory -> (pointer, bytes an id, how many)."""
+    """Token ids, one-dimensional and contiguous -> (pointer, bytes an id, how many)."""
     if t.get_device() != dev or t.dtype not in _ID_BYTES:
         raise TypeError("ids must be an int64 or int32 tensor on the current CUDA device")
     if t.dim() != 1 or (t.shape[0] > 1 and t.stride(0) != 1):
