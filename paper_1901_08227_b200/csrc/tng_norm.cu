@@ -16,7 +16,14 @@
 //   kDirect   shorter ones: a team of 8, 16 or 32 lanes, which needs no barrier; an SM holds enough of them to keep memory busy (65536 x
 //             64 bf16 with a copy a row: 29 us)
 //   kApart    rows that start anywhere: single elements, neighbours by neighbouring lanes
-// The weights stay in shared memory.
+// The weights stay in shared memory.  The border at 1024 columns, 2^25 elements, kDirect / kStaged in us, bf16 and fp32 (codes with a residual; y;
+// gradient with dres):
+//   512     45 / 45, 74 / 72       29 / 31, 51 / 52       63 / 69, 93 / 97
+//   768     49 / 64, 72 / 74       29 / 45, 51 / 55       81 / 65, 99 / 114
+//   1024    41 / 47, 74 / 76       25 / 33, 49 / 55       69 / 56, 89 / 93
+//   1280    102 / 57, 115 / 74     78 / 39, 92 / 57       95 / 69, 112 / 99
+//   2048    64 / 47, 78 / 74       45 / 33, 64 / 55       71 / 54, 93 / 91
+// (16-bit gradients of 768 to 1024 columns would gain by the other side; one border serves all.)
 #include <math_constants.h>
 
 #include <type_traits>
@@ -292,8 +299,9 @@ template <bool VEC> struct Weights {
 };
 
 // ---- forward -----------------------------------------------------------------------------------------
-// blockDim.y teams of blockDim.x threads, G groups of eight elements a thread.  16384 x 8192 bf16 with a residual into codes: 152 us, 0.95 of
-// the copy rate, 161 in long runs; 65536 x 128: 20 us; rows that start anywhere, 16384 x 1001 fp32: 60 us, 3.5 TB/s.
+// blockDim.y teams of blockDim.x threads, G groups of eight elements a thread.  16384 x 8192 bf16 with a residual into codes: 154 us by itself, 161 to
+// 170 in long runs (0.89 to 0.84 of the copy rate); y alone 100 us (0.82); 65536 x 128 into codes: 20 us; rows that start anywhere, 16384 x 1001 with
+// a residual into codes: fp32 64 us, 3.3 TB/s, bf16 71 us, 1.6 TB/s.
 template <typename T, Mode MODE, int G>
 __global__ void __launch_bounds__(1024) norm_kernel(const __grid_constant__ NormArgs a) {
     constexpr bool STAGED = MODE == kStaged, VEC = MODE != kApart;
@@ -391,7 +399,7 @@ __global__ void __launch_bounds__(1024) norm_kernel(const __grid_constant__ Norm
     if constexpr (STAGED) rows_in.leave(stages);
 }
 
-// Rows longer than a block holds: read twice, the second time from the caches.  Where h is written it is what the second pass
+// Rows longer than a block holds: read twice, the second time from the caches (2048 x 20000 bf16 with a residual into codes: 150 us, 1.9 TB/s).  Where h is written it is what the second pass
 // reads (it may have replaced an input).
 template <typename T>
 __global__ void __launch_bounds__(1024) norm_long_kernel(const __grid_constant__ NormArgs a) {
@@ -437,7 +445,8 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const __grid_constant__
 // ---- gradient ----------------------------------------------------------------------------------------
 // With g = dy w: dx = r (g - h r^2 mean(g h)) + dres; dw = sum of dy h r over the rows.  A thread adds up dw of its columns over its
 // team's rows, a block its teams', and leaves that in `part`; a second kernel adds the blocks' shares, always in the same order.
-// 16384 x 4096 bf16 with dres: 90 us, 0.91 of the copy rate; 16384 x 1024: 39 us.
+// 16384 x 4096 bf16 with dres: 91 to 94 us, 0.9 of the copy rate; 16384 x 1024: 40 us; 8192 x 4096 fp32: 95 us, 0.86; rows that start anywhere, 16384 x
+// 1001: fp32 60 us, bf16 71.
 // kStaged: a row is read from shared memory twice, before the meeting and after it, and its place is free once the team has met
 // again.  (kApart with G = 4 has no room to keep it either.)
 template <typename T, Mode MODE, int G>
@@ -555,7 +564,7 @@ __global__ void __launch_bounds__(512, MODE == kStaged ? 1 : 2) norm_grad_kernel
     }
 }
 
-// Rows longer than a block holds, dx: read twice.
+// Rows longer than a block holds, dx: read twice (2048 x 20000 bf16 with dres and dw: 274 us, 1.2 TB/s; fp32 323).
 template <typename T>
 __global__ void __launch_bounds__(1024) norm_grad_long_kernel(const __grid_constant__ NormGradArgs a) {
     __shared__ RowSums sh;
@@ -627,7 +636,15 @@ struct NormShape {
     uint32_t stages, arrays;
 };
 constexpr uint64_t kMostSmem = 220 << 10;
-// Rows that each find an SM's room for themselves: as many threads as groups.
+// Rows that each find an SM's room for themselves: as many threads as groups.  In chains of launches (bf16, us, this way / the way of many rows):
+//             codes with a residual           gradient with dres
+//   columns   64 rows       296 rows          64 rows       296 rows
+//   512       3.0 / 2.6     3.1 / 2.7         7.8 / 5.5     8.4 / 5.8
+//   1536      2.6 / 3.5     2.9 / 3.6         5.8 / 6.0     7.1 / 6.3
+//   4096      2.9 / 3.6     3.9 / 3.8         6.4 / 7.5     8.5 / 8.3
+//   16384     5.5 / 5.9     8.6 / 8.7         15.2 / 15.1   27.8 / 20.1
+// It is for the rows of a layer's width, one to a few a call; short ones, and gradients of more rows than SMs, lose by it.  At 444 rows it is
+// slower at 4096 columns (5.5 / 5.0).
 bool few_rows(uint64_t rows) { return rows <= 2 * 148; }
 
 // Staged: of the cuts into `threads` threads that leave room for `least` rows a team, the one with the fewest instructions a row: a

@@ -5,7 +5,10 @@
 // computed, and written twice), then B X.  With s the shorter side and l the longer, 3 s^2 l + s^3 operations.
 //
 // Accuracy.  Every factor is held as two fp16 numbers, hi + lo, 22 bits together, times a power of two that keeps the bounds below in
-// fp16's range and its steps far below the entries; a product is three (hi lo, lo hi, hi hi), lo lo being below 2^-22 of it.
+// fp16's range; a product is three (hi lo, lo hi, hi hi), lo lo being below 2^-22 of it.  The scales are fixed, so that the smallest steps are 2^-38 of
+// |V| for X, 2^-37 and 2^-36 for G and B: 22 bits hold for entries of X from 2^-16 of |V| up, and a row or column far smaller than the
+// rest keeps fewer (256 x 512, five steps, 32 rows at 1e-4 of the others: off by 3.8e-6 of their norm, at 1e-6 3.7e-4, at 1e-8 3.7e-2; fp32
+// products 5.3e-7 throughout).  The error of the whole is below that of fp32 products (512 x 512: 1.5e-6 and 2.1e-6 of the norm).
 // (bf16 factors alone, 8 bits, would do for the singular values that are near one, but a step multiplies what lies in the
 // directions of the small ones by up to a: after five steps rounding noise of 2^-9 has grown by a factor of hundreds there.)  The tensor
 // memory's sums lose about half a step of fp32 with every instruction, all in one direction; so they run over one or two
@@ -13,9 +16,10 @@
 //
 // Long matrices with 16-bit results take several steps (up to kMostGroup) with one look at X: G after a step is B G B, so that only
 // products of the shorter side's size lie between G = X X^T and the product of the Bs, which X then takes at once: for m steps
-// 3 s^2 l + (4 m - 3) s^3 operations instead of 3 m s^2 l + m s^3 (4096 x 16384, five steps: 11.4 ms, so 6.4).  The rounding of B G B is
-// several times that of X X^T and takes the result's error from 1.1e-6 to 8.5e-6 of its norm: nothing beside bf16's 1.7e-3 or
-// fp16's 2e-4, but more than fp32 products throughout leave (2.9e-6), so results in fp32 go step by step.
+// 3 s^2 l + (4 m - 3) s^3 operations instead of 3 m s^2 l + m s^3 (4096 x 16384, five steps: 11.4 ms, so 6.3).  The rounding of B G B is
+// several times that of X X^T and takes the result's error before its rounding from 1.5e-6 to 1.1e-5 of its entries (1024 x 4096: from 1.9e-6 to
+// 6.0e-6): nothing beside bf16's 1.7e-3 or fp16's 2e-4, but more than fp32 products throughout leave (2.8e-6), so results in fp32 go step by
+// step.
 //
 // Bounds (checked on the host for the given coefficients): singular values of X at most 2, so entries of X at most 2, of G 4, and of B
 // 15; stored as X 2^14, G 2^13, B 2^12.
